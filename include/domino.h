@@ -267,6 +267,99 @@ DOMINO_API int domino_verify_tree_sample(const float* target_logits, const int32
                                          int B, int N, int V, int32_t* row_sample, int32_t* accepted_nodes,
                                          int32_t* accepted_count, int32_t* bonus_token, void* stream);
 
+/* Element types of the logits (and their gradients) that the entry points below take. */
+enum domino_dtype { DOMINO_F32 = 0, DOMINO_BF16 = 1, DOMINO_F16 = 2 };
+
+/* One token per row of logits after temperature, top-k, top-p and min-p, drawn with the caller's
+ * uniforms: the sampling rule of a target (or of a draft) that decodes with these filters.
+ * Per row: z = logits / T; ids ordered by (z descending, id ascending); of them
+ *   top_k: the first k stay (k < 1 or k >= V: all);
+ *   top_p: of those, the ones before which less than top_p of their mass lies (top_p >= 1 or NaN: all);
+ *   min_p: of those, the ones whose probability is at least min_p times the greatest (min_p <= 0 or
+ *          NaN: all);
+ *   the first id always stays.  The token is the first kept id, in id order, whose cumulative mass
+ *   exceeds u times the kept mass (u outside [0, 1), or NaN, is clamped to it).
+ * T <= 0 or NaN draws the first id (argmax, equal values: the lowest id).  Ids of logit -inf or NaN are
+ * never drawn; a row without any other gives id 0 and logp -inf; where logits are +inf, they share the
+ * mass evenly.  Sums are exact integers of 2^-44 of the greatest weight: the draw does not depend on the
+ * order in which they are formed, and borders (of top_p, of u) lie within about 1e-11 of the mass of
+ * where exact arithmetic puts them.
+ *   logits: device [rows, row_stride] of `dtype`, element-aligned; ids 0 .. V - 1 of a row are read,
+ *     row_stride >= V.  V <= 8 * 49152 (a row is staged in shared memory once).
+ *   temperature, top_p, min_p (fp32) and top_k (int32): device [rows], or NULL (T = 1, filter off).
+ *   uniforms: device fp32 [rows].
+ * Outputs (device): tokens int32 [rows]; logp fp32 [rows] or NULL: the token's log-probability among
+ *   the kept ids.
+ * One kernel on `stream`, no workspace; the tensors and the stream belong to the current device.
+ * Returns DOMINO_OK once enqueued, DOMINO_ERR_UNSUPPORTED for a larger V or another dtype, or another
+ * negative code (bad sizes or pointers, logits of another device) with nothing enqueued. */
+DOMINO_API int domino_sample_filtered(const void* logits, int dtype, int64_t row_stride, const float* temperature,
+                                      const int32_t* top_k, const float* top_p, const float* min_p,
+                                      const float* uniforms, int rows, int V, int32_t* tokens, float* logp,
+                                      void* stream);
+
+/* domino_verify_tree_sample for a target that decodes with top-k, top-p and min-p: every row's draw is
+ * domino_sample_filtered's, and the walk is the one on those draws, so that what is accepted is
+ * distributed as the filtered target's own samples.
+ *   target_logits: device [B * (N + 1), row_stride] of `dtype` (row b (N + 1): after the anchor of
+ *     sequence b; row b (N + 1) + i + 1: after its node i).
+ *   temperature, top_k, top_p, min_p: device [B], one entry per sequence, or NULL.
+ *   uniforms: device fp32 [B, N + 1].  tree_parent / tree_token: as for domino_verify_tree_greedy.
+ * Outputs (device): row_sample int32 [B, N + 1] and row_logp fp32 [B, N + 1] or NULL, every row's draw
+ *   and its log-probability; accepted_nodes [B, N], accepted_count [B] and bonus_token [B] as for
+ *   domino_verify_tree_greedy.
+ * Two kernels on `stream`, no workspace.  Returns as domino_sample_filtered. */
+DOMINO_API int domino_verify_tree_filtered(const void* target_logits, int dtype, int64_t row_stride,
+                                           const int32_t* tree_parent, const int32_t* tree_token,
+                                           const float* temperature, const int32_t* top_k, const float* top_p,
+                                           const float* min_p, const float* uniforms, int B, int N, int V,
+                                           int32_t* row_sample, float* row_logp, int32_t* accepted_nodes,
+                                           int32_t* accepted_count, int32_t* bonus_token, void* stream);
+
+/* Distillation of a teacher's top logits into rows of student logits, e.g. of the target's best kt
+ * tokens per draft position (the form of domino_draft_step's topk_ids / topk_logp) into the draft's
+ * final or base logits; the row weight carries the position decay exp(-k / gamma) of section 4.2 and
+ * leaves padding out (0).  Per row, with z = logits / T, p = softmax(z):
+ *   DOMINO_DISTILL_RENORM: q_j = softmax(scores / T) over the list; scores are the teacher's logits, or
+ *     log-probabilities up to a constant.  loss = weight * sum_j q_j (log q_j - log p[id_j]).
+ *   DOMINO_DISTILL_TAIL: scores are the teacher's log-probabilities at temperature T; q_j = exp(score_j),
+ *     and rest = max(0, 1 - sum_j q_j) belongs to all other ids together (0 where there is none):
+ *     loss = weight * (sum_j q_j (log q_j - log p[id_j]) + rest (log rest - log sum_{v not listed} p[v])).
+ *   gradient: d loss / d logits[v] * grad_loss = grad_loss weight / T * (p[v] - sum_{j: id_j = v} q_j)
+ *     for a listed v (and for every v without a tail), grad_loss weight / T * p[v] (1 - rest /
+ *     sum_{v' not listed} p[v']) for the others with one.  The loss is not scaled by T^2.
+ * Places of the list whose id lies outside [0, V) are empty; an id may stand in several places.  A row
+ * of weight 0 has loss and gradient 0, whatever its logits hold; a row whose logits are all -inf has
+ * loss +inf (0 where it is weighted 0, or teaches nothing).  Sums in fp32, in a fixed order.
+ *   logits: device [rows, row_stride] of `dtype`, element-aligned, finite or -inf; row_stride >= V;
+ *     V <= 8 * 49152.  teacher_ids int32 [rows, kt], teacher_scores fp32 [rows, kt] (finite or -inf),
+ *     1 <= kt <= 256.  weights fp32 [rows] or NULL (1); grad_loss fp32 [rows] or NULL (1): the upstream
+ *     gradient of the row's loss.  temperature > 0 with 1 / T finite in fp32.
+ * Outputs (device): loss fp32 [rows]; lse fp32 [rows, 2]: the log-sum-exp of z over every id and over
+ *   the ids not listed (-inf where there is none); dlogits [rows, grad_stride] of `dtype`,
+ *   grad_stride >= V, every id written, one rounding of the fp32 gradient; it may be the logits' own memory
+ *   with the same stride.
+ *   domino_distill_loss writes loss and lse (lse may be NULL); domino_distill_grad reads that lse and
+ *   writes dlogits; domino_distill_loss_grad writes all three in one pass over the logits (lse may be
+ *   NULL).
+ * One kernel on `stream`, no workspace; the tensors and the stream belong to the current device.
+ * Returns DOMINO_OK once enqueued, DOMINO_ERR_UNSUPPORTED for a larger V or kt or another dtype, or
+ * another negative code (bad sizes, pointers, temperature or mode, logits of another device) with
+ * nothing enqueued. */
+enum domino_distill_mode { DOMINO_DISTILL_RENORM = 0, DOMINO_DISTILL_TAIL = 1 };
+DOMINO_API int domino_distill_loss(const void* logits, int dtype, int64_t row_stride, const int32_t* teacher_ids,
+                                   const float* teacher_scores, const float* weights, float temperature, int mode,
+                                   int rows, int V, int kt, float* loss, float* lse, void* stream);
+DOMINO_API int domino_distill_grad(const void* logits, int dtype, int64_t row_stride, const int32_t* teacher_ids,
+                                   const float* teacher_scores, const float* weights, const float* grad_loss,
+                                   float temperature, int mode, int rows, int V, int kt, const float* lse,
+                                   void* dlogits, int64_t grad_stride, void* stream);
+DOMINO_API int domino_distill_loss_grad(const void* logits, int dtype, int64_t row_stride,
+                                        const int32_t* teacher_ids, const float* teacher_scores,
+                                        const float* weights, const float* grad_loss, float temperature, int mode,
+                                        int rows, int V, int kt, float* loss, float* lse, void* dlogits,
+                                        int64_t grad_stride, void* stream);
+
 /* The greedy sequential draft loop, the paper's inference loop (section 4.1.2 and Fig. 3: each
  * draft token is chosen from the final logits and becomes the causal encoder's next input), as
  * a variant of domino_draft_step for callers that do not have the prefix (V < 2^22, else
@@ -385,7 +478,9 @@ enum domino_kernel_kind {
   DOMINO_KERNEL_ROLLOUT = 7,      /* domino_rollout_*: the K sequential steps */
   DOMINO_KERNEL_VERIFY = 8,       /* domino_verify_tree_greedy / _sample: row argmax or draw, and
                                      tree walk */
-  DOMINO_KERNEL_KINDS = 9
+  DOMINO_KERNEL_SAMPLE = 9,       /* domino_sample_filtered, and domino_verify_tree_filtered with its walk */
+  DOMINO_KERNEL_DISTILL = 10,     /* domino_distill_* */
+  DOMINO_KERNEL_KINDS = 11
 };
 DOMINO_API int domino_timing_begin(int max_launches);
 DOMINO_API int domino_timing_end(float* total_ms, int* launches, int nkinds);

@@ -27,9 +27,19 @@ SYMBOLS = ("domino_workspace_bytes", "domino_draft_step", "domino_workspace_byte
            "domino_draft_step_static_scratch", "domino_verify_tree_greedy", "domino_rollout_workspace_bytes",
            "domino_rollout_greedy", "domino_rollout_sample", "domino_input_table_bytes",
            "domino_build_input_table", "domino_launches_per_step_table", "domino_debug_hold",
-           "domino_verify_tree_sample", "domino_rollout_sample_gumbel")
+           "domino_verify_tree_sample", "domino_rollout_sample_gumbel", "domino_sample_filtered",
+           "domino_verify_tree_filtered", "domino_distill_loss", "domino_distill_grad", "domino_distill_loss_grad")
 
 DOMINO_STATIC_SCRATCH_BYTES = 16 << 20
+
+# element types of logits (domino_sample_filtered, domino_verify_tree_filtered, domino_distill_*)
+DOMINO_F32 = 0
+DOMINO_BF16 = 1
+DOMINO_F16 = 2
+
+# domino_distill_*: what stands for the ids outside the teacher's list
+DOMINO_DISTILL_RENORM = 0
+DOMINO_DISTILL_TAIL = 1
 
 # domino_debug_hold: what a GRU CTA withholds (a failure-detection test hook)
 DOMINO_HOLD_OFF = 0
@@ -38,7 +48,7 @@ DOMINO_HOLD_CLEAR_BARRIER = 2
 DOMINO_HOLD_ROW_COPY = 3
 
 KERNEL_KINDS = ("gather", "gru_input_proj", "w1_hidden_proj", "gru", "vocab_gemm_softmax_topk", "merge_tree",
-                "rollout_base_gemm", "rollout_steps", "tree_verify")
+                "rollout_base_gemm", "rollout_steps", "tree_verify", "sample_filtered", "distill")
 
 
 class domino_head_weights(ctypes.Structure):
@@ -113,6 +123,17 @@ def load():
     lib.domino_build_input_table.restype = I
     lib.domino_debug_hold.argtypes = [I, I, I]
     lib.domino_debug_hold.restype = I
+    L, F = ctypes.c_int64, ctypes.c_float
+    lib.domino_sample_filtered.argtypes = [P, I, L, P, P, P, P, P, I, I, P, P, P]
+    lib.domino_sample_filtered.restype = I
+    lib.domino_verify_tree_filtered.argtypes = [P, I, L, P, P, P, P, P, P, P, I, I, I, P, P, P, P, P, P]
+    lib.domino_verify_tree_filtered.restype = I
+    lib.domino_distill_loss.argtypes = [P, I, L, P, P, P, F, I, I, I, I, P, P, P]
+    lib.domino_distill_loss.restype = I
+    lib.domino_distill_grad.argtypes = [P, I, L, P, P, P, P, F, I, I, I, I, P, P, L, P]
+    lib.domino_distill_grad.restype = I
+    lib.domino_distill_loss_grad.argtypes = [P, I, L, P, P, P, P, F, I, I, I, I, P, P, P, L, P]
+    lib.domino_distill_loss_grad.restype = I
     _lib = lib
     return lib
 
@@ -242,6 +263,54 @@ def domino_verify_tree_sample(target_logits, tree_parent, tree_token, uniforms, 
                                                 _addr(uniforms), float(temperature), B, N, V, _addr(row_sample),
                                                 _addr(accepted_nodes), _addr(accepted_count), _addr(bonus_token),
                                                 _stream(stream)))
+
+
+def domino_sample_filtered(logits, dtype, row_stride, temperature, top_k, top_p, min_p, uniforms, rows, V, tokens,
+                           logp=None, stream=None) -> int:
+    """One token per row of ``logits`` [rows, row_stride] after temperature, top-k, top-p and min-p (device
+    arrays [rows] or None), drawn with ``uniforms`` fp32 [rows]; logp: its log-probability among the kept ids."""
+    return int(load().domino_sample_filtered(_addr(logits), int(dtype), int(row_stride), _addr(temperature),
+                                             _addr(top_k), _addr(top_p), _addr(min_p), _addr(uniforms), rows, V,
+                                             _addr(tokens), _addr(logp), _stream(stream)))
+
+
+def domino_verify_tree_filtered(target_logits, dtype, row_stride, tree_parent, tree_token, temperature, top_k, top_p,
+                                min_p, uniforms, B, N, V, row_sample, row_logp, accepted_nodes, accepted_count,
+                                bonus_token, stream=None) -> int:
+    """Verification of B draft trees against a target that decodes with the filters of domino_sample_filtered
+    (settings [B] per sequence or None): logits [B (N + 1), row_stride], one uniform per row."""
+    return int(load().domino_verify_tree_filtered(_addr(target_logits), int(dtype), int(row_stride),
+                                                  _addr(tree_parent), _addr(tree_token), _addr(temperature),
+                                                  _addr(top_k), _addr(top_p), _addr(min_p), _addr(uniforms), B, N, V,
+                                                  _addr(row_sample), _addr(row_logp), _addr(accepted_nodes),
+                                                  _addr(accepted_count), _addr(bonus_token), _stream(stream)))
+
+
+def domino_distill_loss(logits, dtype, row_stride, teacher_ids, teacher_scores, weights, temperature, mode, rows, V,
+                        kt, loss, lse=None, stream=None) -> int:
+    """Loss of every row of student logits against the teacher's list of kt ids and scores, and the two
+    log-sum-exps [rows, 2] that domino_distill_grad takes."""
+    return int(load().domino_distill_loss(_addr(logits), int(dtype), int(row_stride), _addr(teacher_ids),
+                                          _addr(teacher_scores), _addr(weights), float(temperature), int(mode), rows,
+                                          V, kt, _addr(loss), _addr(lse), _stream(stream)))
+
+
+def domino_distill_grad(logits, dtype, row_stride, teacher_ids, teacher_scores, weights, grad_loss, temperature, mode,
+                        rows, V, kt, lse, dlogits, grad_stride, stream=None) -> int:
+    """Gradient of domino_distill_loss by the logits, times ``grad_loss`` [rows] (None: 1)."""
+    return int(load().domino_distill_grad(_addr(logits), int(dtype), int(row_stride), _addr(teacher_ids),
+                                          _addr(teacher_scores), _addr(weights), _addr(grad_loss), float(temperature),
+                                          int(mode), rows, V, kt, _addr(lse), _addr(dlogits), int(grad_stride),
+                                          _stream(stream)))
+
+
+def domino_distill_loss_grad(logits, dtype, row_stride, teacher_ids, teacher_scores, weights, grad_loss, temperature,
+                             mode, rows, V, kt, loss, lse, dlogits, grad_stride, stream=None) -> int:
+    """domino_distill_loss and domino_distill_grad in one pass over the logits."""
+    return int(load().domino_distill_loss_grad(_addr(logits), int(dtype), int(row_stride), _addr(teacher_ids),
+                                               _addr(teacher_scores), _addr(weights), _addr(grad_loss),
+                                               float(temperature), int(mode), rows, V, kt, _addr(loss), _addr(lse),
+                                               _addr(dlogits), int(grad_stride), _stream(stream)))
 
 
 def domino_rollout_workspace_bytes(B, K, H, V, Ds, R) -> int:

@@ -931,6 +931,166 @@ int domino_verify_tree_sample(const float* target_logits, const int32_t* tree_pa
   return rc;
 }
 
+// ---------------------------------------------------------------- rows of logits: draws, distillation
+static_assert(dm::kF32 == DOMINO_F32 && dm::kBf16 == DOMINO_BF16 && dm::kF16 == DOMINO_F16, "element types");
+
+namespace {
+bool aligned(const void* p, size_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
+
+// What every entry point on rows of logits asks of them; `rows` CTA clusters are launched.
+int check_rows(const void* logits, int dtype, int64_t stride, long long rows, int V) {
+  if (!logits || rows < 1 || V < 1 || stride < V) return DOMINO_ERR_INVALID_ARG;
+  if (rows > 0x7fffffffLL / 8) return DOMINO_ERR_INVALID_ARG;
+  if (dtype != DOMINO_F32 && dtype != DOMINO_BF16 && dtype != DOMINO_F16) return DOMINO_ERR_UNSUPPORTED;
+  if (V > dm::kMaxRowVocab) return DOMINO_ERR_UNSUPPORTED;
+  const size_t size = dtype == DOMINO_F32 ? 4 : 2;
+  // the last row's end stays addressable
+  if (stride > static_cast<int64_t>((1LL << 62) / size) / rows) return DOMINO_ERR_INVALID_ARG;
+  return aligned(logits, size) ? DOMINO_OK : DOMINO_ERR_INVALID_ARG;
+}
+
+// The logits lie on the current device (whose stream the caller gives), an sm_103.
+int check_device(const void* logits) {
+  int sms = 0, major = 0, minor = 0, dev = 0;
+  const int rc = device_sms(&sms, &major, &minor);
+  if (rc != DOMINO_OK) return rc;
+  if (major != 10 || minor != 3) return DOMINO_ERR_UNSUPPORTED;
+  cudaPointerAttributes at{};
+  if (cudaGetDevice(&dev) != cudaSuccess || cudaPointerGetAttributes(&at, logits) != cudaSuccess) return DOMINO_ERR_CUDA;
+  return at.type == cudaMemoryTypeDevice && at.device != dev ? DOMINO_ERR_INVALID_ARG : DOMINO_OK;
+}
+
+int enqueue_draw(const dm::DrawParams& d, int dtype, long long rows, cudaStream_t st) {
+  return cuda_rc(dm::launch_filtered_draw(d, dtype, static_cast<int>(rows), st));
+}
+
+int run_distill(const void* logits, int dtype, int64_t row_stride, const int32_t* teacher_ids,
+                const float* teacher_scores, const float* weights, const float* grad_loss, float temperature, int mode,
+                int rows, int V, int kt, float* loss, float* lse, void* dlogits, int64_t grad_stride, void* stream) {
+  int rc = check_rows(logits, dtype, row_stride, rows, V);
+  if (rc != DOMINO_OK) return rc;
+  if (!teacher_ids || !teacher_scores || kt < 1) return DOMINO_ERR_INVALID_ARG;
+  if (!aligned(teacher_ids, 4) || !aligned(teacher_scores, 4) || !aligned(weights, 4) || !aligned(grad_loss, 4) ||
+      !aligned(loss, 4) || !aligned(lse, 4))
+    return DOMINO_ERR_INVALID_ARG;
+  const float inv_t = 1.0f / temperature;
+  if (!(temperature > 0.f) || !std::isfinite(temperature) || !std::isfinite(inv_t)) return DOMINO_ERR_INVALID_ARG;
+  if (mode != DOMINO_DISTILL_RENORM && mode != DOMINO_DISTILL_TAIL) return DOMINO_ERR_INVALID_ARG;
+  if (kt > dm::kMaxTeacher) return DOMINO_ERR_UNSUPPORTED;
+  if (dlogits) {
+    rc = check_rows(dlogits, dtype, grad_stride, rows, V);
+    if (rc != DOMINO_OK) return rc;
+    if (dlogits == logits && grad_stride != row_stride) return DOMINO_ERR_INVALID_ARG;
+  }
+  rc = check_device(logits);
+  if (rc != DOMINO_OK) return rc;
+  dm::DistillParams d{};
+  d.logits = logits; d.stride = row_stride;
+  d.V = V; d.kt = kt;
+  d.ids = teacher_ids; d.scores = teacher_scores; d.weights = weights; d.grad_loss = grad_loss;
+  d.inv_t = inv_t;
+  d.k2 = static_cast<float>(1.4426950408889634 / static_cast<double>(temperature));
+  d.tail = mode == DOMINO_DISTILL_TAIL;
+  d.loss = loss; d.lse = lse;
+  d.dlogits = dlogits; d.grad_stride = grad_stride;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const int ts = timing_open(DOMINO_KERNEL_DISTILL, st);
+  rc = cuda_rc(dm::launch_distill(d, dtype, rows, st));
+  timing_close(ts, st);
+  return rc;
+}
+}  // namespace
+
+int domino_sample_filtered(const void* logits, int dtype, int64_t row_stride, const float* temperature,
+                           const int32_t* top_k, const float* top_p, const float* min_p, const float* uniforms,
+                           int rows, int V, int32_t* tokens, float* logp, void* stream) try {
+  int rc = check_rows(logits, dtype, row_stride, rows, V);
+  if (rc != DOMINO_OK) return rc;
+  if (!uniforms || !tokens) return DOMINO_ERR_INVALID_ARG;
+  if (!aligned(temperature, 4) || !aligned(top_k, 4) || !aligned(top_p, 4) || !aligned(min_p, 4) ||
+      !aligned(uniforms, 4) || !aligned(tokens, 4) || !aligned(logp, 4))
+    return DOMINO_ERR_INVALID_ARG;
+  rc = check_device(logits);
+  if (rc != DOMINO_OK) return rc;
+  dm::DrawParams d{};
+  d.logits = logits; d.stride = row_stride; d.V = V; d.rows_per_set = 1;
+  d.temperature = temperature; d.top_k = top_k; d.top_p = top_p; d.min_p = min_p;
+  d.uniforms = uniforms; d.tokens = tokens; d.logp = logp;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const int ts = timing_open(DOMINO_KERNEL_SAMPLE, st);
+  rc = enqueue_draw(d, dtype, rows, st);
+  timing_close(ts, st);
+  return rc;
+} catch (...) {
+  return DOMINO_ERR_CUDA;
+}
+
+int domino_verify_tree_filtered(const void* target_logits, int dtype, int64_t row_stride, const int32_t* tree_parent,
+                                const int32_t* tree_token, const float* temperature, const int32_t* top_k,
+                                const float* top_p, const float* min_p, const float* uniforms, int B, int N, int V,
+                                int32_t* row_sample, float* row_logp, int32_t* accepted_nodes,
+                                int32_t* accepted_count, int32_t* bonus_token, void* stream) try {
+  if (B < 1 || N < 0 || N > (1 << 20)) return DOMINO_ERR_INVALID_ARG;
+  const long long rows = static_cast<long long>(B) * (N + 1);
+  int rc = check_rows(target_logits, dtype, row_stride, rows, V);
+  if (rc != DOMINO_OK) return rc;
+  if (!uniforms || !row_sample || !accepted_count || !bonus_token) return DOMINO_ERR_INVALID_ARG;
+  if (N > 0 && (!tree_parent || !tree_token || !accepted_nodes)) return DOMINO_ERR_INVALID_ARG;
+  if (!aligned(temperature, 4) || !aligned(top_k, 4) || !aligned(top_p, 4) || !aligned(min_p, 4) ||
+      !aligned(uniforms, 4) || !aligned(row_sample, 4) || !aligned(row_logp, 4) || !aligned(tree_parent, 4) ||
+      !aligned(tree_token, 4) || !aligned(accepted_nodes, 4) || !aligned(accepted_count, 4) ||
+      !aligned(bonus_token, 4))
+    return DOMINO_ERR_INVALID_ARG;
+  rc = check_device(target_logits);
+  if (rc != DOMINO_OK) return rc;
+  dm::DrawParams d{};
+  d.logits = target_logits; d.stride = row_stride; d.V = V; d.rows_per_set = static_cast<unsigned>(N) + 1;
+  d.temperature = temperature; d.top_k = top_k; d.top_p = top_p; d.min_p = min_p;
+  d.uniforms = uniforms; d.tokens = row_sample; d.logp = row_logp;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const int ts = timing_open(DOMINO_KERNEL_SAMPLE, st);
+  rc = enqueue_draw(d, dtype, rows, st);
+  if (rc == DOMINO_OK)
+    rc = cuda_rc(dm::launch_walk(tree_parent, tree_token, row_sample, B, N, accepted_nodes, accepted_count,
+                                 bonus_token, st));
+  timing_close(ts, st);
+  return rc;
+} catch (...) {
+  return DOMINO_ERR_CUDA;
+}
+
+int domino_distill_loss(const void* logits, int dtype, int64_t row_stride, const int32_t* teacher_ids,
+                        const float* teacher_scores, const float* weights, float temperature, int mode, int rows,
+                        int V, int kt, float* loss, float* lse, void* stream) try {
+  if (!loss) return DOMINO_ERR_INVALID_ARG;
+  return run_distill(logits, dtype, row_stride, teacher_ids, teacher_scores, weights, nullptr, temperature, mode, rows,
+                     V, kt, loss, lse, nullptr, 0, stream);
+} catch (...) {
+  return DOMINO_ERR_CUDA;
+}
+
+int domino_distill_grad(const void* logits, int dtype, int64_t row_stride, const int32_t* teacher_ids,
+                        const float* teacher_scores, const float* weights, const float* grad_loss, float temperature,
+                        int mode, int rows, int V, int kt, const float* lse, void* dlogits, int64_t grad_stride,
+                        void* stream) try {
+  if (!lse || !dlogits) return DOMINO_ERR_INVALID_ARG;
+  return run_distill(logits, dtype, row_stride, teacher_ids, teacher_scores, weights, grad_loss, temperature, mode,
+                     rows, V, kt, nullptr, const_cast<float*>(lse), dlogits, grad_stride, stream);
+} catch (...) {
+  return DOMINO_ERR_CUDA;
+}
+
+int domino_distill_loss_grad(const void* logits, int dtype, int64_t row_stride, const int32_t* teacher_ids,
+                             const float* teacher_scores, const float* weights, const float* grad_loss,
+                             float temperature, int mode, int rows, int V, int kt, float* loss, float* lse,
+                             void* dlogits, int64_t grad_stride, void* stream) try {
+  if (!loss || !dlogits) return DOMINO_ERR_INVALID_ARG;
+  return run_distill(logits, dtype, row_stride, teacher_ids, teacher_scores, weights, grad_loss, temperature, mode,
+                     rows, V, kt, loss, lse, dlogits, grad_stride, stream);
+} catch (...) {
+  return DOMINO_ERR_CUDA;
+}
+
 // ---------------------------------------------------------------- input-projection table
 namespace {
 __device__ int g_table_status;  // device status of domino_build_input_table's GEMM

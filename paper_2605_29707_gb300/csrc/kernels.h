@@ -252,5 +252,48 @@ void arm_row_hold(int row);
 cudaError_t launch_verify_sample(const float* logits, const int32_t* parent, const int32_t* token,
                                  const float* uniforms, int B, int N, int V, float inv_t, int32_t* row_sample,
                                  int32_t* nodes, int32_t* count, int32_t* bonus, cudaStream_t stream);
+// The walk alone on given row choices, a programmatic dependent of the kernel before it on the stream.
+cudaError_t launch_walk(const int32_t* parent, const int32_t* token, const int32_t* row_choice, int B, int N,
+                        int32_t* nodes, int32_t* count, int32_t* bonus, cudaStream_t stream);
+
+// ---------------------------------------------------------------- rows of logits (sample.cu, distill.cu)
+// Element types; numerically equal to enum domino_dtype.
+constexpr int kF32 = 0, kBf16 = 1, kF16 = 2;
+constexpr int kMaxRowVocab = 8 * 49152;  // ids of a row: eight slices that shared memory holds
+constexpr int kMaxTeacher = 256;         // places of a teacher's list
+
+struct DrawParams {
+  const void* logits;        // [rows][stride]
+  long long stride;
+  int V;
+  unsigned rows_per_set;     // consecutive rows that share one entry of the settings
+  const float* temperature;  // settings: nullptr = off
+  const int32_t* top_k;
+  const float* top_p;
+  const float* min_p;
+  const float* uniforms;     // [rows]
+  int32_t* tokens;           // [rows]
+  float* logp;               // [rows] or nullptr
+  int slice;                 // set by the launch: ids per CTA
+};
+cudaError_t launch_filtered_draw(DrawParams p, int dtype, int rows, cudaStream_t stream);
+
+struct DistillParams {
+  const void* logits;  // [rows][stride]
+  long long stride;
+  int V, kt;
+  const int32_t* ids;    // [rows][kt], -1: empty
+  const float* scores;   // [rows][kt]
+  const float* weights;  // [rows] or nullptr (1)
+  const float* grad_loss;  // [rows] or nullptr (1)
+  float inv_t, k2;       // 1 / T, log2(e) / T
+  int tail;              // the ids not listed share one bucket of the teacher's remaining mass
+  float* loss;           // [rows]; nullptr: the gradient alone, from lse
+  float* lse;            // [rows][2]: log-sum-exp of z over every id, over the ids not listed
+  void* dlogits;         // [rows][grad_stride] or nullptr
+  long long grad_stride;
+  int slice;             // set by the launch: ids per CTA
+};
+cudaError_t launch_distill(DistillParams p, int dtype, int rows, cudaStream_t stream);
 
 }  // namespace dm

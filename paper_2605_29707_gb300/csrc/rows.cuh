@@ -1,0 +1,135 @@
+// rows.cuh -- building blocks of the kernels that work on rows of vocabulary logits held across a
+// cluster of CTAs (sample.cu, distill.cu): element types, staging of a row slice in shared memory,
+// and reductions and scans over a block and over the cluster.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <math.h>
+
+#include "kernels.h"
+#include "ptx.cuh"
+
+namespace dm {
+
+constexpr int kRowSplit = 8;  // CTAs (one cluster) per row
+
+// ------------------------------------------------------------------ element types
+__device__ __forceinline__ float to_f32(float x) { return x; }
+__device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162float(x); }
+__device__ __forceinline__ float to_f32(__half x) { return __half2float(x); }
+
+// One rounding, to nearest even, of a value computed in fp32 to the element type.
+__device__ __forceinline__ void from_f32(float v, float* out) { *out = v; }
+__device__ __forceinline__ void from_f32(float v, __nv_bfloat16* out) { *out = __float2bfloat16_rn(v); }
+__device__ __forceinline__ void from_f32(float v, __half* out) { *out = __float2half_rn(v); }
+
+template <typename T>
+struct Vec {  // 16 bytes of elements
+  static constexpr int kN = 16 / sizeof(T);
+  union {
+    uint4 raw;
+    T e[kN];
+  };
+  __device__ __forceinline__ Vec() {}
+};
+
+// ------------------------------------------------------------------ staging
+// Elements [0, len) of `src` come to rest at s[shift .. shift + len), where `shift` is the number of
+// elements between the 16-byte boundary below src and src itself, so that whole 16-byte units of
+// global memory are whole units of shared memory whatever the row's alignment.  The units that lie
+// wholly inside the range are copied asynchronously (cp.async, 16 bytes a thread, committed as one
+// group); the first and the last few elements, whose units hold what is not the row's, are read one
+// by one.  The rest of those two units is -inf (an element that carries no weight).
+template <typename T>
+__device__ __forceinline__ int row_shift(const T* src) {
+  return static_cast<int>((reinterpret_cast<uintptr_t>(src) & 15) / sizeof(T));
+}
+
+// 16-byte units that hold a staged slice.
+template <typename T>
+__device__ __forceinline__ int row_units(int shift, int len) {
+  return len > 0 ? (shift + len + Vec<T>::kN - 1) / Vec<T>::kN : 0;
+}
+
+__device__ __forceinline__ void cp_async16(void* dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16;" ::"r"(smem_u32(dst)), "l"(src) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void cp_async_wait_all() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+
+template <typename T, int THREADS>
+__device__ __forceinline__ void stage_slice(T* s, const T* src, int len, int tid) {
+  constexpr int N = Vec<T>::kN;
+  const int shift = row_shift(src);
+  const int first = shift ? 1 : 0;          // first whole unit
+  const int last = (shift + len) / N;       // one past the last whole unit
+  const T* base = src - shift;              // 16-byte boundary; only whole units are read from it
+  for (int q = first + tid; q < last; q += THREADS) cp_async16(s + q * N, base + static_cast<size_t>(q) * N);
+  cp_async_commit();
+  const int units = row_units<T>(shift, len);
+  T none;
+  from_f32(-INFINITY, &none);
+  if (len > 0) {
+    if (first && tid < N) s[tid] = tid >= shift && tid < shift + len ? src[tid - shift] : none;
+    if (units > last && !(first && last == 0) && tid >= 32 && tid < 32 + N) {
+      const int i = last * N + tid - 32;
+      s[i] = i < shift + len ? src[i - shift] : none;
+    }
+  }
+}
+
+// ------------------------------------------------------------------ clusters
+__device__ __forceinline__ uint32_t ld_cluster(const uint32_t* local, uint32_t rank) {
+  return ld_cluster_u32(cluster_addr(local, rank));
+}
+__device__ __forceinline__ float ld_cluster(const float* local, uint32_t rank) {
+  return __uint_as_float(ld_cluster_u32(cluster_addr(local, rank)));
+}
+__device__ __forceinline__ unsigned long long ld_cluster(const unsigned long long* local, uint32_t rank) {
+  unsigned long long v;
+  asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(cluster_addr(local, rank)) : "memory");
+  return v;
+}
+
+// ------------------------------------------------------------------ block reductions and scans
+__device__ __forceinline__ float warp_max(float v) {
+#pragma unroll
+  for (int o = 16; o; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+  return v;
+}
+__device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
+  for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
+template <typename I>
+__device__ __forceinline__ I warp_scan(I v, int lane) {  // inclusive, integers
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const I y = __shfl_up_sync(0xffffffffu, v, o);
+    if (lane >= o) v += y;
+  }
+  return v;
+}
+
+// Inclusive scan of one integer a thread, in thread order; *total: the block's sum.  `s` holds one
+// value a warp; the caller's next use of it needs a barrier in between.
+template <typename I, int THREADS>
+__device__ __forceinline__ I block_scan(I v, I* s, int tid, I* total) {
+  const int warp = tid >> 5, lane = tid & 31;
+  I x = warp_scan(v, lane);
+  if (lane == 31) s[warp] = x;
+  __syncthreads();
+  I before = 0, all = 0;
+#pragma unroll
+  for (int w = 0; w < THREADS / 32; ++w) {
+    const I y = s[w];
+    if (w < warp) before += y;
+    all += y;
+  }
+  *total = all;
+  return x + before;
+}
+
+}  // namespace dm

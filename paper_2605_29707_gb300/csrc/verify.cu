@@ -41,11 +41,6 @@ __device__ __forceinline__ uint32_t dsmem_addr(const void* local, uint32_t rank)
   return r;
 }
 
-__device__ __forceinline__ void cluster_arrive() {
-  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-}
-__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
-
 // Asks for `bytes` (a multiple of 16) at a 16-byte aligned address to be brought into L2.
 __device__ __forceinline__ void l2_prefetch_bulk(const void* p, uint32_t bytes) {
   asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(p), "r"(bytes) : "memory");
@@ -179,8 +174,8 @@ __global__ void __launch_bounds__(32) tree_walk_kernel(const int32_t* __restrict
 
 // The walk, launched as a programmatic dependent of the row kernel before it, which triggers it by
 // exiting: the launch, not the walk's work, overlaps the row kernel's last CTAs.
-static cudaError_t launch_walk(const int32_t* parent, const int32_t* token, const int32_t* row_choice, int B,
-                               int N, int32_t* nodes, int32_t* count, int32_t* bonus, cudaStream_t stream) {
+cudaError_t launch_walk(const int32_t* parent, const int32_t* token, const int32_t* row_choice, int B, int N,
+                        int32_t* nodes, int32_t* count, int32_t* bonus, cudaStream_t stream) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(B));
   cfg.blockDim = dim3(32);
