@@ -157,7 +157,7 @@ __global__ void __launch_bounds__(kDistillThreads) distill_kernel(const DistillP
     Vec<T> f;
     f.raw = v[q].raw;
 #pragma unroll
-    for (int i = 0; i < N; ++i) sum += exp2f((to_f32(f.e[i]) - base) * p.k2);
+    for (int i = 0; i < N; ++i) sum += ex2((to_f32(f.e[i]) - base) * p.k2);
   }
   sum = block_sum<kDistillThreads>(sum, s_red, tid);
   if (tid == 0) s_part2 = sum;
@@ -171,10 +171,10 @@ __global__ void __launch_bounds__(kDistillThreads) distill_kernel(const DistillP
   const float top = block_max<kDistillThreads>(fmaxf(e.x, m), s_red, tid);
   const bool empty = !(top > -INFINITY) && !isnan(top);  // every logit is -inf
   const float ref = empty ? 0.f : top;
-  const float mine = e.first ? exp2f((e.x - ref) * p.k2) : 0.f;
+  const float mine = e.first ? ex2((e.x - ref) * p.k2) : 0.f;
   const float listed = block_sum<kDistillThreads>(mine, s_red, tid);
   const float m_top = m > -INFINITY ? m - ref : 0.f;
-  const float r_top = r * exp2f(m_top * p.k2);
+  const float r_top = r * ex2(m_top * p.k2);
   const float z = r_top + listed;
   const float log_z = logf(z);  // relative to ref
   const float log_r = m_top * p.inv_t + logf(r);
@@ -195,13 +195,13 @@ __global__ void __launch_bounds__(kDistillThreads) distill_kernel(const DistillP
     const float up = p.grad_loss ? __ldg(p.grad_loss + row) : 1.f;
     const float scale = w == 0.f ? 0.f : up * w * p.inv_t;
     const float inv_z = z == 0.f ? 0.f : 1.f / z;
-    // exp(z_v - log R) (R / Z - rest), with exp2f((x - base) k2) = exp(z_v - log R) r
+    // exp(z_v - log R) (R / Z - rest), with 2^((x - base) k2) = exp(z_v - log R) r
     const float a = r == 0.f ? 0.f : scale * (r_top * inv_z - rest) / r;
     T* dx = static_cast<T*>(p.dlogits) + row * static_cast<size_t>(p.grad_stride) + lo;
     const bool zero = w == 0.f;
     auto grad = [&](T xv) {
       T g;
-      from_f32(zero ? 0.f : a * exp2f((to_f32(xv) - base) * p.k2), &g);
+      from_f32(zero ? 0.f : a * ex2((to_f32(xv) - base) * p.k2), &g);
       return g;
     };
     if (row_shift(dx) == shift) {

@@ -34,6 +34,28 @@ struct Vec {  // 16 bytes of elements
   __device__ __forceinline__ Vec() {}
 };
 
+// 2^x by the special function unit (relative error below 2^-22; results below 2^-126 are 0).
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+// The greatest of the unit's elements; NaN never is (-inf if there is nothing else).
+__device__ __forceinline__ float vec_max(const Vec<float>& f) {
+  return fmaxf(fmaxf(f.e[0], f.e[1]), fmaxf(f.e[2], f.e[3]));
+}
+template <typename T, typename T2>
+__device__ __forceinline__ float vec_max_pairs(const Vec<T>& f) {
+  const T2* h = reinterpret_cast<const T2*>(f.e);
+  const T2 a = __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));
+  return fmaxf(to_f32(a.x), to_f32(a.y));
+}
+__device__ __forceinline__ float vec_max(const Vec<__nv_bfloat16>& f) {
+  return vec_max_pairs<__nv_bfloat16, __nv_bfloat162>(f);
+}
+__device__ __forceinline__ float vec_max(const Vec<__half>& f) { return vec_max_pairs<__half, __half2>(f); }
+
 // ------------------------------------------------------------------ staging
 // Elements [0, len) of `src` come to rest at s[shift .. shift + len), where `shift` is the number of
 // elements between the 16-byte boundary below src and src itself, so that whole 16-byte units of
@@ -90,6 +112,11 @@ __device__ __forceinline__ unsigned long long ld_cluster(const unsigned long lon
   unsigned long long v;
   asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(cluster_addr(local, rank)) : "memory");
   return v;
+}
+
+__device__ __forceinline__ void st_cluster(uint2* local, uint32_t rank, uint2 v) {
+  asm volatile("st.shared::cluster.v2.u32 [%0], {%1, %2};" ::"r"(cluster_addr(local, rank)), "r"(v.x), "r"(v.y)
+               : "memory");
 }
 
 // ------------------------------------------------------------------ block reductions and scans

@@ -54,7 +54,7 @@ __device__ __forceinline__ u64 weight(float x, const Scale& sc, const u64* pow2)
   const float d = x - sc.m;
   const float t = d * sc.k_hi;
   if (!(t >= kNoWeight)) return 0ull;
-  if (t < kCoarse) return static_cast<u64>(__float2uint_rn(exp2f(t + static_cast<float>(kWeightBits))));
+  if (t < kCoarse) return static_cast<u64>(__float2uint_rn(ex2(t + static_cast<float>(kWeightBits))));
   // x - m = d + d_lo
   const float xv = d + sc.m;
   const float mv = d - xv;
@@ -79,6 +79,10 @@ __device__ __forceinline__ u64 weight(float x, const Scale& sc, const u64* pow2)
 // The order of preference as integers: greater value, greater key; -0 as +0, NaN last.
 __device__ __forceinline__ uint32_t value_key(float x) { return x != x ? 0u : f32_ord(x + 0.f); }
 
+__device__ __forceinline__ float key_value(uint32_t k) {
+  return __uint_as_float((k & 0x80000000u) ? k & 0x7fffffffu : ~k);
+}
+
 struct DrawShared {
   u64 pow2[32];
   u64 mass[2][256];      // a round's histogram, by round parity (read by the cluster)
@@ -86,13 +90,18 @@ struct DrawShared {
   u64 sum;               // kept mass of this CTA (read by the cluster)
   u64 total[256];        // the cluster's histogram
   u64 need;
+  double floor;          // T log(min_p)
+  float group[kDrawThreads];  // maxima of groups of threads
   float red[kDrawThreads / 32];
-  float max;             // this CTA's maximum (read by the cluster)
-  float k_hi, k_lo, floor;
-  float m;
+  float red2[kDrawThreads / 32];
+  float max, aux;        // this CTA's maximum, and its bound on where the candidates begin (read by the cluster)
+  float k_hi, k_lo;
+  float m, tau;
   uint32_t prefix;
-  uint32_t equal;        // this CTA's elements at the cut (read by the cluster)
   int cut;
+  uint32_t count[2];     // this CTA's candidates, before and after their bound is raised (read by the cluster)
+  u64 tail[2];           // mass of its other ids (read by the cluster)
+  int last_bin;
 };
 
 // The cut that a selection leaves: an element stays when its key is greater, or when it is equal and its
@@ -157,8 +166,7 @@ __device__ Cut radix_cut(const T* s, int shift, int len, u64 need, const Cut& ol
   const u64* hist = sh.mass[(round - 1) & 1];
   u64 each = 1;
   if (WEIGHTED) {
-    const uint32_t b = (prefix & 0x80000000u) ? prefix & 0x7fffffffu : ~prefix;
-    each = weight(__uint_as_float(b), sc, sh.pow2);
+    each = weight(key_value(prefix), sc, sh.pow2);
   }
   const u64 count = (need + each - 1) / each;  // equal elements that stay, over the cluster
   u64 before = 0, own = 0;
@@ -196,6 +204,181 @@ __device__ Cut radix_cut(const T* s, int shift, int len, u64 need, const Cut& ol
   return cut;
 }
 
+// ------------------------------------------------------------------ few candidates: one CTA finishes the row
+constexpr int kListCap = 2048;                            // candidates the cluster's first CTA can take
+constexpr int kPerThread = kListCap / kDrawThreads;
+constexpr int kBins = 512;                                // of the candidates' values
+constexpr int kGroupsSmall = 128;                         // groups whose maxima bound the k-th greatest
+
+// Bits of an element type's keys that say nothing (an order-preserving shift of the key drops them).
+template <typename T>
+constexpr int kKeyShift = sizeof(T) == 4 ? 0 : 13;
+template <>
+constexpr int kKeyShift<__nv_bfloat16> = 16;
+
+// A lower bound (16 bits of the key) on the j-th greatest of the warp's 32 * PER values.
+template <int PER>
+__device__ __forceinline__ float jth_greatest(const float* v, int j, int lane) {
+  uint32_t key[PER];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) key[i] = value_key(v[i * 32 + lane]) >> 16;
+  uint32_t prefix = 0;
+  for (int bit = 15; bit >= 0; --bit) {
+    const uint32_t c = prefix | (1u << bit);
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) n += __popc(__ballot_sync(0xffffffffu, key[i] >= c));
+    if (n >= j) prefix = c;
+  }
+  return prefix <= 0x7fu ? -INFINITY : key_value(prefix << 16);  // keys up to 0x7fffff: -inf and NaN
+}
+
+// Radix selection within the block, over the list entries (4 a thread at most, in id order) that `kept` has bits
+// for; `amount` as in radix_cut.  Returns the bits that stay.  `range`: the entries' keys differ in bits below it.
+template <bool WEIGHTED>
+__device__ __forceinline__ unsigned block_cut(const uint32_t (&key)[kPerThread], const u64 (&w)[kPerThread],
+                                              unsigned kept, u64 need, int range, DrawShared& sh) {
+  const int tid = threadIdx.x;
+  uint32_t prefix = 0, mask = 0;
+  int bit = range;
+  while (bit > 0) {
+    const int width = min(8, bit);
+    bit -= width;
+    u64* hist = sh.mass[0];
+    __syncthreads();
+    if (tid < 256) hist[tid] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kPerThread; ++i)
+      if ((kept >> i & 1) && (key[i] & mask) == prefix)
+        atomicAdd(&hist[(key[i] >> bit) & ((1u << width) - 1u)], WEIGHTED ? w[i] : 1ull);
+    __syncthreads();
+    if (tid < 32) {
+      u64 mine[8], sum = 0;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        mine[j] = hist[255 - (8 * tid + j)];
+        sum += mine[j];
+      }
+      u64 above = warp_scan(sum, tid) - sum;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        if (above < need && need <= above + mine[j]) {
+          sh.prefix = static_cast<uint32_t>(255 - (8 * tid + j)) << bit;
+          sh.need = need - above;
+        }
+        above += mine[j];
+      }
+    }
+    __syncthreads();
+    prefix |= sh.prefix;
+    need = sh.need;
+    mask |= ((1u << width) - 1u) << bit;
+  }
+  // greater: stay; equal: the first in id order whose predecessors carry less than `need`
+  unsigned stay = 0, equal = 0;
+  u64 each = 0;
+#pragma unroll
+  for (int i = 0; i < kPerThread; ++i) {
+    if (!(kept >> i & 1)) continue;
+    const uint32_t k = key[i] & mask;
+    if (k > prefix) stay |= 1u << i;
+    if (k == prefix) {
+      equal |= 1u << i;
+      each = WEIGHTED ? w[i] : 1ull;
+    }
+  }
+  u64 all;
+  const u64 own = each * __popc(equal);
+  __syncthreads();
+  u64 before = block_scan<u64, kDrawThreads>(own, sh.scan, tid, &all) - own;
+#pragma unroll
+  for (int i = 0; i < kPerThread; ++i)
+    if (equal >> i & 1) {
+      if (before < need) stay |= 1u << i;
+      before += each;
+    }
+  return stay;
+}
+
+__device__ __forceinline__ u64 share_of(float f, u64 all, bool up) {  // floor or ceil of f * all, 0 <= f < 1
+  const u64 f64 = static_cast<u64>(static_cast<double>(f) * 18446744073709551616.0);
+  return __umul64hi(f64, all) + (up && f64 * all != 0);
+}
+
+__device__ __forceinline__ float clamped_uniform(float u) {
+  if (!(u >= 0.f)) return 0.f;
+  return u >= 1.f ? 0x1.fffffep-1f : u;  // the largest float below 1
+}
+
+struct Settings {
+  float temp, top_p, min_p, u;
+  int top_k;
+  bool use_k, use_p, use_m;
+};
+
+// The first CTA's end of a row: n candidates (values and ids, in id order), every id of the row that can stay among
+// them; `tail`: the mass of the others, where top-p goes by it.
+template <typename T>
+__device__ void finish_list(const uint2* list, int n, u64 tail, const Settings& set, const Scale& sc, DrawShared& sh,
+                            int32_t* token, float* logp) {
+  const int tid = threadIdx.x;
+  const int per = (n + kDrawThreads - 1) / kDrawThreads;  // <= kPerThread
+  float x[kPerThread];
+  uint32_t key[kPerThread];
+  u64 w[kPerThread];
+  unsigned kept = 0;
+#pragma unroll
+  for (int i = 0; i < kPerThread; ++i) {
+    const int at = tid * per + i;
+    x[i] = -INFINITY;
+    if (i < per && at < n) {
+      x[i] = __uint_as_float(list[at].x);
+      kept |= 1u << i;
+    }
+    key[i] = value_key(x[i]) >> kKeyShift<T>;
+    w[i] = 0;
+  }
+  const int range = 32 - __clz((value_key(sc.m) >> kKeyShift<T>) ^ (value_key(sh.tau) >> kKeyShift<T>));
+  if (set.use_k && set.top_k < n)
+    kept = block_cut<false>(key, w, kept, static_cast<u64>(set.top_k), range, sh);
+  u64 mine = 0;
+#pragma unroll
+  for (int i = 0; i < kPerThread; ++i)
+    if (kept >> i & 1) {
+      w[i] = weight(x[i], sc, sh.pow2);
+      mine += w[i];
+    }
+  if (set.use_p) {
+    u64 all;
+    __syncthreads();
+    block_scan<u64, kDrawThreads>(mine, sh.scan, tid, &all);
+    const u64 need = set.top_p > 0.f ? share_of(set.top_p, all + tail, true) : 0;
+    if (need < all) kept = block_cut<true>(key, w, kept, max(need, 1ull), range, sh);
+  }
+  mine = 0;
+  const float floor = set.use_m ? __double2float_ru(sc.m + sh.floor) : -INFINITY;
+#pragma unroll
+  for (int i = 0; i < kPerThread; ++i) {
+    if (!(kept >> i & 1) || !(x[i] >= floor)) w[i] = 0;
+    mine += w[i];
+  }
+  u64 all;
+  __syncthreads();
+  u64 at = block_scan<u64, kDrawThreads>(mine, sh.scan, tid, &all) - mine;
+  const u64 goal = share_of(set.u, all, false);
+  if (at <= goal && goal < at + mine) {
+#pragma unroll
+    for (int i = 0; i < kPerThread; ++i) {
+      if (at <= goal && goal < at + w[i]) {
+        *token = static_cast<int32_t>(list[tid * per + i].y);
+        if (logp) *logp = (x[i] - sc.m) / set.temp - logf(static_cast<float>(all) * 0x1p-44f);
+      }
+      at += w[i];
+    }
+  }
+}
+
 template <typename T>
 __global__ void __launch_bounds__(kDrawThreads) filtered_draw_kernel(const DrawParams p) {
   extern __shared__ __align__(16) unsigned char s_raw[];
@@ -211,39 +394,99 @@ __global__ void __launch_bounds__(kDrawThreads) filtered_draw_kernel(const DrawP
   stage_slice<T, kDrawThreads>(s, src, len, tid);
 
   // ---- the row's settings
-  const size_t set = row / p.rows_per_set;
-  float temp = p.temperature ? __ldg(p.temperature + set) : 1.f;
-  int top_k = p.top_k ? __ldg(p.top_k + set) : 0;
-  const float top_p = p.top_p ? __ldg(p.top_p + set) : 1.f;
-  const float min_p = p.min_p ? __ldg(p.min_p + set) : 0.f;
-  if (!(temp > 0.f)) {  // greedy
-    temp = 1.f;
-    top_k = 1;
+  const unsigned at_set = static_cast<unsigned>(row) / p.rows_per_set;
+  Settings set;
+  set.temp = p.temperature ? __ldg(p.temperature + at_set) : 1.f;
+  set.top_k = p.top_k ? __ldg(p.top_k + at_set) : 0;
+  set.top_p = p.top_p ? __ldg(p.top_p + at_set) : 1.f;
+  set.min_p = p.min_p ? __ldg(p.min_p + at_set) : 0.f;
+  set.u = clamped_uniform(__ldg(p.uniforms + row));
+  if (!(set.temp > 0.f)) {  // greedy
+    set.temp = 1.f;
+    set.top_k = 1;
   }
+  set.use_k = set.top_k >= 1 && set.top_k < p.V;
+  set.use_p = set.top_p < 1.f;
+  set.use_m = set.min_p > 0.f;
+  const int mask_words = (p.slice + 16 + 31) / 32;
+  uint32_t* mask = reinterpret_cast<uint32_t*>(s + p.slice + 16);  // one bit per staged element: a candidate
+  uint2* list = reinterpret_cast<uint2*>(mask + ((mask_words + 3) & ~3));
+  for (int i = tid; i < mask_words; i += kDrawThreads) mask[i] = 0;
   if (tid < 32) sh.pow2[tid] = c_pow2[tid];
   if (tid == 0) {
-    const double k = 1.4426950408889634 / static_cast<double>(temp);
+    const double k = 1.4426950408889634 / static_cast<double>(set.temp);
     sh.k_hi = static_cast<float>(fmin(k, 3.0e38));  // a T so small leaves the maximum alone either way
     sh.k_lo = k < 3.0e38 ? static_cast<float>(k - static_cast<double>(sh.k_hi)) : 0.f;
-    sh.floor = -INFINITY;  // of x - max
+    const double d = set.use_m ? static_cast<double>(set.temp) * log(fmin(static_cast<double>(set.min_p), 1.0)) : 0.0;
+    sh.floor = d == d ? d : -INFINITY;  // an infinite T makes all ids alike
   }
 
-  // ---- the row maximum (NaN never is)
+  // ---- the row maximum (NaN never is), and what bounds the candidates from below
   cp_async_wait_all();
   __syncthreads();
+  constexpr int N = Vec<T>::kN;
+  const Vec<T>* v = reinterpret_cast<const Vec<T>*>(s);
+  const int units = row_units<T>(shift, len);
   float mx = -INFINITY;
-  for (int i = tid; i < len; i += kDrawThreads) mx = fmaxf(mx, to_f32(s[shift + i]));
-  mx = warp_max(mx);
-  if (lane == 0) sh.red[warp] = mx;
+  for (int q = tid; q < units; q += kDrawThreads) {
+    Vec<T> f;
+    f.raw = v[q].raw;
+    mx = fmaxf(mx, vec_max(f));
+  }
+  // top-k: where every CTA has ceil(k / 8) groups of elements whose maxima reach a value, k elements do
+  const int in_cta = (set.top_k + kRowSplit - 1) / kRowSplit;
+  const bool small_k = in_cta <= kGroupsSmall / 2;
+  const bool bound_k = set.use_k && in_cta <= kDrawThreads / 2;
+  if (bound_k) {
+    float g = mx;
+    if (small_k) {
+      g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, 1));
+      g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, 2));
+      if ((tid & 3) == 0) sh.group[tid >> 2] = g;
+    } else {
+      sh.group[tid] = g;
+    }
+  }
+  const float wmx = warp_max(mx);
+  if (lane == 0) sh.red[warp] = wmx;
   __syncthreads();
-  if (tid == 0) {
-    for (int w = 1; w < kDrawThreads / 32; ++w) mx = fmaxf(mx, sh.red[w]);
-    sh.max = mx;
+  float own_max = sh.red[0];
+#pragma unroll
+  for (int w = 1; w < kDrawThreads / 32; ++w) own_max = fmaxf(own_max, sh.red[w]);
+  if (set.use_p && !set.use_k) {  // top-p: the maxima's own mass is a lower bound of the whole
+    float e = warp_sum(mx > -INFINITY ? ex2((mx - own_max) * sh.k_hi) : 0.f);
+    if (lane == 0) sh.red2[warp] = e;
+    __syncthreads();
+  }
+  if (warp == 0) {
+    float aux = -INFINITY;
+    if (bound_k)
+      aux = small_k ? jth_greatest<kGroupsSmall / 32>(sh.group, in_cta, lane)
+                    : jth_greatest<kDrawThreads / 32>(sh.group, in_cta, lane);
+    if (set.use_p && !set.use_k) aux = warp_sum(lane < kDrawThreads / 32 ? sh.red2[lane] : 0.f);
+    if (lane == 0) {
+      sh.max = own_max;
+      sh.aux = aux;
+    }
   }
   cluster_sync();
   if (warp == 0) {
-    const float m = warp_max(lane < kRowSplit ? ld_cluster(&sh.max, lane) : -INFINITY);
-    if (lane == 0) sh.m = m;
+    const float cm = lane < kRowSplit ? ld_cluster(&sh.max, lane) : -INFINITY;
+    const float ca = lane < kRowSplit ? ld_cluster(&sh.aux, lane) : INFINITY;
+    const float m = warp_max(cm);
+    float tau = -INFINITY;
+    if (set.use_k) {
+      tau = set.top_k == 1 ? m : -warp_max(-ca);
+    } else if (set.use_p) {
+      // mass below tau <= V exp((tau - m) / T) <= (1 - p) * mass
+      const float z = warp_sum(cm > -INFINITY && lane < kRowSplit ? ca * ex2((cm - m) * sh.k_hi) : 0.f);
+      tau = m + log2f((1.f - set.top_p) * z / static_cast<float>(p.V) * 0.999f) / sh.k_hi;
+    }
+    if (set.use_m && !(set.use_k && set.use_p)) tau = fmaxf(tau, __double2float_rd(m + sh.floor));
+    if (lane == 0) {
+      sh.m = m;
+      sh.tau = fminf(tau, m);
+    }
   }
   __syncthreads();
   const Scale sc{sh.m, sh.k_hi, sh.k_lo, sh.m == INFINITY};
@@ -256,11 +499,125 @@ __global__ void __launch_bounds__(kDrawThreads) filtered_draw_kernel(const DrawP
     return;
   }
 
+  // ---- the candidates: marked in every slice, gathered by the first CTA if they are few
+  const float tau = sh.tau;
+  if ((tau > -INFINITY || p.V <= kListCap) && !sc.inf) {
+    const bool with_tail = set.use_p && !set.use_k;
+    float rest = 0.f;
+    for (int q = tid; q < units; q += kDrawThreads) {
+      Vec<T> f;
+      f.raw = v[q].raw;
+      if (with_tail) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const float x = to_f32(f.e[i]);
+          const float e = ex2((x - sc.m) * sc.k_hi);
+          rest += x < tau ? e : 0.f;
+        }
+      }
+      if (vec_max(f) >= tau) {
+        unsigned bits = 0;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const int at = q * N + i - shift;
+          if (to_f32(f.e[i]) >= tau && at >= 0 && at < len) bits |= 1u << i;
+        }
+        if (bits) atomicOr(&mask[q * N / 32], bits << (q * N % 32));
+      }
+    }
+    __syncthreads();
+    const int words = (units * N + 31) / 32;
+    const int per = (words + kDrawThreads - 1) / kDrawThreads;
+    int place = 0, n = 0;
+    u64 tail = 0;
+    bool fits = false;
+    for (int round = 0; round < 2; ++round) {
+      int mine = 0;
+      for (int i = tid * per; i < min(words, tid * per + per); ++i) mine += __popc(mask[i]);
+      int own;
+      place = block_scan<int, kDrawThreads>(mine, reinterpret_cast<int*>(sh.scan), tid, &own) - mine;
+      __syncthreads();
+      if (with_tail && round == 0) {
+        u64 t;
+        block_scan<u64, kDrawThreads>(static_cast<u64>(rest * 0x1p44f), sh.scan, tid, &t);
+        if (tid == 0) sh.tail[0] = t;
+      }
+      if (tid == 0) sh.count[round] = static_cast<uint32_t>(own);
+      cluster_sync();
+      int before = 0;
+      n = 0;
+      tail = 0;
+#pragma unroll
+      for (int c = 0; c < kRowSplit; ++c) {
+        const int y = static_cast<int>(ld_cluster(&sh.count[round], c));
+        if (c < static_cast<int>(part)) before += y;
+        n += y;
+        if (with_tail) tail += ld_cluster(&sh.tail[round], c);
+      }
+      place += before;
+      fits = n <= kListCap;
+      if (fits || !with_tail || round) break;
+
+      // top-p with too many candidates: count them by value, and raise tau to where the mass above it surely holds
+      // the share.  A bin's mass lies between its count times the weights at its two ends.
+      uint32_t* bins = reinterpret_cast<uint32_t*>(sh.mass);
+      const float scale = static_cast<float>(kBins) / (sc.m - tau) * 0.9999f;
+      if (tid < kBins) bins[tid] = 0;
+      __syncthreads();
+      for (int i = tid; i < words; i += kDrawThreads)
+        for (uint32_t w = mask[i]; w; w &= w - 1) {
+          const float x = to_f32(s[i * 32 + __ffs(w) - 1]);
+          atomicAdd(&bins[static_cast<int>((sc.m - x) * scale)], 1u);
+        }
+      cluster_sync();
+      uint32_t count = 0;
+      for (int c = 0; c < kRowSplit; ++c) count += ld_cluster(&bins[tid], c);
+      const float hi_w = ex2(-static_cast<float>(tid) / scale * sc.k_hi);
+      const float lo_w = ex2(-static_cast<float>(tid + 1) / scale * sc.k_hi);
+      if (tid == 0) sh.last_bin = kBins - 1;
+      u64 hi_all, lo_all;
+      __syncthreads();
+      const u64 hi = block_scan<u64, kDrawThreads>(static_cast<u64>(static_cast<float>(count) * hi_w * 0x1p40f), sh.scan,
+                                                   tid, &hi_all);
+      __syncthreads();
+      const u64 lo = block_scan<u64, kDrawThreads>(static_cast<u64>(static_cast<float>(count) * lo_w * 0x1p40f), sh.scan,
+                                                   tid, &lo_all);
+      const float below = static_cast<float>(hi_all - hi + (tail >> 4));
+      if ((1.f - set.top_p) * static_cast<float>(lo) >= 1.001f * set.top_p * below) atomicMin(&sh.last_bin, tid);
+      __syncthreads();
+      const int last_bin = sh.last_bin;
+      u64 mid = 0, t;
+      for (int i = tid; i < words; i += kDrawThreads) {
+        uint32_t left = 0;
+        for (uint32_t w = mask[i]; w; w &= w - 1) {
+          const float x = to_f32(s[i * 32 + __ffs(w) - 1]);
+          if (static_cast<int>((sc.m - x) * scale) <= last_bin) left |= w & -w;
+          else mid += weight(x, sc, sh.pow2);
+        }
+        mask[i] = left;
+      }
+      block_scan<u64, kDrawThreads>(mid, sh.scan, tid, &t);
+      if (tid == 0) sh.tail[1] = sh.tail[0] + t;
+      __syncthreads();
+    }
+    if (fits) {
+      for (int i = tid * per; i < min(words, tid * per + per); ++i)
+        for (uint32_t w = mask[i]; w; w &= w - 1) {
+          const int e = i * 32 + __ffs(w) - 1;
+          st_cluster(&list[place++], 0, make_uint2(__float_as_uint(to_f32(s[e])), static_cast<uint32_t>(lo + e - shift)));
+        }
+      cluster_sync();
+      if (part == 0)
+        finish_list<T>(list, n, tail, set, sc, sh, p.tokens + row, p.logp ? p.logp + row : nullptr);
+      return;
+    }
+    cluster_sync();  // done with the counts before their memory is used again
+  }
+
   // ---- the three cuts
   Cut cut{0u, len};
-  if (top_k >= 1 && top_k < p.V)
-    cut = radix_cut<T, false>(s, shift, len, static_cast<u64>(top_k), cut, sc, sh, part);
-  if (top_p < 1.f) {
+  if (set.use_k) cut = radix_cut<T, false>(s, shift, len, static_cast<u64>(set.top_k), cut, sc, sh, part);
+  if (set.use_p) {
     u64 mine = 0;
     for (int i = tid; i < len; i += kDrawThreads) {
       const float x = to_f32(s[shift + i]);
@@ -273,21 +630,12 @@ __global__ void __launch_bounds__(kDrawThreads) filtered_draw_kernel(const DrawP
     u64 all = 0;
     for (int c = 0; c < kRowSplit; ++c) all += ld_cluster(&sh.sum, c);
     cluster_sync();
-    // mass before < p * all, in integers: before < ceil(p * all)
-    u64 need = 1;
-    if (top_p > 0.f) {
-      const u64 p64 = static_cast<u64>(static_cast<double>(top_p) * 18446744073709551616.0);
-      need = __umul64hi(p64, all) + (p64 * all != 0);
-    }
+    const u64 need = set.top_p > 0.f ? share_of(set.top_p, all, true) : 0;
     cut = radix_cut<T, true>(s, shift, len, max(need, 1ull), cut, sc, sh, part);
   }
-  if (min_p > 0.f) {
-    if (tid == 0) {
-      const double d = static_cast<double>(temp) * log(static_cast<double>(min_p));
-      sh.floor = sc.inf ? INFINITY : __double2float_ru(fmin(static_cast<double>(sc.m) + d, static_cast<double>(sc.m)));
-    }
-    __syncthreads();
-    const uint32_t key = value_key(sh.floor);
+  if (set.use_m) {
+    const float floor = sc.inf ? INFINITY : __double2float_ru(sc.m + sh.floor);
+    const uint32_t key = value_key(floor);
     if (key > cut.key) cut = Cut{key, len};
   }
 
@@ -311,10 +659,7 @@ __global__ void __launch_bounds__(kDrawThreads) filtered_draw_kernel(const DrawP
     all += n;
   }
   cluster_arrive();  // done with the other CTAs' shared memory
-  float u = __ldg(p.uniforms + row);
-  if (!(u >= 0.f)) u = 0.f;
-  if (u >= 1.f) u = 0x1.fffffep-1f;  // the largest float below 1
-  const u64 goal = __umul64hi(static_cast<u64>(static_cast<double>(u) * 18446744073709551616.0), all);
+  const u64 goal = share_of(set.u, all, false);
   u64 at = before + incl - mine;
   if (mine && at <= goal && goal < at + mine) {
     for (int i = i0; i < i1; ++i) {
@@ -325,7 +670,7 @@ __global__ void __launch_bounds__(kDrawThreads) filtered_draw_kernel(const DrawP
       if (goal < at) {
         p.tokens[row] = lo + i;
         if (p.logp) {
-          const float z = sc.inf ? 0.f : (x - sc.m) / temp;
+          const float z = sc.inf ? 0.f : (x - sc.m) / set.temp;
           p.logp[row] = z - logf(static_cast<float>(all) * 0x1p-44f);
         }
         break;
@@ -337,7 +682,8 @@ __global__ void __launch_bounds__(kDrawThreads) filtered_draw_kernel(const DrawP
 
 template <typename T>
 static cudaError_t launch_draw(const DrawParams& p, int rows, cudaStream_t stream) {
-  const size_t smem = (static_cast<size_t>(p.slice) + 16) * sizeof(T);
+  const int mask_words = (p.slice + 16 + 31) / 32;
+  const size_t smem = (static_cast<size_t>(p.slice) + 16) * sizeof(T) + ((mask_words + 3) & ~3) * 4 + kListCap * 8;
   cudaError_t e = ensure_smem_attr(reinterpret_cast<const void*>(filtered_draw_kernel<T>), smem, false);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
