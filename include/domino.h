@@ -285,7 +285,7 @@ enum domino_dtype { DOMINO_F32 = 0, DOMINO_BF16 = 1, DOMINO_F16 = 2 };
  * order in which they are formed, and borders (of top_p, of u) lie within about 1e-11 of the mass of
  * where exact arithmetic puts them.
  *   logits: device [rows, row_stride] of `dtype`, element-aligned; ids 0 .. V - 1 of a row are read,
- *     row_stride >= V.  V <= 8 * 49152 (a row is staged in shared memory once).
+ *     row_stride >= V.  V <= 524288 (the sum of the weights fits 63 bits).
  *   temperature, top_p, min_p (fp32) and top_k (int32): device [rows], or NULL (T = 1, filter off).
  *   uniforms: device fp32 [rows].
  * Outputs (device): tokens int32 [rows]; logp fp32 [rows] or NULL: the token's log-probability among

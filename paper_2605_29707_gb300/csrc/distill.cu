@@ -326,7 +326,7 @@ static cudaError_t launch_type(const DistillParams& p, int rows, cudaStream_t st
 cudaError_t launch_distill(DistillParams p, int dtype, int rows, cudaStream_t stream) {
   if (rows <= 0 || rows > 0x7fffffff / kRowSplit) return cudaErrorInvalidValue;
   p.slice = ((p.V + kRowSplit - 1) / kRowSplit + 7) & ~7;
-  if (p.V > kMaxRowVocab) return cudaErrorInvalidValue;
+  if (p.V > kMaxDistillVocab) return cudaErrorInvalidValue;
   if (dtype == kF32) return launch_type<float>(p, rows, stream);
   if (dtype == kBf16) return launch_type<__nv_bfloat16>(p, rows, stream);
   return launch_type<__half>(p, rows, stream);

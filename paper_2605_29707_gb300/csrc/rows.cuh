@@ -32,6 +32,11 @@ struct Vec {  // 16 bytes of elements
     T e[kN];
   };
   __device__ __forceinline__ Vec() {}
+  __device__ __forceinline__ Vec(const Vec& o) : raw(o.raw) {}
+  __device__ __forceinline__ Vec& operator=(const Vec& o) {
+    raw = o.raw;
+    return *this;
+  }
 };
 
 // 2^x by the special function unit (relative error below 2^-22; results below 2^-126 are 0).
@@ -117,6 +122,26 @@ __device__ __forceinline__ unsigned long long ld_cluster(const unsigned long lon
 __device__ __forceinline__ void st_cluster(uint2* local, uint32_t rank, uint2 v) {
   asm volatile("st.shared::cluster.v2.u32 [%0], {%1, %2};" ::"r"(cluster_addr(local, rank)), "r"(v.x), "r"(v.y)
                : "memory");
+}
+
+__device__ __forceinline__ uint4 ld_cluster(const uint4* local, uint32_t rank) {
+  uint4 v;
+  asm volatile("ld.shared::cluster.v4.u32 {%0, %1, %2, %3}, [%4];"
+               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+               : "r"(cluster_addr(local, rank))
+               : "memory");
+  return v;
+}
+__device__ __forceinline__ uint32_t atom_add_cluster(uint32_t* local, uint32_t rank, uint32_t v) {
+  uint32_t old;
+  asm volatile("atom.relaxed.cluster.shared::cluster.add.u32 %0, [%1], %2;"
+               : "=r"(old)
+               : "r"(cluster_addr(local, rank)), "r"(v)
+               : "memory");
+  return old;
+}
+__device__ __forceinline__ void red_add_cluster(unsigned long long* local, uint32_t rank, unsigned long long v) {
+  asm volatile("red.relaxed.cluster.shared::cluster.add.u64 [%0], %1;" ::"r"(cluster_addr(local, rank)), "l"(v) : "memory");
 }
 
 // ------------------------------------------------------------------ block reductions and scans

@@ -6,16 +6,23 @@
 // with exp(z - max z) >= min_p; the first always.  The token is the first kept id, in id order, whose
 // cumulative mass exceeds u times the kept mass.
 //
-// Weights are integers: 2^44 exp(z - max z), rounded.  At most 2^19 of them fit 64 bits, so every sum
+// Weights are integers: 2^44 exp(z - max z), rounded.  At most 2^19 of them fit 63 bits, so every sum
 // is exact and the same in any order: splitting a row over CTAs, atomics and the order of threads
-// change nothing.  Where a weight can move a border (above 2^-14 of the greatest) it is computed to
-// about 2^-38 of its value (weight()), below that in fp32: a border then lies where 64-bit arithmetic
-// puts it but for about 1e-11 of the mass.
+// change nothing.  A weight above 2^-14 of the greatest is computed to about 2^-38 of its value
+// (weight()), one below in fp32.  (z, id) is one 64-bit integer (Order), so every cut is a bound on it.
 //
-// A cluster of eight CTAs holds a row in shared memory, one DRAM read.  The cut by top-k and the cut by
-// top-p are each a radix selection over the order-preserving integer of the value, 8 bits a round,
-// with a histogram of counts (top-k) or of weights (top-p) per CTA that the cluster adds up; ties at the
-// cut are resolved by id from the CTAs' counts of them.  The draw scans the kept weights in id order.
+// A cluster of eight CTAs takes a row, an eighth each, and reads it twice, the second time from L2: eight
+// slices of 76 KB (V = 151936, fp32) per SM would not fit its shared memory, while what is in flight on
+// the whole chip fits L2, and a plain re-read of L2-resident slices ran at 11 TB/s against 7 from DRAM.
+//   1. the row maximum, and a value below which no id can stay: with top-k, where every CTA has k / 8
+//      groups of elements whose maxima reach it; with top-p, where V ids of its weight would carry less
+//      than 1 - p of what those maxima carry already; with min-p, from its definition;
+//   2. the ids above it, the candidates, go to the first CTA, which finishes the row alone while the
+//      others leave; with top-p the weights of the other ids are added up on the way, in fp32.
+// Too many candidates (more than kListCap) under top-p: the candidates' weights are added up by value
+// in kBins bins, the bin that holds the border is found, and either the candidates down to it are few
+// enough, or those in it are and decide the border.  What else leaves too many is cut by a radix selection
+// over the whole row.  Then, and without any filter, the cluster scans the kept weights in id order.
 #include <math.h>
 
 #include "kernels.h"
@@ -23,8 +30,14 @@
 
 namespace dm {
 
-constexpr int kDrawThreads = 512;
-constexpr int kWeightBits = 44;    // the greatest weight is 2^44
+constexpr int kDrawThreads = 256;
+constexpr int kDrawWarps = kDrawThreads / 32;
+constexpr int kDrawBatch = 4;       // 16-byte loads a thread has in flight
+constexpr int kListCap = 2048;      // candidates the cluster's first CTA can take
+constexpr int kBins = 512;          // of values, or of ids
+constexpr int kSubCap = 256;        // entries of one bin that are ranked against each other
+constexpr int kDirect = 128;        // entries that are ranked without bins
+constexpr int kWeightBits = 44;     // the greatest weight is 2^44
 constexpr float kNoWeight = -45.f;  // log2 of a relative weight that rounds to nothing
 constexpr float kCoarse = -14.f;    // below this (log2) a weight is computed in fp32
 
@@ -76,145 +89,113 @@ __device__ __forceinline__ u64 weight(float x, const Scale& sc, const u64* pow2)
   return (v + ((1ull << n) >> 1)) >> n;
 }
 
-// The order of preference as integers: greater value, greater key; -0 as +0, NaN last.
+// The order of preference as integers: greater value, greater key (-0 as +0, NaN last); equal values: the lower id.
 __device__ __forceinline__ uint32_t value_key(float x) { return x != x ? 0u : f32_ord(x + 0.f); }
-
 __device__ __forceinline__ float key_value(uint32_t k) {
   return __uint_as_float((k & 0x80000000u) ? k & 0x7fffffffu : ~k);
 }
+__device__ __forceinline__ u64 order_of(uint32_t key, uint32_t id) { return (static_cast<u64>(key) << 32) | (~id); }
+__device__ __forceinline__ u64 order_of(float x, uint32_t id) { return order_of(value_key(x), id); }
 
-struct DrawShared {
-  u64 pow2[32];
-  u64 mass[2][256];      // a round's histogram, by round parity (read by the cluster)
-  u64 scan[kDrawThreads / 32];
-  u64 sum;               // kept mass of this CTA (read by the cluster)
-  u64 total[256];        // the cluster's histogram
-  u64 need;
-  double floor;          // T log(min_p)
-  float group[kDrawThreads];  // maxima of groups of threads
-  float red[kDrawThreads / 32];
-  float red2[kDrawThreads / 32];
-  float max, aux;        // this CTA's maximum, and its bound on where the candidates begin (read by the cluster)
-  float k_hi, k_lo;
-  float m, tau;
-  uint32_t prefix;
-  int cut;
-  uint32_t count[2];     // this CTA's candidates, before and after their bound is raised (read by the cluster)
-  u64 tail[2];           // mass of its other ids (read by the cluster)
-  int last_bin;
-};
-
-// The cut that a selection leaves: an element stays when its key is greater, or when it is equal and its
-// place in this CTA's slice lies below `cut`.
-struct Cut {
-  uint32_t key;
-  int at;
-  __device__ __forceinline__ bool keeps(uint32_t k, int i) const { return k > key || (k == key && i < at); }
-};
-
-// Radix selection across the cluster.  Every element that `old` keeps carries `amount` (1, or its weight);
-// the new cut keeps the elements whose predecessors in the order of preference carry less than `need`.
-// The amounts of all of them add up to at least `need` >= 1.
-template <typename T, bool WEIGHTED>
-__device__ Cut radix_cut(const T* s, int shift, int len, u64 need, const Cut& old, const Scale& sc, DrawShared& sh,
-                         uint32_t part) {
-  const int tid = threadIdx.x;
-  uint32_t prefix = 0, mask = 0;
-  int round = 0;
-  for (int bit = 24; bit >= 0; bit -= 8, ++round) {
-    u64* hist = sh.mass[round & 1];
-    if (tid < 256) hist[tid] = 0;
-    __syncthreads();
-    for (int i = tid; i < len; i += kDrawThreads) {
-      const float x = to_f32(s[shift + i]);
-      const uint32_t k = value_key(x);
-      if ((k & mask) == prefix && old.keeps(k, i))
-        atomicAdd(&hist[(k >> bit) & 255], WEIGHTED ? weight(x, sc, sh.pow2) : 1ull);
-    }
-    cluster_sync();  // every CTA's histogram is in place
-    if (tid < 256) {
-      u64 all = 0;
-#pragma unroll
-      for (int c = 0; c < kRowSplit; ++c) all += ld_cluster(&hist[tid], c);
-      sh.total[tid] = all;
-    }
-    __syncthreads();
-    if (tid < 32) {  // the digit at which the amounts, from the greatest digit down, reach `need`
-      u64 mine[8], sum = 0;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        mine[j] = sh.total[255 - (8 * tid + j)];
-        sum += mine[j];
-      }
-      u64 above = warp_scan(sum, tid) - sum;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        if (above < need && need <= above + mine[j]) {
-          sh.prefix = prefix | (static_cast<uint32_t>(255 - (8 * tid + j)) << bit);
-          sh.need = need - above;
-        }
-        above += mine[j];
-      }
-    }
-    __syncthreads();
-    prefix = sh.prefix;
-    need = sh.need;
-    mask |= 255u << bit;
-  }
-  // ties: `need` of what the equal elements carry goes to the ones of lowest id.  They weigh the same, so
-  // the last histogram gives every CTA the number of them before its slice.
-  const u64* hist = sh.mass[(round - 1) & 1];
-  u64 each = 1;
-  if (WEIGHTED) {
-    each = weight(key_value(prefix), sc, sh.pow2);
-  }
-  const u64 count = (need + each - 1) / each;  // equal elements that stay, over the cluster
-  u64 before = 0, own = 0;
-#pragma unroll
-  for (int c = 0; c < kRowSplit; ++c) {
-    const u64 n = ld_cluster(&hist[prefix & 255], c) / each;
-    if (c < static_cast<int>(part)) before += n;
-    if (c == static_cast<int>(part)) own = n;
-  }
-  Cut cut{prefix, len};
-  const long long stay = static_cast<long long>(count) - static_cast<long long>(before);
-  if (stay <= 0) {
-    cut.at = 0;
-  } else if (stay < static_cast<long long>(own)) {  // the place of the stay-th equal element
-    const int run = (len + kDrawThreads - 1) / kDrawThreads;
-    const int i0 = min(len, tid * run), i1 = min(len, i0 + run);
-    int n = 0;
-    for (int i = i0; i < i1; ++i) {
-      const uint32_t k = value_key(to_f32(s[shift + i]));
-      n += k == prefix && old.keeps(k, i);
-    }
-    int all;
-    int seen = block_scan<int, kDrawThreads>(n, reinterpret_cast<int*>(sh.scan), tid, &all) - n;
-    if (seen < stay && stay <= seen + n) {
-      for (int i = i0; i < i1; ++i) {
-        const uint32_t k = value_key(to_f32(s[shift + i]));
-        if (k == prefix && old.keeps(k, i) && ++seen == stay) sh.cut = i + 1;
-      }
-    }
-    __syncthreads();
-    cut.at = sh.cut;
-  }
-  if (old.key == prefix) cut.at = min(cut.at, old.at);
-  cluster_sync();  // the histograms may be written again
-  return cut;
+// The bin of a value at most `top`, counted from there down; monotone, and in range whatever is rounded.
+__device__ __forceinline__ int value_bin(float x, float top, float scale) {
+  return min(max(static_cast<int>((top - x) * scale), 0), kBins - 1);
 }
 
-// ------------------------------------------------------------------ few candidates: one CTA finishes the row
-constexpr int kListCap = 2048;                            // candidates the cluster's first CTA can take
-constexpr int kPerThread = kListCap / kDrawThreads;
-constexpr int kBins = 512;                                // of the candidates' values
-constexpr int kGroupsSmall = 128;                         // groups whose maxima bound the k-th greatest
+struct Settings {
+  float temp, top_p, u;
+  int top_k;
+  bool use_k, use_p, use_m;
+};
 
-// Bits of an element type's keys that say nothing (an order-preserving shift of the key drops them).
+struct DrawShared {  // dynamic shared memory
+  uint2 local[kListCap];  // this CTA's candidates (value, id); in the first CTA, later, the list's weights
+  uint2 list[kListCap];   // the first CTA: the cluster's candidates
+  uint4 bins[kBins];      // count and weights (three limbs of 15 bits) by value or id
+  u64 pow2[32];
+  u64 sub_order[kSubCap];
+  u64 sub_amount[kSubCap];
+  u64 scan[kDrawWarps];
+  u64 digit[2][256];      // a radix round's histogram, by round parity (read by the cluster)
+  u64 total[256];
+  u64 sum;                // kept mass of this CTA (read by the cluster)
+  u64 tail;               // the first CTA: mass of the ids that are no candidates
+  u64 need, result;
+  u64 cut;                // the first CTA: the border of top-p (read by the cluster)
+  double floor;           // T log(min_p)
+  float group[kDrawThreads];
+  float red[kDrawWarps], red2[kDrawWarps];
+  float max, aux;         // this CTA's maximum, and its part of the candidates' bound (read by the cluster)
+  float k_hi, k_lo;
+  float m, tau, lowest;   // lowest: the least value that min-p keeps
+  uint32_t key;
+  int n_local;            // entries of local
+  uint32_t n_list[2];     // the first CTA: the cluster's candidates, of the first and the second gathering
+  int base, n_sub, bin, n_upto, n_in, before;
+};
+
+// A row's slice: ids [lo, lo + len), read in units of 16 bytes aligned in global memory.  Whole units are one load;
+// the first and the last unit, which may hold what is not the row's, are read element by element.
 template <typename T>
-constexpr int kKeyShift = sizeof(T) == 4 ? 0 : 13;
-template <>
-constexpr int kKeyShift<__nv_bfloat16> = 16;
+struct Slice {
+  static constexpr int N = Vec<T>::kN;
+  const T* src;
+  int lo, len, shift, units, first, last;
+  __device__ __forceinline__ Slice(const T* row, int from, int n) : src(row + from), lo(from), len(n) {
+    shift = row_shift(src);
+    units = row_units<T>(shift, len);
+    first = shift ? 1 : 0;
+    last = (shift + len) / N;
+  }
+  __device__ __forceinline__ Vec<T> load(int q) const {
+    Vec<T> f;
+    if (q >= first && q < last) {
+      f.raw = __ldcg(reinterpret_cast<const uint4*>(src + (q * N - shift)));
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const int at = q * N + i - shift;
+        if (at >= 0 && at < len) f.e[i] = src[at];
+        else from_f32(-INFINITY, &f.e[i]);
+      }
+    }
+    return f;
+  }
+  __device__ __forceinline__ bool holds(int q, int i) const {
+    const int at = q * N + i - shift;
+    return at >= 0 && at < len;
+  }
+  __device__ __forceinline__ uint32_t id(int q, int i) const { return static_cast<uint32_t>(lo + q * N + i - shift); }
+  // f(unit, its index) for every unit, a batch of loads at a time
+  template <typename F>
+  __device__ __forceinline__ void each(F&& f) const {
+    for (int q0 = threadIdx.x; q0 < units; q0 += kDrawThreads * kDrawBatch) {
+      Vec<T> v[kDrawBatch];
+#pragma unroll
+      for (int j = 0; j < kDrawBatch; ++j)
+        if (q0 + j * kDrawThreads < units) v[j] = load(q0 + j * kDrawThreads);
+#pragma unroll
+      for (int j = 0; j < kDrawBatch; ++j)
+        if (q0 + j * kDrawThreads < units) f(v[j], q0 + j * kDrawThreads);
+    }
+  }
+  // the units of this warp's share of the slice, in id order: [*q0, *q1)
+  __device__ __forceinline__ void warp_share(int* q0, int* q1) const {
+    const int per = (units + kDrawWarps - 1) / kDrawWarps;
+    *q0 = min(units, static_cast<int>(threadIdx.x >> 5) * per);
+    *q1 = min(units, *q0 + per);
+  }
+};
+
+// floor(f * all), or the ceiling, for 0 <= f < 1 (f's bits below 2^-64 are dropped)
+__device__ __forceinline__ u64 share_of(float f, u64 all, bool up) {
+  const uint32_t b = __float_as_uint(f);
+  const int e = static_cast<int>(b >> 23);  // f = (mantissa) 2^(e - 150)
+  const u64 mant = e ? (b & 0x7fffffu) | 0x800000u : 0u;
+  const int by = e - 150 + 64;
+  const u64 f64 = by >= 0 ? mant << by : (by > -64 ? mant >> -by : 0);
+  return __umul64hi(f64, all) + (up && f64 * all != 0);
+}
 
 // A lower bound (16 bits of the key) on the j-th greatest of the warp's 32 * PER values.
 template <int PER>
@@ -233,237 +214,401 @@ __device__ __forceinline__ float jth_greatest(const float* v, int j, int lane) {
   return prefix <= 0x7fu ? -INFINITY : key_value(prefix << 16);  // keys up to 0x7fffff: -inf and NaN
 }
 
-// Radix selection within the block, over the list entries (4 a thread at most, in id order) that `kept` has bits
-// for; `amount` as in radix_cut.  Returns the bits that stay.  `range`: the entries' keys differ in bits below it.
-template <bool WEIGHTED>
-__device__ __forceinline__ unsigned block_cut(const uint32_t (&key)[kPerThread], const u64 (&w)[kPerThread],
-                                              unsigned kept, u64 need, int range, DrawShared& sh) {
+__device__ __forceinline__ void add_to_bin(uint4* bin, u64 w) {
+  atomicAdd(&bin->x, 1u);
+  atomicAdd(&bin->y, static_cast<uint32_t>(w) & 0x7fffu);
+  atomicAdd(&bin->z, static_cast<uint32_t>(w >> 15) & 0x7fffu);
+  atomicAdd(&bin->w, static_cast<uint32_t>(w >> 30));
+}
+__device__ __forceinline__ u64 bin_mass(const uint4& b) {
+  return static_cast<u64>(b.y) + (static_cast<u64>(b.z) << 15) + (static_cast<u64>(b.w) << 30);
+}
+
+__device__ __forceinline__ u64 block_total(u64 v, DrawShared& sh) {
+  u64 all;
+  __syncthreads();
+  block_scan<u64, kDrawThreads>(v, sh.scan, threadIdx.x, &all);
+  return all;
+}
+
+// ------------------------------------------------------------------ the first CTA: searches over its list
+// The entry at which the amounts (1, or the weights) of the list's entries, from the first in the order on, reach
+// `need`: its order.  Entries below `cut` do not count; the order is that of preference, or that of ids.
+struct ListView {
+  const uint2* list;
+  const u64* wt;
+  int n;
+  u64 cut;
+  __device__ __forceinline__ bool entry(int e, bool weighted, bool by_id, u64* order, u64* amount) const {
+    const uint2 v = list[e];
+    const u64 o = order_of(__uint_as_float(v.x), v.y);
+    if (o < cut) return false;
+    *order = by_id ? static_cast<u64>(~v.y) : o;
+    *amount = weighted ? wt[e] : 1ull;
+    return true;
+  }
+};
+
+template <bool WEIGHTED, bool BY_ID>
+__device__ u64 find_border(const ListView& l, u64 need, float top, float scale, uint32_t id_width, DrawShared& sh) {
+  const int tid = threadIdx.x;
+  u64 o = 0, a = 0;
+  __syncthreads();
+  if (tid == 0) sh.n_sub = 0;
+  if (l.n <= kDirect) {
+    if (tid < l.n) {
+      if (!l.entry(tid, WEIGHTED, BY_ID, &o, &a)) o = a = 0;
+      sh.sub_order[tid] = o;
+      sh.sub_amount[tid] = a;
+    }
+    __syncthreads();
+    if (tid == 0) sh.n_sub = l.n;
+  } else {
+    for (int i = tid; i < kBins; i += kDrawThreads) sh.bins[i] = make_uint4(0, 0, 0, 0);
+    __syncthreads();
+    auto bin_of = [&](int e) {
+      const uint2 v = l.list[e];
+      return BY_ID ? static_cast<int>(v.y / id_width) : value_bin(__uint_as_float(v.x), top, scale);
+    };
+    for (int e = tid; e < l.n; e += kDrawThreads)
+      if (l.entry(e, WEIGHTED, BY_ID, &o, &a)) {
+        if (WEIGHTED) add_to_bin(&sh.bins[bin_of(e)], a);
+        else atomicAdd(&sh.bins[bin_of(e)].y, 1u);
+      }
+    __syncthreads();
+    u64 mine[kBins / kDrawThreads], sum = 0, all;
+#pragma unroll
+    for (int i = 0; i < kBins / kDrawThreads; ++i) {
+      mine[i] = bin_mass(sh.bins[tid * (kBins / kDrawThreads) + i]);
+      sum += mine[i];
+    }
+    u64 before = block_scan<u64, kDrawThreads>(sum, sh.scan, tid, &all) - sum;
+#pragma unroll
+    for (int i = 0; i < kBins / kDrawThreads; ++i) {
+      if (before < need && need <= before + mine[i]) {
+        sh.bin = tid * (kBins / kDrawThreads) + i;
+        sh.need = need - before;
+      }
+      before += mine[i];
+    }
+    __syncthreads();
+    const int bin = sh.bin;
+    for (int e = tid; e < l.n; e += kDrawThreads)
+      if (bin_of(e) == bin && l.entry(e, WEIGHTED, BY_ID, &o, &a)) {
+        const int at = atomicAdd(&sh.n_sub, 1);
+        if (at < kSubCap) {
+          sh.sub_order[at] = o;
+          sh.sub_amount[at] = a;
+        }
+      }
+  }
+  __syncthreads();
+  const int c = sh.n_sub;
+  if (c <= kSubCap) {  // each against each
+    const u64 want = l.n <= kDirect ? need : sh.need;
+    const bool pairs = c <= kDrawThreads / 2;  // two threads an entry
+    const int e = pairs ? tid >> 1 : tid;
+    o = e < c ? sh.sub_order[e] : ~0ull;
+    u64 before = 0;
+    for (int j = pairs ? tid & 1 : 0; j < c; j += pairs ? 2 : 1)
+      if (sh.sub_order[j] > o) before += sh.sub_amount[j];
+    if (pairs) before += __shfl_xor_sync(0xffffffffu, before, 1);
+    if (e < c && before < want && want <= before + sh.sub_amount[e]) sh.result = o;
+  } else {  // one bit of the order at a time: the greatest order from which on the amounts reach `need`
+    u64 prefix = 0;
+    for (int bit = BY_ID ? 31 : 63; bit >= 0; --bit) {
+      const u64 c2 = prefix | (1ull << bit);
+      u64 sum = 0;
+      for (int i = tid; i < l.n; i += kDrawThreads)
+        if (l.entry(i, WEIGHTED, BY_ID, &o, &a) && o >= c2) sum += a;
+      if (block_total(sum, sh) >= need) prefix = c2;
+    }
+    if (tid == 0) sh.result = prefix;
+  }
+  __syncthreads();
+  return sh.result;
+}
+
+// The end of a row in the cluster's first CTA: n candidates, every id that can stay among them; `tail`: the mass of
+// the others, where top-p goes by it.
+__device__ void finish_list(int n, u64 tail, const Settings& set, const Scale& sc, int V, DrawShared& sh, int32_t* token,
+                            float* logp) {
+  const int tid = threadIdx.x;
+  u64* wt = reinterpret_cast<u64*>(sh.local);
+  ListView l{sh.list, wt, n, 0};
+  const float scale = sh.tau > -INFINITY && sc.m > sh.tau ? static_cast<float>(kBins) / (sc.m - sh.tau) * 0.9999f : 0.f;
+  const uint32_t id_width = static_cast<uint32_t>((V + kBins - 1) / kBins);
+  u64 mine = 0;
+  for (int e = tid; e < n; e += kDrawThreads) {
+    const u64 w = weight(__uint_as_float(sh.list[e].x), sc, sh.pow2);
+    wt[e] = w;
+    mine += w;
+  }
+  u64 all = block_total(mine, sh);
+  auto kept = [&] {  // the mass from the cut on
+    u64 sum = 0;
+    for (int e = tid; e < n; e += kDrawThreads)
+      if (order_of(__uint_as_float(sh.list[e].x), sh.list[e].y) >= l.cut) sum += wt[e];
+    return block_total(sum, sh);
+  };
+  if (set.use_k && set.top_k < n) {
+    l.cut = find_border<false, false>(l, static_cast<u64>(set.top_k), sc.m, scale, 1, sh);
+    all = kept();
+  }
+  if (set.use_p) {
+    const u64 need = set.top_p > 0.f ? max(share_of(set.top_p, all + tail, true), 1ull) : 1ull;
+    if (need < all) {
+      l.cut = max(l.cut, find_border<true, false>(l, need, sc.m, scale, 1, sh));
+      all = kept();
+    }
+  }
+  if (set.use_m) {
+    const u64 low = static_cast<u64>(value_key(sh.lowest)) << 32;
+    if (low > l.cut) {
+      l.cut = low;
+      all = kept();
+    }
+  }
+  const u64 goal = share_of(set.u, all, false);
+  const uint32_t y = ~static_cast<uint32_t>(find_border<true, true>(l, goal + 1, sc.m, scale, id_width, sh));
+  for (int e = tid; e < n; e += kDrawThreads)
+    if (sh.list[e].y == y) {
+      *token = static_cast<int32_t>(y);
+      if (logp) *logp = (__uint_as_float(sh.list[e].x) - sc.m) / set.temp - logf(static_cast<float>(all) * 0x1p-44f);
+    }
+}
+
+// ------------------------------------------------------------------ the whole cluster
+// This CTA's candidates into the first CTA's list (as far as they fit); the cluster's number of them.
+__device__ int gather(DrawShared& sh, int round) {
+  const int tid = threadIdx.x;
+  __syncthreads();
+  const int n = sh.n_local;
+  if (tid == 0) sh.base = static_cast<int>(atom_add_cluster(&sh.n_list[round], 0, static_cast<uint32_t>(n)));
+  __syncthreads();
+  const int base = sh.base;
+  const int fit = min(min(n, kListCap), kListCap - base);
+  for (int i = tid; i < fit; i += kDrawThreads) st_cluster(&sh.list[base + i], 0, sh.local[i]);
+  cluster_sync();
+  return static_cast<int>(ld_cluster(&sh.n_list[round], 0));
+}
+
+// Of amounts a(value, id) over the slice, in id order: every warp's total into sh.scan; returns the CTA's.
+template <typename T, typename A>
+__device__ u64 slice_total(const Slice<T>& sl, DrawShared& sh, A&& amount) {
+  int q0, q1;
+  sl.warp_share(&q0, &q1);
+  u64 sum = 0;
+#pragma unroll 2
+  for (int q = q0 + (threadIdx.x & 31); q < q1; q += 32) {
+    const Vec<T> f = sl.load(q);
+#pragma unroll
+    for (int i = 0; i < Vec<T>::kN; ++i)
+      if (sl.holds(q, i)) sum += amount(to_f32(f.e[i]), sl.id(q, i));
+  }
+#pragma unroll
+  for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  __syncthreads();
+  if ((threadIdx.x & 31) == 0) sh.scan[threadIdx.x >> 5] = sum;
+  __syncthreads();
+  u64 all = 0;
+  for (int w = 0; w < kDrawWarps; ++w) all += sh.scan[w];
+  return all;
+}
+
+// After slice_total, with the same amounts: calls f(value, id) for the element at which the amounts pass `target`
+// (their sum before it is at most `target`, with it more); `target` is below the CTA's total.
+template <typename T, typename A, typename F>
+__device__ void slice_locate(const Slice<T>& sl, u64 target, DrawShared& sh, A&& amount, F&& f) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  u64 at = 0;
+  for (int w = 0; w < warp; ++w) at += sh.scan[w];
+  if (target < at || target >= at + sh.scan[warp]) return;
+  int q0, q1;
+  sl.warp_share(&q0, &q1);
+  for (int q = q0 + lane; q - lane < q1; q += 32) {
+    Vec<T> v;
+    u64 sum = 0;
+    if (q < q1) {
+      v = sl.load(q);
+#pragma unroll
+      for (int i = 0; i < Vec<T>::kN; ++i)
+        if (sl.holds(q, i)) sum += amount(to_f32(v.e[i]), sl.id(q, i));
+    }
+    const u64 incl = warp_scan(sum, lane);
+    const u64 all = __shfl_sync(0xffffffffu, incl, 31);
+    if (target < at + all) {
+      u64 mine = at + incl - sum;
+      if (sum && mine <= target && target < mine + sum) {
+        bool done = false;
+#pragma unroll
+        for (int i = 0; i < Vec<T>::kN; ++i) {
+          if (done || !sl.holds(q, i)) continue;
+          mine += amount(to_f32(v.e[i]), sl.id(q, i));
+          if (target < mine) {
+            f(to_f32(v.e[i]), sl.id(q, i));
+            done = true;
+          }
+        }
+      }
+      return;
+    }
+    at += all;
+  }
+}
+
+// Radix selection across the cluster, for rows whose candidates no bound thins out.  Every element from `old` on
+// carries `amount` (1, or its weight); the cut is the order at which the amounts, from the first on, reach `need`
+// >= 1 (at most what they carry together).  Ties are cut by id, CTA by CTA: the result holds for this CTA's ids.
+template <typename T, bool WEIGHTED>
+__device__ u64 radix_cut(const Slice<T>& sl, u64 need, u64 old, const Scale& sc, DrawShared& sh, uint32_t part) {
   const int tid = threadIdx.x;
   uint32_t prefix = 0, mask = 0;
-  int bit = range;
-  while (bit > 0) {
-    const int width = min(8, bit);
-    bit -= width;
-    u64* hist = sh.mass[0];
+  int round = 0;
+  for (int bit = 24; bit >= 0; bit -= 8, ++round) {
+    u64* hist = sh.digit[round & 1];
+    hist[tid] = 0;
     __syncthreads();
-    if (tid < 256) hist[tid] = 0;
-    __syncthreads();
+    sl.each([&](const Vec<T>& f, int q) {
 #pragma unroll
-    for (int i = 0; i < kPerThread; ++i)
-      if ((kept >> i & 1) && (key[i] & mask) == prefix)
-        atomicAdd(&hist[(key[i] >> bit) & ((1u << width) - 1u)], WEIGHTED ? w[i] : 1ull);
+      for (int i = 0; i < Vec<T>::kN; ++i) {
+        const float x = to_f32(f.e[i]);
+        const uint32_t k = value_key(x);
+        if ((k & mask) == prefix && sl.holds(q, i) && order_of(k, sl.id(q, i)) >= old)
+          atomicAdd(&hist[(k >> bit) & 255], WEIGHTED ? weight(x, sc, sh.pow2) : 1ull);
+      }
+    });
+    cluster_sync();  // every CTA's histogram is in place
+    u64 all = 0;
+#pragma unroll
+    for (int c = 0; c < kRowSplit; ++c) all += ld_cluster(&hist[tid], c);
+    sh.total[tid] = all;
     __syncthreads();
-    if (tid < 32) {
+    if (tid < 32) {  // the digit at which the amounts, from the greatest digit down, reach `need`
       u64 mine[8], sum = 0;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        mine[j] = hist[255 - (8 * tid + j)];
+        mine[j] = sh.total[255 - (8 * tid + j)];
         sum += mine[j];
       }
       u64 above = warp_scan(sum, tid) - sum;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         if (above < need && need <= above + mine[j]) {
-          sh.prefix = static_cast<uint32_t>(255 - (8 * tid + j)) << bit;
+          sh.key = prefix | (static_cast<uint32_t>(255 - (8 * tid + j)) << bit);
           sh.need = need - above;
         }
         above += mine[j];
       }
     }
     __syncthreads();
-    prefix |= sh.prefix;
+    prefix = sh.key;
     need = sh.need;
-    mask |= ((1u << width) - 1u) << bit;
+    mask |= 255u << bit;
   }
-  // greater: stay; equal: the first in id order whose predecessors carry less than `need`
-  unsigned stay = 0, equal = 0;
-  u64 each = 0;
+  // ties: `need` of what the equal elements carry goes to the ones of lowest id.  They weigh the same, so the last
+  // histogram gives every CTA the number of them before its slice.
+  const u64* hist = sh.digit[(round - 1) & 1];
+  const u64 each = WEIGHTED ? max(weight(key_value(prefix), sc, sh.pow2), 1ull) : 1ull;
+  const u64 count = (need + each - 1) / each;  // equal elements that stay, over the cluster
+  u64 before = 0, own = 0;
 #pragma unroll
-  for (int i = 0; i < kPerThread; ++i) {
-    if (!(kept >> i & 1)) continue;
-    const uint32_t k = key[i] & mask;
-    if (k > prefix) stay |= 1u << i;
-    if (k == prefix) {
-      equal |= 1u << i;
-      each = WEIGHTED ? w[i] : 1ull;
-    }
+  for (int c = 0; c < kRowSplit; ++c) {
+    const u64 n = ld_cluster(&hist[prefix & 255], c) / each;
+    if (c < static_cast<int>(part)) before += n;
+    if (c == static_cast<int>(part)) own = n;
   }
-  u64 all;
-  const u64 own = each * __popc(equal);
-  __syncthreads();
-  u64 before = block_scan<u64, kDrawThreads>(own, sh.scan, tid, &all) - own;
-#pragma unroll
-  for (int i = 0; i < kPerThread; ++i)
-    if (equal >> i & 1) {
-      if (before < need) stay |= 1u << i;
-      before += each;
-    }
-  return stay;
-}
-
-__device__ __forceinline__ u64 share_of(float f, u64 all, bool up) {  // floor or ceil of f * all, 0 <= f < 1
-  const u64 f64 = static_cast<u64>(static_cast<double>(f) * 18446744073709551616.0);
-  return __umul64hi(f64, all) + (up && f64 * all != 0);
-}
-
-__device__ __forceinline__ float clamped_uniform(float u) {
-  if (!(u >= 0.f)) return 0.f;
-  return u >= 1.f ? 0x1.fffffep-1f : u;  // the largest float below 1
-}
-
-struct Settings {
-  float temp, top_p, min_p, u;
-  int top_k;
-  bool use_k, use_p, use_m;
-};
-
-// The first CTA's end of a row: n candidates (values and ids, in id order), every id of the row that can stay among
-// them; `tail`: the mass of the others, where top-p goes by it.
-template <typename T>
-__device__ void finish_list(const uint2* list, int n, u64 tail, const Settings& set, const Scale& sc, DrawShared& sh,
-                            int32_t* token, float* logp) {
-  const int tid = threadIdx.x;
-  const int per = (n + kDrawThreads - 1) / kDrawThreads;  // <= kPerThread
-  float x[kPerThread];
-  uint32_t key[kPerThread];
-  u64 w[kPerThread];
-  unsigned kept = 0;
-#pragma unroll
-  for (int i = 0; i < kPerThread; ++i) {
-    const int at = tid * per + i;
-    x[i] = -INFINITY;
-    if (i < per && at < n) {
-      x[i] = __uint_as_float(list[at].x);
-      kept |= 1u << i;
-    }
-    key[i] = value_key(x[i]) >> kKeyShift<T>;
-    w[i] = 0;
-  }
-  const int range = 32 - __clz((value_key(sc.m) >> kKeyShift<T>) ^ (value_key(sh.tau) >> kKeyShift<T>));
-  if (set.use_k && set.top_k < n)
-    kept = block_cut<false>(key, w, kept, static_cast<u64>(set.top_k), range, sh);
-  u64 mine = 0;
-#pragma unroll
-  for (int i = 0; i < kPerThread; ++i)
-    if (kept >> i & 1) {
-      w[i] = weight(x[i], sc, sh.pow2);
-      mine += w[i];
-    }
-  if (set.use_p) {
-    u64 all;
+  cluster_sync();  // the histograms may be written again
+  u64 cut = order_of(prefix, 0u) + 1;  // none of the equal ones
+  if (before + own <= count) {
+    cut = order_of(prefix, 0xffffffffu);  // all of them
+  } else if (before < count) {
+    auto equal = [&](float x, uint32_t id) { return static_cast<u64>(value_key(x) == prefix && order_of(prefix, id) >= old); };
+    slice_total(sl, sh, equal);
+    slice_locate(sl, count - before - 1, sh, equal, [&](float, uint32_t id) { sh.result = order_of(prefix, id); });
     __syncthreads();
-    block_scan<u64, kDrawThreads>(mine, sh.scan, tid, &all);
-    const u64 need = set.top_p > 0.f ? share_of(set.top_p, all + tail, true) : 0;
-    if (need < all) kept = block_cut<true>(key, w, kept, max(need, 1ull), range, sh);
+    cut = sh.result;
   }
-  mine = 0;
-  const float floor = set.use_m ? __double2float_ru(sc.m + sh.floor) : -INFINITY;
-#pragma unroll
-  for (int i = 0; i < kPerThread; ++i) {
-    if (!(kept >> i & 1) || !(x[i] >= floor)) w[i] = 0;
-    mine += w[i];
-  }
-  u64 all;
-  __syncthreads();
-  u64 at = block_scan<u64, kDrawThreads>(mine, sh.scan, tid, &all) - mine;
-  const u64 goal = share_of(set.u, all, false);
-  if (at <= goal && goal < at + mine) {
-#pragma unroll
-    for (int i = 0; i < kPerThread; ++i) {
-      if (at <= goal && goal < at + w[i]) {
-        *token = static_cast<int32_t>(list[tid * per + i].y);
-        if (logp) *logp = (x[i] - sc.m) / set.temp - logf(static_cast<float>(all) * 0x1p-44f);
-      }
-      at += w[i];
-    }
-  }
+  return max(cut, old);
 }
 
 template <typename T>
-__global__ void __launch_bounds__(kDrawThreads) filtered_draw_kernel(const DrawParams p) {
+__global__ void __launch_bounds__(kDrawThreads, 4) filtered_draw_kernel(const DrawParams p) {
   extern __shared__ __align__(16) unsigned char s_raw[];
-  __shared__ DrawShared sh;
-  T* s = reinterpret_cast<T*>(s_raw);
-  const size_t row = blockIdx.x / kRowSplit;
+  DrawShared& sh = *reinterpret_cast<DrawShared*>(s_raw);
+  const unsigned row = blockIdx.x / kRowSplit;
   const uint32_t part = cluster_ctarank();  // == blockIdx.x % kRowSplit
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int lo = min(p.V, static_cast<int>(part) * p.slice);
-  const int len = min(p.V, lo + p.slice) - lo;
-  const T* src = static_cast<const T*>(p.logits) + row * static_cast<size_t>(p.stride) + lo;
-  const int shift = row_shift(src);
-  stage_slice<T, kDrawThreads>(s, src, len, tid);
+  const Slice<T> sl(static_cast<const T*>(p.logits) + row * static_cast<size_t>(p.stride), lo,
+                    min(p.V, lo + p.slice) - lo);
+  constexpr int N = Vec<T>::kN;
 
   // ---- the row's settings
-  const unsigned at_set = static_cast<unsigned>(row) / p.rows_per_set;
+  const unsigned at_set = row / p.rows_per_set;
   Settings set;
   set.temp = p.temperature ? __ldg(p.temperature + at_set) : 1.f;
   set.top_k = p.top_k ? __ldg(p.top_k + at_set) : 0;
   set.top_p = p.top_p ? __ldg(p.top_p + at_set) : 1.f;
-  set.min_p = p.min_p ? __ldg(p.min_p + at_set) : 0.f;
-  set.u = clamped_uniform(__ldg(p.uniforms + row));
+  const float min_p = p.min_p ? __ldg(p.min_p + at_set) : 0.f;
+  set.u = __ldg(p.uniforms + row);
+  if (!(set.u >= 0.f)) set.u = 0.f;
+  if (set.u >= 1.f) set.u = 0x1.fffffep-1f;  // the largest float below 1
+
+  // ---- the row maximum (NaN never is)
+  float mx = -INFINITY;
+  sl.each([&](const Vec<T>& f, int) { mx = fmaxf(mx, vec_max(f)); });
+
   if (!(set.temp > 0.f)) {  // greedy
     set.temp = 1.f;
     set.top_k = 1;
   }
   set.use_k = set.top_k >= 1 && set.top_k < p.V;
   set.use_p = set.top_p < 1.f;
-  set.use_m = set.min_p > 0.f;
-  const int mask_words = (p.slice + 16 + 31) / 32;
-  uint32_t* mask = reinterpret_cast<uint32_t*>(s + p.slice + 16);  // one bit per staged element: a candidate
-  uint2* list = reinterpret_cast<uint2*>(mask + ((mask_words + 3) & ~3));
-  for (int i = tid; i < mask_words; i += kDrawThreads) mask[i] = 0;
+  set.use_m = min_p > 0.f;
+  const bool with_tail = set.use_p && !set.use_k;
   if (tid < 32) sh.pow2[tid] = c_pow2[tid];
-  if (tid == 0) {
+  if (tid == 32) {
     const double k = 1.4426950408889634 / static_cast<double>(set.temp);
     sh.k_hi = static_cast<float>(fmin(k, 3.0e38));  // a T so small leaves the maximum alone either way
     sh.k_lo = k < 3.0e38 ? static_cast<float>(k - static_cast<double>(sh.k_hi)) : 0.f;
-    const double d = set.use_m ? static_cast<double>(set.temp) * log(fmin(static_cast<double>(set.min_p), 1.0)) : 0.0;
+    sh.n_local = 0;
+    sh.n_list[0] = sh.n_list[1] = 0;
+    sh.tail = 0;
+  }
+  if (tid == 64 && set.use_m) {
+    const double d = static_cast<double>(set.temp) * log(fmin(static_cast<double>(min_p), 1.0));
     sh.floor = d == d ? d : -INFINITY;  // an infinite T makes all ids alike
   }
+  if (with_tail)
+    for (int i = tid; i < kBins; i += kDrawThreads) sh.bins[i] = make_uint4(0, 0, 0, 0);
 
-  // ---- the row maximum (NaN never is), and what bounds the candidates from below
-  cp_async_wait_all();
-  __syncthreads();
-  constexpr int N = Vec<T>::kN;
-  const Vec<T>* v = reinterpret_cast<const Vec<T>*>(s);
-  const int units = row_units<T>(shift, len);
-  float mx = -INFINITY;
-  for (int q = tid; q < units; q += kDrawThreads) {
-    Vec<T> f;
-    f.raw = v[q].raw;
-    mx = fmaxf(mx, vec_max(f));
-  }
+  // ---- what bounds the candidates from below
   // top-k: where every CTA has ceil(k / 8) groups of elements whose maxima reach a value, k elements do
   const int in_cta = (set.top_k + kRowSplit - 1) / kRowSplit;
-  const bool small_k = in_cta <= kGroupsSmall / 2;
+  const bool small_k = in_cta <= kDrawThreads / 4;
   const bool bound_k = set.use_k && in_cta <= kDrawThreads / 2;
   if (bound_k) {
-    float g = mx;
-    if (small_k) {
-      g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, 1));
-      g = fmaxf(g, __shfl_xor_sync(0xffffffffu, g, 2));
-      if ((tid & 3) == 0) sh.group[tid >> 2] = g;
-    } else {
-      sh.group[tid] = g;
-    }
+    const float g = small_k ? fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1)) : mx;
+    if (!small_k) sh.group[tid] = g;
+    else if ((tid & 1) == 0) sh.group[tid >> 1] = g;
   }
   const float wmx = warp_max(mx);
   if (lane == 0) sh.red[warp] = wmx;
   __syncthreads();
   float own_max = sh.red[0];
 #pragma unroll
-  for (int w = 1; w < kDrawThreads / 32; ++w) own_max = fmaxf(own_max, sh.red[w]);
-  if (set.use_p && !set.use_k) {  // top-p: the maxima's own mass is a lower bound of the whole
-    float e = warp_sum(mx > -INFINITY ? ex2((mx - own_max) * sh.k_hi) : 0.f);
+  for (int w = 1; w < kDrawWarps; ++w) own_max = fmaxf(own_max, sh.red[w]);
+  if (with_tail) {  // top-p: the maxima's own mass is a lower bound of the whole
+    const float e = warp_sum(mx > -INFINITY ? ex2((mx - own_max) * sh.k_hi) : 0.f);
     if (lane == 0) sh.red2[warp] = e;
     __syncthreads();
   }
   if (warp == 0) {
     float aux = -INFINITY;
     if (bound_k)
-      aux = small_k ? jth_greatest<kGroupsSmall / 32>(sh.group, in_cta, lane)
-                    : jth_greatest<kDrawThreads / 32>(sh.group, in_cta, lane);
-    if (set.use_p && !set.use_k) aux = warp_sum(lane < kDrawThreads / 32 ? sh.red2[lane] : 0.f);
+      aux = small_k ? jth_greatest<kDrawWarps / 2>(sh.group, in_cta, lane) : jth_greatest<kDrawWarps>(sh.group, in_cta, lane);
+    if (with_tail) aux = warp_sum(lane < kDrawWarps ? sh.red2[lane] : 0.f);
     if (lane == 0) {
       sh.max = own_max;
       sh.aux = aux;
@@ -482,31 +627,40 @@ __global__ void __launch_bounds__(kDrawThreads) filtered_draw_kernel(const DrawP
       const float z = warp_sum(cm > -INFINITY && lane < kRowSplit ? ca * ex2((cm - m) * sh.k_hi) : 0.f);
       tau = m + log2f((1.f - set.top_p) * z / static_cast<float>(p.V) * 0.999f) / sh.k_hi;
     }
-    if (set.use_m && !(set.use_k && set.use_p)) tau = fmaxf(tau, __double2float_rd(m + sh.floor));
+    float lowest = -INFINITY;
+    if (set.use_m) {
+      if (lane == 0) {
+        const double d = m + sh.floor;
+        lowest = m == INFINITY ? INFINITY : __double2float_ru(d);
+        if (!(set.use_k && set.use_p)) tau = fmaxf(tau, __double2float_rd(d));
+      }
+    }
     if (lane == 0) {
       sh.m = m;
       sh.tau = fminf(tau, m);
+      sh.lowest = lowest;
     }
   }
   __syncthreads();
   const Scale sc{sh.m, sh.k_hi, sh.k_lo, sh.m == INFINITY};
+  float* logp = p.logp ? p.logp + row : nullptr;
   if (sc.m == -INFINITY) {  // nothing to draw from: the same in every CTA of the cluster
     if (part == 0 && tid == 0) {
       p.tokens[row] = 0;
-      if (p.logp) p.logp[row] = -INFINITY;
+      if (logp) *logp = -INFINITY;
     }
     cluster_sync();  // no CTA leaves while another may still read its maximum
     return;
   }
 
-  // ---- the candidates: marked in every slice, gathered by the first CTA if they are few
+  // ---- the candidates, to the first CTA if they are few
   const float tau = sh.tau;
+  u64 cut = 0;  // the order of the last id that stays
+  bool cut_k = set.use_k, cut_p = set.use_p;  // still to be found
   if ((tau > -INFINITY || p.V <= kListCap) && !sc.inf) {
-    const bool with_tail = set.use_p && !set.use_k;
+    const float scale = tau > -INFINITY && sc.m > tau ? static_cast<float>(kBins) / (sc.m - tau) * 0.9999f : 0.f;
     float rest = 0.f;
-    for (int q = tid; q < units; q += kDrawThreads) {
-      Vec<T> f;
-      f.raw = v[q].raw;
+    sl.each([&](const Vec<T>& f, int q) {
       if (with_tail) {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
@@ -516,140 +670,122 @@ __global__ void __launch_bounds__(kDrawThreads) filtered_draw_kernel(const DrawP
         }
       }
       if (vec_max(f) >= tau) {
-        unsigned bits = 0;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-          const int at = q * N + i - shift;
-          if (to_f32(f.e[i]) >= tau && at >= 0 && at < len) bits |= 1u << i;
+          const float x = to_f32(f.e[i]);
+          if (x >= tau && sl.holds(q, i)) {
+            const int at = atomicAdd(&sh.n_local, 1);
+            if (at < kListCap) sh.local[at] = make_uint2(__float_as_uint(x), sl.id(q, i));
+            if (with_tail) add_to_bin(&sh.bins[value_bin(x, sc.m, scale)], weight(x, sc, sh.pow2));
+          }
         }
-        if (bits) atomicOr(&mask[q * N / 32], bits << (q * N % 32));
       }
+    });
+    if (with_tail) {
+      const u64 t = block_total(static_cast<u64>(rest * 0x1p44f), sh);
+      if (tid == 0) red_add_cluster(&sh.tail, 0, t);
     }
-    __syncthreads();
-    const int words = (units * N + 31) / 32;
-    const int per = (words + kDrawThreads - 1) / kDrawThreads;
-    int place = 0, n = 0;
-    u64 tail = 0;
-    bool fits = false;
-    for (int round = 0; round < 2; ++round) {
-      int mine = 0;
-      for (int i = tid * per; i < min(words, tid * per + per); ++i) mine += __popc(mask[i]);
-      int own;
-      place = block_scan<int, kDrawThreads>(mine, reinterpret_cast<int*>(sh.scan), tid, &own) - mine;
-      __syncthreads();
-      if (with_tail && round == 0) {
-        u64 t;
-        block_scan<u64, kDrawThreads>(static_cast<u64>(rest * 0x1p44f), sh.scan, tid, &t);
-        if (tid == 0) sh.tail[0] = t;
-      }
-      if (tid == 0) sh.count[round] = static_cast<uint32_t>(own);
-      cluster_sync();
-      int before = 0;
-      n = 0;
-      tail = 0;
+    int n = gather(sh, 0);
+    bool fits = n <= kListCap;
+    if (!fits && with_tail) {
+      // the bin that holds top-p's border, found by the first CTA
+      if (part == 0) {
+        constexpr int kPer = kBins / kDrawThreads;
+        u64 mass[kPer], sum = 0, all;
+        int count[kPer], num = 0, n_all;
 #pragma unroll
-      for (int c = 0; c < kRowSplit; ++c) {
-        const int y = static_cast<int>(ld_cluster(&sh.count[round], c));
-        if (c < static_cast<int>(part)) before += y;
-        n += y;
-        if (with_tail) tail += ld_cluster(&sh.tail[round], c);
-      }
-      place += before;
-      fits = n <= kListCap;
-      if (fits || !with_tail || round) break;
-
-      // top-p with too many candidates: count them by value, and raise tau to where the mass above it surely holds
-      // the share.  A bin's mass lies between its count times the weights at its two ends.
-      uint32_t* bins = reinterpret_cast<uint32_t*>(sh.mass);
-      const float scale = static_cast<float>(kBins) / (sc.m - tau) * 0.9999f;
-      if (tid < kBins) bins[tid] = 0;
-      __syncthreads();
-      for (int i = tid; i < words; i += kDrawThreads)
-        for (uint32_t w = mask[i]; w; w &= w - 1) {
-          const float x = to_f32(s[i * 32 + __ffs(w) - 1]);
-          atomicAdd(&bins[static_cast<int>((sc.m - x) * scale)], 1u);
+        for (int i = 0; i < kPer; ++i) {
+          mass[i] = 0;
+          count[i] = 0;
+          for (int c = 0; c < kRowSplit; ++c) {
+            const uint4 b = ld_cluster(&sh.bins[tid * kPer + i], c);
+            mass[i] += bin_mass(b);
+            count[i] += static_cast<int>(b.x);
+          }
+          sum += mass[i];
+          num += count[i];
         }
+        u64 before = block_scan<u64, kDrawThreads>(sum, sh.scan, tid, &all) - sum;
+        __syncthreads();
+        int upto = block_scan<int, kDrawThreads>(num, reinterpret_cast<int*>(sh.scan), tid, &n_all) - num;
+        const u64 need = min(set.top_p > 0.f ? max(share_of(set.top_p, all + sh.tail, true), 1ull) : 1ull, all);
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+          if (before < need && need <= before + mass[i]) {
+            sh.bin = tid * kPer + i;
+            sh.need = need - before;
+            sh.n_upto = upto + count[i];
+            sh.n_in = count[i];
+            sh.total[0] = all + sh.tail - before - mass[i];  // below the bin
+          }
+          before += mass[i];
+          upto += count[i];
+        }
+      }
+      if (tid == 0) sh.n_local = 0;
       cluster_sync();
-      uint32_t count = 0;
-      for (int c = 0; c < kRowSplit; ++c) count += ld_cluster(&bins[tid], c);
-      const float hi_w = ex2(-static_cast<float>(tid) / scale * sc.k_hi);
-      const float lo_w = ex2(-static_cast<float>(tid + 1) / scale * sc.k_hi);
-      if (tid == 0) sh.last_bin = kBins - 1;
-      u64 hi_all, lo_all;
-      __syncthreads();
-      const u64 hi = block_scan<u64, kDrawThreads>(static_cast<u64>(static_cast<float>(count) * hi_w * 0x1p40f), sh.scan,
-                                                   tid, &hi_all);
-      __syncthreads();
-      const u64 lo = block_scan<u64, kDrawThreads>(static_cast<u64>(static_cast<float>(count) * lo_w * 0x1p40f), sh.scan,
-                                                   tid, &lo_all);
-      const float below = static_cast<float>(hi_all - hi + (tail >> 4));
-      if ((1.f - set.top_p) * static_cast<float>(lo) >= 1.001f * set.top_p * below) atomicMin(&sh.last_bin, tid);
-      __syncthreads();
-      const int last_bin = sh.last_bin;
-      u64 mid = 0, t;
-      for (int i = tid; i < words; i += kDrawThreads) {
-        uint32_t left = 0;
-        for (uint32_t w = mask[i]; w; w &= w - 1) {
-          const float x = to_f32(s[i * 32 + __ffs(w) - 1]);
-          if (static_cast<int>((sc.m - x) * scale) <= last_bin) left |= w & -w;
-          else mid += weight(x, sc, sh.pow2);
+      const int bin = static_cast<int>(ld_cluster(reinterpret_cast<uint32_t*>(&sh.bin), 0));
+      const int n_upto = static_cast<int>(ld_cluster(reinterpret_cast<uint32_t*>(&sh.n_upto), 0));
+      const int n_in = static_cast<int>(ld_cluster(reinterpret_cast<uint32_t*>(&sh.n_in), 0));
+      fits = n_upto <= kListCap;
+      if (fits || n_in <= kListCap) {
+        sl.each([&](const Vec<T>& f, int q) {
+          if (!(vec_max(f) >= tau)) return;
+#pragma unroll
+          for (int i = 0; i < N; ++i) {
+            const float x = to_f32(f.e[i]);
+            if (!(x >= tau) || !sl.holds(q, i)) continue;
+            const int b = value_bin(x, sc.m, scale);
+            if (b == bin || (fits && b < bin))
+              sh.local[atomicAdd(&sh.n_local, 1)] = make_uint2(__float_as_uint(x), sl.id(q, i));
+          }
+        });
+        n = gather(sh, 1);
+        if (!fits) {  // the border's bin decides the border
+          if (part == 0) {
+            u64* wt = reinterpret_cast<u64*>(sh.local);
+            const u64 need = sh.need;
+            for (int e = tid; e < n; e += kDrawThreads) wt[e] = weight(__uint_as_float(sh.list[e].x), sc, sh.pow2);
+            const float top = sc.m - static_cast<float>(bin) / scale;  // of the bin, which is binned again
+            const u64 border = find_border<true, false>(ListView{sh.list, wt, n, 0}, need, top,
+                                                        scale * static_cast<float>(kBins), 1, sh);
+            if (tid == 0) sh.cut = border;
+          }
+          cluster_sync();
+          cut = ld_cluster(&sh.cut, 0);
+          cut_p = false;
+        } else if (part == 0 && tid == 0) {
+          sh.tail = sh.total[0];
         }
-        mask[i] = left;
       }
-      block_scan<u64, kDrawThreads>(mid, sh.scan, tid, &t);
-      if (tid == 0) sh.tail[1] = sh.tail[0] + t;
-      __syncthreads();
     }
     if (fits) {
-      for (int i = tid * per; i < min(words, tid * per + per); ++i)
-        for (uint32_t w = mask[i]; w; w &= w - 1) {
-          const int e = i * 32 + __ffs(w) - 1;
-          st_cluster(&list[place++], 0, make_uint2(__float_as_uint(to_f32(s[e])), static_cast<uint32_t>(lo + e - shift)));
-        }
-      cluster_sync();
-      if (part == 0)
-        finish_list<T>(list, n, tail, set, sc, sh, p.tokens + row, p.logp ? p.logp + row : nullptr);
+      if (part != 0) return;
+      __syncthreads();
+      finish_list(n, sh.tail, set, sc, p.V, sh, p.tokens + row, logp);
+      cluster_sync();  // this CTA stays until the others, which read its counts, have left
       return;
     }
-    cluster_sync();  // done with the counts before their memory is used again
   }
 
-  // ---- the three cuts
-  Cut cut{0u, len};
-  if (set.use_k) cut = radix_cut<T, false>(s, shift, len, static_cast<u64>(set.top_k), cut, sc, sh, part);
-  if (set.use_p) {
-    u64 mine = 0;
-    for (int i = tid; i < len; i += kDrawThreads) {
-      const float x = to_f32(s[shift + i]);
-      if (cut.keeps(value_key(x), i)) mine += weight(x, sc, sh.pow2);
-    }
-    u64 sum;
-    block_scan<u64, kDrawThreads>(mine, sh.scan, tid, &sum);
-    if (tid == 0) sh.sum = sum;
+  // ---- the cluster goes on together: what is left to cut
+  if (cut_k) cut = radix_cut<T, false>(sl, static_cast<u64>(set.top_k), cut, sc, sh, part);
+  auto kept_weight = [&](float x, uint32_t id) { return order_of(x, id) >= cut ? weight(x, sc, sh.pow2) : 0ull; };
+  if (cut_p) {
+    const u64 own = slice_total(sl, sh, kept_weight);
+    if (tid == 0) sh.sum = own;
     cluster_sync();
     u64 all = 0;
     for (int c = 0; c < kRowSplit; ++c) all += ld_cluster(&sh.sum, c);
     cluster_sync();
-    const u64 need = set.top_p > 0.f ? share_of(set.top_p, all, true) : 0;
-    cut = radix_cut<T, true>(s, shift, len, max(need, 1ull), cut, sc, sh, part);
+    const u64 need = set.top_p > 0.f ? max(share_of(set.top_p, all, true), 1ull) : 1ull;
+    cut = radix_cut<T, true>(sl, need, cut, sc, sh, part);
   }
-  if (set.use_m) {
-    const float floor = sc.inf ? INFINITY : __double2float_ru(sc.m + sh.floor);
-    const uint32_t key = value_key(floor);
-    if (key > cut.key) cut = Cut{key, len};
-  }
+  if (set.use_m) cut = max(cut, static_cast<u64>(value_key(sh.lowest)) << 32);
 
   // ---- the draw, in id order
-  const int run = ((len + kDrawThreads - 1) / kDrawThreads) | 1;
-  const int i0 = min(len, tid * run), i1 = min(len, i0 + run);
-  u64 mine = 0;
-  for (int i = i0; i < i1; ++i) {
-    const float x = to_f32(s[shift + i]);
-    if (cut.keeps(value_key(x), i)) mine += weight(x, sc, sh.pow2);
-  }
-  u64 sum;
-  const u64 incl = block_scan<u64, kDrawThreads>(mine, sh.scan, tid, &sum);
-  if (tid == 0) sh.sum = sum;
+  const u64 own = slice_total(sl, sh, kept_weight);
+  if (tid == 0) sh.sum = own;
   cluster_sync();
   u64 all = 0, before = 0;
 #pragma unroll
@@ -660,30 +796,17 @@ __global__ void __launch_bounds__(kDrawThreads) filtered_draw_kernel(const DrawP
   }
   cluster_arrive();  // done with the other CTAs' shared memory
   const u64 goal = share_of(set.u, all, false);
-  u64 at = before + incl - mine;
-  if (mine && at <= goal && goal < at + mine) {
-    for (int i = i0; i < i1; ++i) {
-      const float x = to_f32(s[shift + i]);
-      if (!cut.keeps(value_key(x), i)) continue;
-      const u64 w = weight(x, sc, sh.pow2);
-      at += w;
-      if (goal < at) {
-        p.tokens[row] = lo + i;
-        if (p.logp) {
-          const float z = sc.inf ? 0.f : (x - sc.m) / set.temp;
-          p.logp[row] = z - logf(static_cast<float>(all) * 0x1p-44f);
-        }
-        break;
-      }
-    }
-  }
+  if (before <= goal && goal < before + own)
+    slice_locate(sl, goal - before, sh, kept_weight, [&](float x, uint32_t id) {
+      p.tokens[row] = static_cast<int32_t>(id);
+      if (logp) *logp = (sc.inf ? 0.f : (x - sc.m) / set.temp) - logf(static_cast<float>(all) * 0x1p-44f);
+    });
   cluster_wait();
 }
 
 template <typename T>
 static cudaError_t launch_draw(const DrawParams& p, int rows, cudaStream_t stream) {
-  const int mask_words = (p.slice + 16 + 31) / 32;
-  const size_t smem = (static_cast<size_t>(p.slice) + 16) * sizeof(T) + ((mask_words + 3) & ~3) * 4 + kListCap * 8;
+  constexpr size_t smem = sizeof(DrawShared);
   cudaError_t e = ensure_smem_attr(reinterpret_cast<const void*>(filtered_draw_kernel<T>), smem, false);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
@@ -704,8 +827,8 @@ static cudaError_t launch_draw(const DrawParams& p, int rows, cudaStream_t strea
 
 cudaError_t launch_filtered_draw(DrawParams p, int dtype, int rows, cudaStream_t stream) {
   if (rows <= 0 || rows > 0x7fffffff / kRowSplit) return cudaErrorInvalidValue;
+  if (p.V > kMaxDrawVocab) return cudaErrorInvalidValue;
   p.slice = ((p.V + kRowSplit - 1) / kRowSplit + 7) & ~7;
-  if (p.V > kMaxRowVocab) return cudaErrorInvalidValue;
   if (dtype == kF32) return launch_draw<float>(p, rows, stream);
   if (dtype == kBf16) return launch_draw<__nv_bfloat16>(p, rows, stream);
   return launch_draw<__half>(p, rows, stream);
