@@ -277,7 +277,7 @@ struct DrawParams {
   float* logp;               // [rows] or nullptr
   int slice;                 // set by the launch: ids per CTA
 };
-cudaError_t launch_filtered_draw(DrawParams p, int dtype, int rows, cudaStream_t stream);
+cudaError_t launch_filtered_draw(const DrawParams& p, int dtype, int rows, cudaStream_t stream);
 
 struct DistillParams {
   const void* logits;  // [rows][stride]

@@ -173,15 +173,10 @@ __device__ __forceinline__ I block_scan(I v, I* s, int tid, I* total) {
   I x = warp_scan(v, lane);
   if (lane == 31) s[warp] = x;
   __syncthreads();
-  I before = 0, all = 0;
-#pragma unroll
-  for (int w = 0; w < THREADS / 32; ++w) {
-    const I y = s[w];
-    if (w < warp) before += y;
-    all += y;
-  }
-  *total = all;
-  return x + before;
+  const I sums = warp_scan(lane < THREADS / 32 ? s[lane] : I(0), lane);  // every warp scans the warps' sums
+  const I before = __shfl_sync(0xffffffffu, sums, warp > 0 ? warp - 1 : 0);
+  *total = __shfl_sync(0xffffffffu, sums, 31);
+  return warp > 0 ? x + before : x;
 }
 
 }  // namespace dm

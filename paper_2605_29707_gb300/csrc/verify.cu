@@ -41,11 +41,6 @@ __device__ __forceinline__ uint32_t dsmem_addr(const void* local, uint32_t rank)
   return r;
 }
 
-// Asks for `bytes` (a multiple of 16) at a 16-byte aligned address to be brought into L2.
-__device__ __forceinline__ void l2_prefetch_bulk(const void* p, uint32_t bytes) {
-  asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(p), "r"(bytes) : "memory");
-}
-
 __device__ __forceinline__ void better_of(float& v, int& id, float v2, int id2) {
   if (v2 > v || (v2 == v && id2 < id)) { v = v2; id = id2; }
 }

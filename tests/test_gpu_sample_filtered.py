@@ -83,6 +83,21 @@ def check(x, u, got, lp, T=None, k=None, p=None, m=None):
     assert close <= 1
 
 
+def run_and_check(x, dtype, u, **a):
+    """The rows by themselves (few: one kernel for latency), and four times over (many: the other)."""
+    got, lp = run(x, dtype, u, **a)
+    check(x, u, got, lp, **a)
+    rows, V = x.shape
+    stride, skew = x.stride(0), x.storage_offset()
+    buf = torch.empty(4 * rows * stride + skew, dtype=x.dtype, device=DEV)
+    y = torch.as_strided(buf, (4 * rows, V), (stride, 1), skew)
+    y.copy_(x.repeat(4, 1))
+    got, lp = run(y, dtype, u.repeat(4), **{k: v * 4 for k, v in a.items()})
+    for i in (0, 3):
+        check(x, u, got[i * rows:(i + 1) * rows], lp[i * rows:(i + 1) * rows], **a)
+    return got[:rows], lp[:rows]
+
+
 RULES = {
     "none": {},
     "temp": dict(T=[0.7, 1.0, 1.6, 0.3, 3.0, 0.05]),
@@ -104,8 +119,7 @@ RULES = {
 def test_draw_matches_the_plain_form(rule, dtype, V, pad, skew):
     x = logits(6, V, dtype, V + 11, pad=pad, skew=skew)
     u = uniforms(6, V)
-    got, lp = run(x, dtype, u, **RULES[rule])
-    check(x, u, got, lp, **RULES[rule])
+    run_and_check(x, dtype, u, **RULES[rule])
 
 
 @pytest.mark.parametrize("rule", sorted(RULES))
@@ -113,8 +127,7 @@ def test_draw_matches_the_plain_form(rule, dtype, V, pad, skew):
 def test_draw_full_vocabulary(rule, dtype, V):
     x = logits(6, V, dtype, 77, std=5.1)
     u = uniforms(6, 77)
-    got, lp = run(x, dtype, u, **RULES[rule])
-    check(x, u, got, lp, **RULES[rule])
+    run_and_check(x, dtype, u, **RULES[rule])
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
@@ -124,8 +137,7 @@ def test_draw_flat_and_sharp_rows(dtype, std, rule):
     """Rows of equal logits, rows so flat that most of the vocabulary stays, and rows with one survivor."""
     x = logits(6, 40003, dtype, 5, std=std)
     u = uniforms(6, 5)
-    got, lp = run(x, dtype, u, **RULES[rule])
-    check(x, u, got, lp, **RULES[rule])
+    run_and_check(x, dtype, u, **RULES[rule])
 
 
 @pytest.mark.parametrize("dtype,V", [(F32, 1 << 19), (BF16, (1 << 19) - 3)])
@@ -133,8 +145,7 @@ def test_draw_largest_vocabulary(dtype, V):
     x = logits(6, V, dtype, 6, std=3.0)
     u = uniforms(6, 6)
     for rule in ("none", "all"):
-        got, lp = run(x, dtype, u, **RULES[rule])
-        check(x, u, got, lp, **RULES[rule])
+        run_and_check(x, dtype, u, **RULES[rule])
 
 
 @pytest.mark.parametrize("rule", ["topk", "topp", "all", "none"])
@@ -143,8 +154,7 @@ def test_draw_ties(rule):
     x = (logits(6, 20011, F32, 8, std=1.5) * 2).round() / 2  # -0 among them
     u = uniforms(6, 8)
     for t, y in ((F32, x), (BF16, x.bfloat16())):
-        got, lp = run(y, t, u, **RULES[rule])
-        check(y, u, got, lp, **RULES[rule])
+        run_and_check(y.contiguous(), t, u, **RULES[rule])
 
 
 @pytest.mark.parametrize("order", ["rising", "falling"])
@@ -153,8 +163,7 @@ def test_draw_sorted_rows(order, rule):
     """All candidates side by side: at one end of the vocabulary."""
     x = logits(6, 30000, F32, 9).sort(dim=1, descending=order == "falling").values.contiguous()
     u = uniforms(6, 9)
-    got, lp = run(x, F32, u, **RULES[rule])
-    check(x, u, got, lp, **RULES[rule])
+    run_and_check(x, F32, u, **RULES[rule])
 
 
 def test_draw_masked_and_infinite_logits():
@@ -177,8 +186,7 @@ def test_draw_masked_and_infinite_logits():
         u = uniforms(10, 12)
         for a in ({}, dict(k=[40] * 10), dict(p=[0.9] * 10), dict(m=[0.05] * 10), dict(T=[0.0] * 10),
                   dict(T=[0.5] * 10, k=[2000] * 10, p=[0.8] * 10, m=[0.01] * 10)):
-            got, lp = run(x, dtype, u, **a)
-            check(x, u, got, lp, **a)
+            got, lp = run_and_check(x, dtype, u, **a)
             assert got[3] == 0 and got[4] == 0 and lp[3] == -math.inf
 
 
