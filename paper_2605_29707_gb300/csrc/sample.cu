@@ -33,8 +33,8 @@ namespace dm {
 constexpr int kDrawThreads = 256;   // threads of a CTA
 constexpr int kWarps = kDrawThreads / 32;
 constexpr int kDrawBatch = 4;       // 16-byte loads a thread has in flight
-constexpr int kLocalCap = 1024;     // candidates a CTA holds, a segment of them a warp
-constexpr int kListCap = 4096;      // candidates the cluster's first CTA can take
+constexpr int kLocalCap = 2048;     // candidates a CTA holds, a segment of them a warp
+constexpr int kListCap = 3072;      // candidates the cluster's first CTA can take
 constexpr int kMaxSteps = 264;      // of 32 units that a warp has of a slice
 constexpr int kBins = 512;          // of values, or of ids
 constexpr int kSubCap = 256;        // entries of one bin that are ranked against each other
@@ -159,7 +159,7 @@ struct DrawShared {  // dynamic shared memory
   uint32_t n_list[5];     // the first CTA: the cluster's candidates, by gathering
   float best[8 * kWarps]; // the greatest values of every warp's sample (read by the cluster)
   uint32_t slot[kSlots];  // the sample's mass by half octaves (read by the cluster)
-  int base, n_sub, bin, n_upto, n_in;
+  int n_sub, bin, n_upto, n_in, enough;
 };
 
 // A row's slice: ids [lo, lo + len), read in units of 16 bytes aligned in global memory.  Whole units are one load;
@@ -882,8 +882,12 @@ __device__ bool draw_from_sample(const Slice<T>& sl, const Vec<T> (&v)[8 / SP], 
     } else if (set.use_p) {
       tau = sampled_bound<SP>(sh, m, k, -0.5f * (1.f - set.top_p));  // a half of what may be left out of the sample
     }
-    if (set.use_m && !(set.use_k && set.use_p) && lane == 0) tau = fmaxf(tau, __double2float_rd(m + sh.floor));
     if (lane == 0) {
+      // under min-p nothing below m + T log(min_p) stays, m being at most the maximum (with top-k and top-p, top-p
+      // still goes by what top-k leaves)
+      const float low = set.use_m && !(set.use_k && set.use_p) ? __double2float_rd(m + sh.floor) : -INFINITY;
+      sh.enough = low >= tau ? 1 : set.top_k;  // candidates that there have to be
+      tau = fmaxf(tau, low);
       sh.m = m;
       sh.tau = fminf(tau, m);
     }
@@ -916,7 +920,7 @@ __device__ bool draw_from_sample(const Slice<T>& sl, const Vec<T> (&v)[8 / SP], 
     if (with_tail) add_masses(sh, 2 + attempt, rest, hits);
     push(sh, n_own, 3 + attempt);
     n = gathered(sh, 3 + attempt);
-    bool good = n >= 1 && n <= kListCap && (!set.use_k || n >= set.top_k);
+    bool good = n >= 1 && n <= kListCap && (!set.use_k || n >= sh.enough);
     if (with_tail) {
       tail = ld_cluster(&sh.tail[2 + attempt], 0);
       const float t = static_cast<float>(tail), h = static_cast<float>(ld_cluster(&sh.mass[2 + attempt], 0));
@@ -1115,7 +1119,7 @@ __global__ void __launch_bounds__(kDrawThreads, 4) filtered_draw_kernel(const Dr
   // ---- the candidates, to the first CTA if they are few
   u64 cut = 0;  // the order of the last id that stays
   bool cut_k = set.use_k, cut_p = set.use_p;  // still to be found
-  if ((sh.tau > -INFINITY || p.V <= kLocalCap) && !sc.inf) {
+  if ((sh.tau > -INFINITY || p.V <= 1024) && !sc.inf) {
     if (with_tail && sh.tau > -INFINITY) {
       // That bound is safe but low.  A nearer one, to be checked: where the groups' maxima below it carry a third of
       // what top-p may leave out.
@@ -1238,8 +1242,10 @@ __global__ void __launch_bounds__(kDrawThreads, 4) filtered_draw_kernel(const Dr
       const int bin = static_cast<int>(ld_cluster(reinterpret_cast<uint32_t*>(&sh.bin), 0));
       const int n_upto = static_cast<int>(ld_cluster(reinterpret_cast<uint32_t*>(&sh.n_upto), 0));
       const int n_in = static_cast<int>(ld_cluster(reinterpret_cast<uint32_t*>(&sh.n_in), 0));
-      fits = n_upto <= kListCap;
-      if (fits || n_in <= kListCap) {
+      // (as many as the warps' segments hold where the ids lie anyhow: five eighths of them)
+      constexpr int kSafe = kListCap < kLocalCap / 8 * 5 * SP ? kListCap : kLocalCap / 8 * 5 * SP;
+      fits = n_upto <= kSafe;
+      if (fits || n_in <= kSafe) {
         auto wanted = [&](float x) {
           const int b = value_bin(x, sc.m, scale);
           return b == bin || (fits && b < bin);
