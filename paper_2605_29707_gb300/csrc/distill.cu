@@ -12,9 +12,11 @@
 // the student agrees with the teacher.  Terms with q = 0 or rest = 0 are 0; a row of weight 0 has loss and
 // gradient 0 whatever its logits hold.
 //
-// Bound by DRAM.  For the loss, and for loss and gradient together, a cluster of eight CTAs holds the row
-// in shared memory: every logit is read once, and written once as a gradient.  The gradient alone, from the
-// two sums that the loss left, is one pass without a cluster.
+// Bound by DRAM.  For the loss, and for loss and gradient together, a cluster of CTAs holds the row in shared
+// memory: every logit is read once, and written once as a gradient.  A thread keeps the maximum of what it
+// reads and the sum relative to it; warps, the CTA and, with one exchange, the cluster join such pairs.  The
+// teacher's list is one warp's work.  The gradient alone, from the two sums that the loss left, is one pass
+// without a cluster.
 #include <math.h>
 
 #include "kernels.h"
@@ -107,19 +109,62 @@ __device__ __forceinline__ Place teacher_place(const DistillParams& p, size_t ro
   return e;
 }
 
-template <typename T, bool GRAD>
-__global__ void __launch_bounds__(kDistillThreads) distill_kernel(const DistillParams p) {
+// A maximum and the sum of 2^((x - m) k2) over what it is the maximum of; m = -inf: nothing.
+struct MaxSum {
+  float m, s;
+};
+__device__ __forceinline__ MaxSum join(MaxSum a, MaxSum b, float k2) {
+  const float m = fmaxf(a.m, b.m);
+  // (a NaN sum stays one; an empty side adds nothing)
+  const float sa = a.m == m ? a.s : a.s * ex2((a.m - m) * k2);
+  const float sb = b.m == m ? b.s : b.s * ex2((b.m - m) * k2);
+  return MaxSum{m, sa + sb};
+}
+__device__ __forceinline__ MaxSum warp_join(MaxSum v, float k2) {
+#pragma unroll
+  for (int o = 16; o; o >>= 1)
+    v = join(v, MaxSum{__shfl_xor_sync(0xffffffffu, v.m, o), __shfl_xor_sync(0xffffffffu, v.s, o)}, k2);
+  return v;
+}
+
+// 2^((x - base) k2) of a unit's elements.  fp32 logits: the difference first, which keeps the argument to 2.5 roundings
+// of itself.  16-bit logits: one multiply-add with -base k2, one instruction less of ten; the argument is then off by up
+// to a rounding of |base k2|, 2^-24 of some tens, which is far below what 8 or 11 bits of logit leave.
+template <typename T>
+__device__ __forceinline__ void unit_exp(const Vec<T>& f, float base, float k2, float (&e)[Vec<T>::kN]) {
+  float x[Vec<T>::kN];
+  unpack(f, x);
+  const float c = -base * k2;
+  if (sizeof(T) == 2 && fabsf(c) < 1e30f) {
+#pragma unroll
+    for (int i = 0; i < Vec<T>::kN; ++i) e[i] = ex2(fmaf(x[i], k2, c));
+  } else {  // (also where all the thread has is a mask's lowest value, whose product would overflow)
+#pragma unroll
+    for (int i = 0; i < Vec<T>::kN; ++i) e[i] = ex2((x[i] - base) * k2);
+  }
+}
+
+constexpr int kLanePlaces = kMaxTeacher / 32;  // places of the list that a lane of the list's warp has
+
+// The list as warp 0 holds it: place 32 i + lane.
+struct LanePlaces {
+  int id[kLanePlaces];
+  float x[kLanePlaces], q[kLanePlaces];
+};
+
+template <typename T, int SP, bool GRAD>
+__global__ void __launch_bounds__(kDistillThreads, 5) distill_kernel(const DistillParams p) {
   extern __shared__ __align__(16) unsigned char s_raw[];
   __shared__ int s_id[kMaxTeacher];
   __shared__ float s_q[kMaxTeacher];
-  __shared__ float s_red[kDistillThreads / 32];
-  __shared__ float s_part;     // this CTA's maximum, then (s_part2) its sum: read by the cluster
-  __shared__ float s_part2;
+  __shared__ MaxSum s_warp[kDistillThreads / 32];
+  __shared__ MaxSum s_part[SP];  // every CTA's ids that are not listed (written by the cluster)
+  __shared__ float s_a, s_base;
   T* s = reinterpret_cast<T*>(s_raw);
   constexpr int N = Vec<T>::kN;
-  const size_t row = blockIdx.x / kRowSplit;
-  const uint32_t part = cluster_ctarank();  // == blockIdx.x % kRowSplit
-  const int tid = threadIdx.x;
+  const unsigned row = blockIdx.x / SP;
+  const uint32_t part = SP > 1 ? cluster_ctarank() : 0;  // == blockIdx.x % SP
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int lo = min(p.V, static_cast<int>(part) * p.slice);
   const int len = min(p.V, lo + p.slice) - lo;
   const T* x = static_cast<const T*>(p.logits) + row * static_cast<size_t>(p.stride);
@@ -127,109 +172,218 @@ __global__ void __launch_bounds__(kDistillThreads) distill_kernel(const DistillP
   const int units = row_units<T>(shift, len);
   stage_slice<T, kDistillThreads>(s, x + lo, len, tid);
   const float w = p.weights ? __ldg(p.weights + row) : 1.f;
-  float rest;
-  const Place e = teacher_place<T, kDistillThreads>(p, row, x, 0, p.V, s_id, s_q, s_red, &rest);
+
+  // ---- the teacher's list, by warp 0: the student's logits, the teacher's probabilities, and what it leaves to the rest
+  LanePlaces e;
+  float rest = 0.f;
+  const int places = (p.kt + 31) / 32;  // of a lane
+  if (warp == 0) {
+    float t[kLanePlaces], top = -INFINITY, sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < kLanePlaces; ++i) {
+      const int j = 32 * i + lane;
+      e.id[i] = -1;
+      e.x[i] = t[i] = -INFINITY;
+      if (j < p.kt) {
+        const int id = __ldg(p.ids + row * static_cast<size_t>(p.kt) + j);
+        if (id >= 0 && id < p.V) {
+          e.id[i] = id;
+          t[i] = __ldg(p.scores + row * static_cast<size_t>(p.kt) + j);
+          e.x[i] = to_f32(x[id]);
+        }
+      }
+      if (!p.tail) t[i] *= p.inv_t;
+      top = fmaxf(top, t[i]);
+    }
+    top = p.tail ? 0.f : warp_max(top);
+#pragma unroll
+    for (int i = 0; i < kLanePlaces; ++i) {
+      e.q[i] = t[i] > -INFINITY || isnan(t[i]) ? expf(t[i] - top) : 0.f;
+      sum += e.q[i];
+    }
+    sum = warp_sum(sum);
+    if (p.tail) rest = fmaxf(0.f, 1.f - sum);
+#pragma unroll
+    for (int i = 0; i < kLanePlaces; ++i) {
+      if (i >= places) break;
+      if (!p.tail) e.q[i] = sum > 0.f ? e.q[i] / sum : 0.f;
+      if (32 * i + lane < p.kt) {
+        s_id[32 * i + lane] = e.id[i];
+        s_q[32 * i + lane] = e.q[i];
+      }
+    }
+  }
   cp_async_wait_all();
   __syncthreads();
 
   // ---- the listed ids leave the slice: what is left is the rest
-  T none;
-  from_f32(-INFINITY, &none);
-  if (e.id >= lo && e.id < lo + len) s[shift + e.id - lo] = none;
+  if (warp == 0) {
+    T none;
+    from_f32(-INFINITY, &none);
+#pragma unroll
+    for (int i = 0; i < kLanePlaces; ++i)
+      if (i < places && e.id[i] >= lo && e.id[i] < lo + len) s[shift + e.id[i] - lo] = none;
+  }
   __syncthreads();
   const Vec<T>* v = reinterpret_cast<const Vec<T>*>(s);
-  float mx = -INFINITY;
+  MaxSum mine{-INFINITY, 0.f};
   for (int q = tid; q < units; q += kDistillThreads) {
     Vec<T> f;
     f.raw = v[q].raw;
-#pragma unroll
-    for (int i = 0; i < N; ++i) mx = fmaxf(mx, to_f32(f.e[i]));
+    mine.m = fmaxf(mine.m, vec_max(f));
   }
-  mx = block_max<kDistillThreads>(mx, s_red, tid);
-  if (tid == 0) s_part = mx;
-  cluster_sync();
-  float m = -INFINITY;  // of the ids not listed
+  {
+    const float base = mine.m > -INFINITY ? mine.m : 0.f;
+    float sum[2] = {0.f, 0.f};
+    for (int q = tid; q < units; q += kDistillThreads) {
+      Vec<T> f;
+      f.raw = v[q].raw;
+      float e2[N];
+      unit_exp(f, base, p.k2, e2);
 #pragma unroll
-  for (int c = 0; c < kRowSplit; ++c) m = fmaxf(m, ld_cluster(&s_part, c));
-  const float base = m > -INFINITY ? m : 0.f;
-  float sum = 0.f;
-  for (int q = tid; q < units; q += kDistillThreads) {
-    Vec<T> f;
-    f.raw = v[q].raw;
-#pragma unroll
-    for (int i = 0; i < N; ++i) sum += ex2((to_f32(f.e[i]) - base) * p.k2);
+      for (int i = 0; i < N; ++i) sum[i & 1] += e2[i];
+    }
+    mine.s = sum[0] + sum[1];
   }
-  sum = block_sum<kDistillThreads>(sum, s_red, tid);
-  if (tid == 0) s_part2 = sum;
-  cluster_sync();
-  float r = 0.f;  // sum over the ids not listed, relative to their maximum
+  mine = warp_join(mine, p.k2);
+  if (lane == 0) s_warp[warp] = mine;
+  __syncthreads();
+  if (warp == 0) {
+    MaxSum all = s_warp[0];
 #pragma unroll
-  for (int c = 0; c < kRowSplit; ++c) r += ld_cluster(&s_part2, c);
-  cluster_arrive();  // done with the other CTAs' shared memory
+    for (int i = 1; i < kDistillThreads / 32; ++i) all = join(all, s_warp[i], p.k2);
+    if (SP == 1) {
+      if (lane == 0) s_part[0] = all;
+    } else if (lane < SP) {
+      st_cluster(reinterpret_cast<uint2*>(&s_part[part]), lane, make_uint2(__float_as_uint(all.m), __float_as_uint(all.s)));
+    }
+  }
+  if (SP > 1) cluster_sync();
+  else __syncthreads();
 
   // ---- every id: the rest and the listed ones, relative to the row's maximum
-  const float top = block_max<kDistillThreads>(fmaxf(e.x, m), s_red, tid);
-  const bool empty = !(top > -INFINITY) && !isnan(top);  // every logit is -inf
-  const float ref = empty ? 0.f : top;
-  const float mine = e.first ? ex2((e.x - ref) * p.k2) : 0.f;
-  const float listed = block_sum<kDistillThreads>(mine, s_red, tid);
-  const float m_top = m > -INFINITY ? m - ref : 0.f;
-  const float r_top = r * ex2(m_top * p.k2);
-  const float z = r_top + listed;
-  const float log_z = logf(z);  // relative to ref
-  const float log_r = m_top * p.inv_t + logf(r);
-  if (part == 0) {
-    float l = 0.f;
-    if (e.q > 0.f) l = empty ? INFINITY : e.q * (logf(e.q) - ((e.x - ref) * p.inv_t - log_z));
-    l = block_sum<kDistillThreads>(l, s_red, tid);
-    if (tid == 0) {
-      if (rest > 0.f) l += empty ? INFINITY : rest * (logf(rest) - (log_r - log_z));
-      p.loss[row] = w == 0.f ? 0.f : w * l;
-      if (p.lse) {
-        p.lse[2 * row] = empty ? -INFINITY : ref * p.inv_t + log_z;
-        p.lse[2 * row + 1] = ref * p.inv_t + log_r;
+  float scale = 0.f, inv_z = 0.f, ref = 0.f;
+  if (warp == 0) {
+    MaxSum r = s_part[0];
+#pragma unroll
+    for (int c = 1; c < SP; ++c) r = join(r, s_part[c], p.k2);
+    float top = r.m;
+    int distinct = 0;
+    unsigned firsts = 0;  // places whose id no earlier place has
+#pragma unroll
+    for (int i = 0; i < kLanePlaces; ++i) {
+      if (i >= places) break;
+      top = fmaxf(top, e.x[i]);
+      bool first = e.id[i] >= 0;
+      for (int j = 0; j < p.kt && j < 32 * i + lane; ++j) first = first && s_id[j] != e.id[i];
+      if (first) firsts |= 1u << i;
+      distinct += __popc(__ballot_sync(0xffffffffu, first));
+    }
+    top = warp_max(top);
+    if (distinct == p.V) rest = 0.f;                            // every id is listed
+    const bool empty = !(top > -INFINITY) && !isnan(r.s);       // every logit is -inf
+    ref = top > -INFINITY ? top : 0.f;
+    float listed = 0.f;
+#pragma unroll
+    for (int i = 0; i < kLanePlaces; ++i)
+      if (firsts >> i & 1) listed += ex2((e.x[i] - ref) * p.k2);
+    listed = warp_sum(listed);
+    const float m_top = r.m > -INFINITY ? r.m - ref : 0.f;
+    const float r_top = r.s * ex2(m_top * p.k2);
+    const float z = r_top + listed;
+    inv_z = z == 0.f ? 0.f : 1.f / z;
+    if (GRAD) {
+      scale = w == 0.f ? 0.f : (p.grad_loss ? __ldg(p.grad_loss + row) : 1.f) * w * p.inv_t;
+      if (lane == 0) {
+        // exp(z_v - log R) (R / Z - rest), with 2^((x - base) k2) = exp(z_v - log R) R
+        s_a = r.s == 0.f ? 0.f : scale * (r_top * inv_z - rest) / r.s;
+        s_base = r.m > -INFINITY ? r.m : 0.f;
+      }
+    }
+    if (part == 0) {
+      const float log_z = logf(z), log_r = m_top * p.inv_t + logf(r.s);  // relative to ref
+      float l = 0.f;
+#pragma unroll
+      for (int i = 0; i < kLanePlaces; ++i)
+        if (i < places && (e.q[i] > 0.f || isnan(e.q[i])))
+          l += empty ? INFINITY : e.q[i] * (logf(e.q[i]) - ((e.x[i] - ref) * p.inv_t - log_z));
+      l = warp_sum(l);
+      if (lane == 0) {
+        if (rest > 0.f) l += empty ? INFINITY : rest * (logf(rest) - (log_r - log_z));
+        p.loss[row] = w == 0.f ? 0.f : w * l;
+        if (p.lse) {
+          p.lse[2 * static_cast<size_t>(row)] = empty ? -INFINITY : ref * p.inv_t + log_z;
+          p.lse[2 * static_cast<size_t>(row) + 1] = ref * p.inv_t + log_r;
+        }
+      }
+    }
+    if (GRAD) {  // each first place's gradient, while the other warps wait for nothing more than s_a
+#pragma unroll
+      for (int i = 0; i < kLanePlaces; ++i) {
+        if (i >= places) break;
+        float q_all = 0.f;
+        if (firsts >> i & 1) {
+          for (int j = 0; j < p.kt; ++j) q_all += s_id[j] == e.id[i] ? s_q[j] : 0.f;
+          e.q[i] = w == 0.f ? 0.f : scale * (ex2((e.x[i] - ref) * p.k2) * inv_z - q_all);
+        } else {
+          e.id[i] = -1;
+        }
       }
     }
   }
   if (GRAD) {
-    const float up = p.grad_loss ? __ldg(p.grad_loss + row) : 1.f;
-    const float scale = w == 0.f ? 0.f : up * w * p.inv_t;
-    const float inv_z = z == 0.f ? 0.f : 1.f / z;
-    // exp(z_v - log R) (R / Z - rest), with 2^((x - base) k2) = exp(z_v - log R) r
-    const float a = r == 0.f ? 0.f : scale * (r_top * inv_z - rest) / r;
+    __syncthreads();
+    const float a = s_a, base = s_base;
     T* dx = static_cast<T*>(p.dlogits) + row * static_cast<size_t>(p.grad_stride) + lo;
     const bool zero = w == 0.f;
-    auto grad = [&](T xv) {
-      T g;
-      from_f32(zero ? 0.f : a * ex2((to_f32(xv) - base) * p.k2), &g);
+    auto grads = [&](int q) {
+      Vec<T> f;
+      f.raw = v[q].raw;
+      float e2[N];
+      if (zero) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) e2[i] = 0.f;
+      } else {
+        unit_exp(f, base, p.k2, e2);
+#pragma unroll
+        for (int i = 0; i < N; ++i) e2[i] *= a;
+      }
+      Vec<T> g;
+      pack(e2, &g);
       return g;
     };
     if (row_shift(dx) == shift) {
-      for (int q = tid; q < units; q += kDistillThreads) {
-        Vec<T> f, g;
-        f.raw = v[q].raw;
-#pragma unroll
-        for (int i = 0; i < N; ++i) g.e[i] = grad(f.e[i]);
-        const int i0 = q * N - shift;
-        if (i0 >= 0 && i0 + N <= len) {
-          *reinterpret_cast<uint4*>(dx + i0) = g.raw;
-        } else {
+      const int last = (shift + len) / N;  // one past the last whole unit
+      for (int q = (shift ? 1 : 0) + tid; q < last; q += kDistillThreads)
+        __stcs(reinterpret_cast<uint4*>(dx + (q * N - shift)), grads(q).raw);
+      if (tid < 2 && units > 0) {  // the first and the last unit, where they are not whole
+        const int q = tid == 0 ? 0 : last;
+        if (tid == 0 ? shift != 0 : last < units && (last > 0 || !shift)) {
+          const Vec<T> g = grads(q);
 #pragma unroll
           for (int i = 0; i < N; ++i)
-            if (i0 + i >= 0 && i0 + i < len) dx[i0 + i] = g.e[i];
+            if (q * N + i >= shift && q * N + i < shift + len) dx[q * N + i - shift] = g.e[i];
         }
       }
     } else {
-      for (int i = tid; i < len; i += kDistillThreads) dx[i] = grad(s[shift + i]);
+      for (int q = tid; q < units; q += kDistillThreads) {
+        const Vec<T> g = grads(q);
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+          if (q * N + i >= shift && q * N + i < shift + len) dx[q * N + i - shift] = g.e[i];
+      }
     }
     __syncthreads();  // the listed ids' places are written again
-    if (e.first && e.id >= lo && e.id < lo + len) {
-      T g;
-      from_f32(zero ? 0.f : scale * (mine * inv_z - e.q_all), &g);
-      dx[e.id - lo] = g;
+    if (warp == 0) {
+#pragma unroll
+      for (int i = 0; i < kLanePlaces; ++i)
+        if (i < places && e.id[i] >= lo && e.id[i] < lo + len) {
+          T g;
+          from_f32(e.q[i], &g);
+          dx[e.id[i] - lo] = g;
+        }
     }
   }
-  cluster_wait();
 }
 
 // The gradient from the sums that the loss left: one CTA per chunk of a row.
@@ -293,39 +447,57 @@ __global__ void __launch_bounds__(kGradThreads) distill_grad_kernel(const Distil
   }
 }
 
-template <typename T, bool GRAD>
-static cudaError_t launch_rows(const DistillParams& p, int rows, cudaStream_t stream) {
+template <typename T, int SP, bool GRAD>
+static cudaError_t launch_rows(DistillParams p, int rows, cudaStream_t stream) {
+  p.slice = ((p.V + SP - 1) / SP + 7) & ~7;
   const size_t smem = (static_cast<size_t>(p.slice) + 16) * sizeof(T);
-  cudaError_t e = ensure_smem_attr(reinterpret_cast<const void*>(distill_kernel<T, GRAD>), smem, false);
+  cudaError_t e = ensure_smem_attr(reinterpret_cast<const void*>(distill_kernel<T, SP, GRAD>), smem, false);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(static_cast<unsigned>(rows) * kRowSplit);
+  cfg.gridDim = dim3(static_cast<unsigned>(rows) * SP);
   cfg.blockDim = dim3(kDistillThreads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = stream;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = kRowSplit;
+  attr[0].val.clusterDim.x = SP;
   attr[0].val.clusterDim.y = 1;
   attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  e = cudaLaunchKernelEx(&cfg, distill_kernel<T, GRAD>, p);
+  cfg.numAttrs = SP > 1 ? 1 : 0;
+  e = cudaLaunchKernelEx(&cfg, distill_kernel<T, SP, GRAD>, p);
   return e != cudaSuccess ? e : cudaGetLastError();
+}
+
+// CTAs a row: eight, so that few rows use many SMs and the longest fit; halved while the rows alone keep four CTAs an SM
+// busy and five slices of twice the length fit an SM's shared memory.
+template <typename T, bool GRAD>
+static cudaError_t launch_split(const DistillParams& p, int rows, cudaStream_t stream) {
+  int dev = 0, sms = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+  if (e != cudaSuccess) return e;
+  int split = 8;
+  while (split > 1 && static_cast<long long>(rows) * split > 4 * sms && p.V / (split / 2) * sizeof(T) <= (44 << 10)) split /= 2;
+  switch (split) {
+    case 8: return launch_rows<T, 8, GRAD>(p, rows, stream);
+    case 4: return launch_rows<T, 4, GRAD>(p, rows, stream);
+    case 2: return launch_rows<T, 2, GRAD>(p, rows, stream);
+  }
+  return launch_rows<T, 1, GRAD>(p, rows, stream);
 }
 
 template <typename T>
 static cudaError_t launch_type(const DistillParams& p, int rows, cudaStream_t stream) {
-  if (p.loss) return p.dlogits ? launch_rows<T, true>(p, rows, stream) : launch_rows<T, false>(p, rows, stream);
+  if (p.loss) return p.dlogits ? launch_split<T, true>(p, rows, stream) : launch_split<T, false>(p, rows, stream);
   const int chunks = (p.V + kGradChunk - 1) / kGradChunk;
   if (static_cast<long long>(rows) * chunks > 0x7fffffffLL) return cudaErrorInvalidValue;
   distill_grad_kernel<T><<<static_cast<unsigned>(rows) * chunks, kGradThreads, 0, stream>>>(p, chunks);
   return cudaGetLastError();
 }
 
-cudaError_t launch_distill(DistillParams p, int dtype, int rows, cudaStream_t stream) {
-  if (rows <= 0 || rows > 0x7fffffff / kRowSplit) return cudaErrorInvalidValue;
-  p.slice = ((p.V + kRowSplit - 1) / kRowSplit + 7) & ~7;
+cudaError_t launch_distill(const DistillParams& p, int dtype, int rows, cudaStream_t stream) {
+  if (rows <= 0 || rows > 0x7fffffff / 8) return cudaErrorInvalidValue;
   if (p.V > kMaxDistillVocab) return cudaErrorInvalidValue;
   if (dtype == kF32) return launch_type<float>(p, rows, stream);
   if (dtype == kBf16) return launch_type<__nv_bfloat16>(p, rows, stream);

@@ -278,6 +278,10 @@ struct DrawParams {
   int slice;                 // set by the launch: ids per CTA
 };
 cudaError_t launch_filtered_draw(const DrawParams& p, int dtype, int rows, cudaStream_t stream);
+// The same by element type (one translation unit each).
+cudaError_t launch_draw_f32(const DrawParams& p, int rows, cudaStream_t stream);
+cudaError_t launch_draw_bf16(const DrawParams& p, int rows, cudaStream_t stream);
+cudaError_t launch_draw_f16(const DrawParams& p, int rows, cudaStream_t stream);
 
 struct DistillParams {
   const void* logits;  // [rows][stride]
@@ -295,6 +299,6 @@ struct DistillParams {
   long long grad_stride;
   int slice;             // set by the launch: ids per CTA
 };
-cudaError_t launch_distill(DistillParams p, int dtype, int rows, cudaStream_t stream);
+cudaError_t launch_distill(const DistillParams& p, int dtype, int rows, cudaStream_t stream);
 
 }  // namespace dm

@@ -12,8 +12,6 @@
 
 namespace dm {
 
-constexpr int kRowSplit = 8;  // CTAs (one cluster) per row
-
 // ------------------------------------------------------------------ element types
 __device__ __forceinline__ float to_f32(float x) { return x; }
 __device__ __forceinline__ float to_f32(__nv_bfloat16 x) { return __bfloat162float(x); }
@@ -44,6 +42,43 @@ __device__ __forceinline__ float ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
+}
+
+// The unit's elements in fp32, and back with one rounding each (pairs of 16-bit elements share an instruction).
+__device__ __forceinline__ void unpack(const Vec<float>& f, float (&v)[4]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = f.e[i];
+}
+__device__ __forceinline__ void unpack(const Vec<__nv_bfloat16>& f, float (&v)[8]) {
+  const uint32_t* w = reinterpret_cast<const uint32_t*>(f.e);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    v[2 * i] = __uint_as_float(w[i] << 16);
+    v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+  }
+}
+__device__ __forceinline__ void unpack(const Vec<__half>& f, float (&v)[8]) {
+  const __half2* h = reinterpret_cast<const __half2*>(f.e);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float2 t = __half22float2(h[i]);
+    v[2 * i] = t.x;
+    v[2 * i + 1] = t.y;
+  }
+}
+__device__ __forceinline__ void pack(const float (&v)[4], Vec<float>* f) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) f->e[i] = v[i];
+}
+__device__ __forceinline__ void pack(const float (&v)[8], Vec<__nv_bfloat16>* f) {
+  __nv_bfloat162* h = reinterpret_cast<__nv_bfloat162*>(f->e);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) h[i] = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+}
+__device__ __forceinline__ void pack(const float (&v)[8], Vec<__half>* f) {
+  __half2* h = reinterpret_cast<__half2*>(f->e);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) h[i] = __floats2half2_rn(v[2 * i], v[2 * i + 1]);
 }
 
 // The greatest of the unit's elements; NaN never is (-inf if there is nothing else).
