@@ -162,7 +162,7 @@ struct DrawShared {  // dynamic shared memory
   uint32_t n_list[5];     // the first CTA: the cluster's candidates, by gathering
   float best[8 * kWarps]; // the greatest values of every warp's sample (read by the cluster)
   uint32_t slot[kSlots];  // the sample's mass by half octaves (read by the cluster)
-  int n_sub, bin, n_upto, n_in, enough;
+  int n_sub, bin, n_upto, n_in, by_min_p;
 };
 
 // A row's slice: ids [lo, lo + len), read in units of 16 bytes aligned in global memory.  Whole units are one load;
@@ -889,7 +889,7 @@ __device__ bool draw_from_sample(const Slice<T>& sl, const Vec<T> (&v)[8 / SP], 
       // under min-p nothing below m + T log(min_p) stays, m being at most the maximum (with top-k and top-p, top-p
       // still goes by what top-k leaves)
       const float low = set.use_m && !(set.use_k && set.use_p) ? __double2float_rd(m + sh.floor) : -INFINITY;
-      sh.enough = low >= tau ? 1 : set.top_k;  // candidates that there have to be
+      sh.by_min_p = low >= tau;
       tau = fmaxf(tau, low);
       sh.m = m;
       sh.tau = fminf(tau, m);
@@ -923,11 +923,11 @@ __device__ bool draw_from_sample(const Slice<T>& sl, const Vec<T> (&v)[8 / SP], 
     if (with_tail) add_masses(sh, 2 + attempt, rest, hits);
     push(sh, n_own, 3 + attempt);
     n = gathered(sh, 3 + attempt);
-    bool good = n >= 1 && n <= kListCap && (!set.use_k || n >= sh.enough);
+    bool good = n >= 1 && n <= kListCap && (!set.use_k || sh.by_min_p || n >= set.top_k);
     if (with_tail) {
       tail = ld_cluster(&sh.tail[2 + attempt], 0);
       const float t = static_cast<float>(tail), h = static_cast<float>(ld_cluster(&sh.mass[2 + attempt], 0));
-      const bool held = t * 1.0001f <= (1.f - set.top_p) * (t + h);
+      const bool held = sh.by_min_p || t * 1.0001f <= (1.f - set.top_p) * (t + h);
       if (!held && attempt == 0) {
         // The sample missed what carries the mass: its lower part, scaled up to the row, against the row's own mass.
         if (warp == 0) {
@@ -1046,7 +1046,7 @@ __global__ void __launch_bounds__(kDrawThreads, 4) filtered_draw_kernel(const Dr
 
   // ---- what bounds the candidates from below
   // top-k: where every CTA has ceil(k / 8) groups of elements whose maxima reach a value, k elements do
-  const int in_cta = (set.top_k + SP - 1) / SP;
+  const int in_cta = set.use_k ? (set.top_k + SP - 1) / SP : 0;
   const bool small_k = in_cta <= 64;
   const bool bound_k = set.use_k && in_cta <= 128;
   if (bound_k) {  // 128 groups, or 256
@@ -1245,9 +1245,11 @@ __global__ void __launch_bounds__(kDrawThreads, 4) filtered_draw_kernel(const Dr
       const int bin = static_cast<int>(ld_cluster(reinterpret_cast<uint32_t*>(&sh.bin), 0));
       const int n_upto = static_cast<int>(ld_cluster(reinterpret_cast<uint32_t*>(&sh.n_upto), 0));
       const int n_in = static_cast<int>(ld_cluster(reinterpret_cast<uint32_t*>(&sh.n_in), 0));
-      // (as many as the warps' segments hold where the ids lie anyhow: five eighths of them)
+      // Down to the border they are gathered if they can be sorted, else those in its bin are (as many as the warps'
+      // segments hold where the ids lie anyhow: five eighths of them): the first CTA alone takes longer over a long list
+      // than the cluster over two more passes (1500 of 151936 ids kept: 160 us against 100).
       constexpr int kSafe = kListCap < kLocalCap / 8 * 5 * SP ? kListCap : kLocalCap / 8 * 5 * SP;
-      fits = n_upto <= kSafe;
+      fits = n_upto <= kSort;
       if (fits || n_in <= kSafe) {
         auto wanted = [&](float x) {
           const int b = value_bin(x, sc.m, scale);
