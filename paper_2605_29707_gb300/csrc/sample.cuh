@@ -37,6 +37,7 @@ constexpr int kDrawThreads = 256;   // threads of a CTA
 constexpr int kWarps = kDrawThreads / 32;
 constexpr int kDrawBatch = 4;       // 16-byte loads a thread has in flight
 constexpr int kLocalCap = 2048;     // candidates a CTA holds, a segment of them a warp
+constexpr int kSeg = kLocalCap / kWarps;
 constexpr int kListCap = 3072;      // candidates the cluster's first CTA can take
 constexpr int kMaxSteps = 264;      // of 32 units that a warp has of a slice
 constexpr int kBins = 512;          // of values, or of ids
@@ -589,7 +590,6 @@ __device__ __forceinline__ void finish_list(int n, u64 tail, const Settings& set
 // The warp's candidates, n of them, into the first CTA's list (as far as they fit); more than a segment: not all are
 // there, and the list counts as full.
 __device__ __forceinline__ void push(DrawShared& sh, int n, int round) {
-  constexpr int kSeg = kLocalCap / kWarps;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (!n) return;
   int to = 0;
@@ -620,18 +620,17 @@ __device__ __forceinline__ int gathered(DrawShared& sh, int round) {
   return static_cast<int>(ld_cluster(&sh.n_list[round], 0));
 }
 
-// Appends the elements of a unit that `wanted` says to the warp's segment of the local list; *n: how many it has.
+// Appends the elements of a unit that `wanted` says to the warp's segment `seg` of a list; *n: how many it has.
 template <typename T, typename W>
-__device__ __forceinline__ void append(const Slice<T>& sl, const Vec<T>& f, int q, int* n, DrawShared& sh, W&& wanted) {
-  constexpr int kSeg = kLocalCap / kWarps;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+__device__ __forceinline__ void append(const Slice<T>& sl, const Vec<T>& f, int q, int* n, uint2* seg, int cap, W&& wanted) {
+  const int lane = threadIdx.x & 31;
 #pragma unroll
   for (int i = 0; i < Vec<T>::kN; ++i) {
     const float x = to_f32(f.e[i]);
     const bool hit = wanted(x) && sl.holds(q, i);
     const unsigned who = __ballot_sync(0xffffffffu, hit);
     const int at = *n + __popc(who & ((1u << lane) - 1u));
-    if (hit && at < kSeg) sh.local[warp * kSeg + at] = make_uint2(__float_as_uint(x), sl.id(q, i));
+    if (hit && at < cap) seg[at] = make_uint2(__float_as_uint(x), sl.id(q, i));
     *n += __popc(who);
   }
 }
@@ -883,7 +882,7 @@ __device__ bool draw_from_sample(const Slice<T>& sl, const Vec<T> (&v)[8 / SP], 
     if (set.use_k) {
       tau = jth_greatest<kPer>(b, nth);
     } else if (set.use_p) {
-      tau = sampled_bound<SP>(sh, m, k, -0.5f * (1.f - set.top_p));  // a half of what may be left out of the sample
+      tau = sampled_bound<SP>(sh, m, k, -0.6f * (1.f - set.top_p));  // a part of what may be left out of the sample
     }
     if (lane == 0) {
       // under min-p nothing below m + T log(min_p) stays, m being at most the maximum (with top-k and top-p, top-p
@@ -918,7 +917,7 @@ __device__ bool draw_from_sample(const Slice<T>& sl, const Vec<T> (&v)[8 / SP], 
           hits += x >= tau ? e : 0.f;
         }
       }
-      if (__any_sync(0xffffffffu, vec_max(f) >= tau)) append<T>(sl, f, q, &n_own, sh, [&](float x) { return x >= tau; });
+      if (__any_sync(0xffffffffu, vec_max(f) >= tau)) append<T>(sl, f, q, &n_own, sh.local + warp * kSeg, kSeg, [&](float x) { return x >= tau; });
     });
     if (with_tail) add_masses(sh, 2 + attempt, rest, hits);
     push(sh, n_own, 3 + attempt);
@@ -933,7 +932,7 @@ __device__ bool draw_from_sample(const Slice<T>& sl, const Vec<T> (&v)[8 / SP], 
         if (warp == 0) {
           const float unit = static_cast<float>(p.V) / (static_cast<float>(SP * kDrawThreads * kSample * N) * 65536.f) *
                              ex2(fmaf(-m, k, 0.5f * static_cast<float>(half_octave(m, k))));
-          const float next = sampled_bound<SP>(sh, m, k, (1.f - set.top_p) * 0.6f * (t + h) * 0x1p-44f / unit);
+          const float next = sampled_bound<SP>(sh, m, k, (1.f - set.top_p) * 0.2f * (t + h) * 0x1p-44f / unit);
           if (lane == 0) sh.tau = fminf(next, tau);
         }
         __syncthreads();
@@ -1168,7 +1167,7 @@ __global__ void __launch_bounds__(kDrawThreads, 4) filtered_draw_kernel(const Dr
             hits += x >= tau ? e : 0.f;
           }
         }
-        if (__any_sync(0xffffffffu, vec_max(f) >= tau)) append<T>(sl, f, q, &n_own, sh, [&](float x) { return x >= tau; });
+        if (__any_sync(0xffffffffu, vec_max(f) >= tau)) append<T>(sl, f, q, &n_own, sh.local + warp * kSeg, kSeg, [&](float x) { return x >= tau; });
       });
       if (lane == 0) sh.n_warp[warp] = n_own;
       if (with_tail) add_masses(sh, attempt, rest, hits);
@@ -1183,8 +1182,7 @@ __global__ void __launch_bounds__(kDrawThreads, 4) filtered_draw_kernel(const Dr
     const float scale = tau > -INFINITY && sc.m > tau ? static_cast<float>(kBins) / (sc.m - tau) * 0.9999f : 0.f;
     bool fits = n <= kListCap;
     if (!fits && with_tail) {
-      constexpr int kSeg = kLocalCap / kWarps;
-      const int n_own = sh.n_warp[warp];
+          const int n_own = sh.n_warp[warp];
       const bool listed = __syncthreads_and(n_own <= kSeg);  // the local list has them all
       // the candidates' weights by value (from the list, or from the slice where it has more than the list holds)
       for (int i = tid; i < kBins; i += kDrawThreads) sh.bins[i] = make_uint4(0, 0, 0, 0);
@@ -1195,13 +1193,25 @@ __global__ void __launch_bounds__(kDrawThreads, 4) filtered_draw_kernel(const Dr
           add_to_bin(&sh.bins[value_bin(x, sc.m, scale)], weight(x, sc, sh.pow2));
         }
       } else {
-        sl.each([&](const Vec<T>& f, int q) {
-#pragma unroll
-          for (int i = 0; i < N; ++i) {
-            const float x = to_f32(f.e[i]);
-            if (x >= tau && sl.holds(q, i)) add_to_bin(&sh.bins[value_bin(x, sc.m, scale)], weight(x, sc, sh.pow2));
+        // (gathered by the warp first, so that whole warps compute weights; the list's memory is free meanwhile)
+        constexpr int kPart = kListCap / kWarps;
+        uint2* part_list = sh.list + warp * kPart;
+        int held = 0;
+        auto flush = [&] {
+          __syncwarp();
+          for (int e = lane; e < held; e += 32) {
+            const float x = __uint_as_float(part_list[e].x);
+            add_to_bin(&sh.bins[value_bin(x, sc.m, scale)], weight(x, sc, sh.pow2));
           }
+          __syncwarp();
+          held = 0;
+        };
+        sl.each([&](const Vec<T>& f, int q) {
+          if (!__any_sync(0xffffffffu, vec_max(f) >= tau)) return;
+          append<T>(sl, f, q, &held, part_list, kPart, [&](float x) { return x >= tau; });
+          if (held > kPart - 32 * N) flush();
         });
+        flush();
       }
       cluster_sync();
       // the bin that holds top-p's border, found by the first CTA
@@ -1269,7 +1279,7 @@ __global__ void __launch_bounds__(kDrawThreads, 4) filtered_draw_kernel(const Dr
         } else {
           sl.each([&](const Vec<T>& f, int q) {
             if (__any_sync(0xffffffffu, vec_max(f) >= tau))
-              append<T>(sl, f, q, &left, sh, [&](float x) { return x >= tau && wanted(x); });
+              append<T>(sl, f, q, &left, sh.local + warp * kSeg, kSeg, [&](float x) { return x >= tau && wanted(x); });
           });
         }
         push(sh, left, 2);
