@@ -148,7 +148,7 @@ struct DrawShared {  // dynamic shared memory
   u64 pow2[32];
   u64 scan[kWarps];
   u64 sum;                // kept mass of this CTA (read by the cluster)
-  u64 tail[4], mass[4];   // the first CTA: mass of the ids that are no candidates, and of those that are, by gathering
+  u64 tail[5], mass[5];   // the first CTA: mass of the ids that are no candidates, and of those that are, by gathering
   u64 need, result, below;
   u64 cut;                // the first CTA: the border of top-p (read by the cluster)
   double floor;           // T log(min_p)
@@ -157,10 +157,10 @@ struct DrawShared {  // dynamic shared memory
   float red[kWarps], red2[kWarps];
   float max, aux;         // this CTA's maximum, and its part of the candidates' bound (read by the cluster)
   float k_hi, k_lo;
-  float m, top, tau, guess, lowest;  // lowest: the least value that min-p keeps
+  float m, top, tau, guess, below_guess, lowest;  // lowest: the least value that min-p keeps
   uint32_t key;
   int n_warp[kWarps];  // entries of the warps' segments of local; more than a segment: not all are there
-  uint32_t n_list[5];     // the first CTA: the cluster's candidates, by gathering
+  uint32_t n_list[6];     // the first CTA: the cluster's candidates, by gathering
   float best[8 * kWarps]; // the greatest values of every warp's sample (read by the cluster)
   uint32_t slot[kSlots];  // the sample's mass by half octaves (read by the cluster)
   int n_sub, bin, n_upto, n_in, by_min_p;
@@ -919,13 +919,13 @@ __device__ bool draw_from_sample(const Slice<T>& sl, const Vec<T> (&v)[8 / SP], 
       }
       if (__any_sync(0xffffffffu, vec_max(f) >= tau)) append<T>(sl, f, q, &n_own, sh.local + warp * kSeg, kSeg, [&](float x) { return x >= tau; });
     });
-    if (with_tail) add_masses(sh, 2 + attempt, rest, hits);
-    push(sh, n_own, 3 + attempt);
-    n = gathered(sh, 3 + attempt);
+    if (with_tail) add_masses(sh, 3 + attempt, rest, hits);
+    push(sh, n_own, 4 + attempt);
+    n = gathered(sh, 4 + attempt);
     bool good = n >= 1 && n <= kListCap && (!set.use_k || sh.by_min_p || n >= set.top_k);
     if (with_tail) {
-      tail = ld_cluster(&sh.tail[2 + attempt], 0);
-      const float t = static_cast<float>(tail), h = static_cast<float>(ld_cluster(&sh.mass[2 + attempt], 0));
+      tail = ld_cluster(&sh.tail[3 + attempt], 0);
+      const float t = static_cast<float>(tail), h = static_cast<float>(ld_cluster(&sh.mass[3 + attempt], 0));
       const bool held = sh.by_min_p || t * 1.0001f <= (1.f - set.top_p) * (t + h);
       if (!held && attempt == 0) {
         // The sample missed what carries the mass: its lower part, scaled up to the row, against the row's own mass.
@@ -970,6 +970,31 @@ __device__ bool draw_from_sample(const Slice<T>& sl, const Vec<T> (&v)[8 / SP], 
   }
   cluster_sync();  // this CTA stays until the others, which read its counts, have left
   return true;
+}
+
+// By one warp: the value below which the groups' maxima carry at most `most` (in units of 2^-20), or, if that is
+// negative, at most its share -most of what they carry together; sh.below_guess: what they do carry below it.
+template <int SP>
+__device__ float maxima_bound(DrawShared& sh, const Scale& sc, float most) {
+  const int lane = threadIdx.x & 31;
+  float a = 0.f, b = 0.f;  // half octaves 2 lane and 2 lane + 1
+#pragma unroll
+  for (int c = 0; c < SP; ++c) {
+    a += static_cast<float>(ld_cluster(&sh.octave[2 * lane], c));
+    b += static_cast<float>(ld_cluster(&sh.octave[2 * lane + 1], c));
+  }
+  float below = a + b;  // this lane's and all lower weights
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const float y = __shfl_down_sync(0xffffffffu, below, o);
+    if (lane + o < 32) below += y;
+  }
+  if (most < 0.f) most *= -__shfl_sync(0xffffffffu, below, 0);
+  const unsigned whole = __ballot_sync(0xffffffffu, below <= most), half = __ballot_sync(0xffffffffu, below - a <= most);
+  const int first = min(whole ? 2 * (__ffs(whole) - 1) : kOctaves, half ? 2 * (__ffs(half) - 1) + 1 : kOctaves);
+  const float left = __shfl_sync(0xffffffffu, first & 1 ? below - a : below, min(first, kOctaves - 1) / 2);
+  if (lane == 0) sh.below_guess = first < kOctaves ? left : 0.f;
+  return sc.m - 0.5f * static_cast<float>(first) / sc.k_hi;
 }
 
 template <typename T, int SP>
@@ -1026,9 +1051,9 @@ __global__ void __launch_bounds__(kDrawThreads, 4) filtered_draw_kernel(const Dr
     sh.k_hi = k;
     sh.k_lo = k > 0.f && k < 1.0e38f ? (fmaf(-k, set.temp, kLog2eHi) + kLog2eLo) / set.temp : 0.f;
 #pragma unroll
-    for (int i = 0; i < 5; ++i) sh.n_list[i] = 0;
+    for (int i = 0; i < 6; ++i) sh.n_list[i] = 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) sh.tail[i] = sh.mass[i] = 0;
+    for (int i = 0; i < 5; ++i) sh.tail[i] = sh.mass[i] = 0;
   }
   __syncthreads();
   if (sampled && (set.use_k || set.use_p || set.use_m))
@@ -1132,22 +1157,8 @@ __global__ void __launch_bounds__(kDrawThreads, 4) filtered_draw_kernel(const Dr
         atomicAdd(&sh.octave[min(static_cast<int>(-2.f * t), kOctaves - 1)], static_cast<uint32_t>(ex2(t) * 0x1p20f));
       cluster_sync();
       if (warp == 0) {
-        float a = 0.f, b = 0.f;  // half octaves 2 lane and 2 lane + 1
-#pragma unroll
-        for (int c = 0; c < SP; ++c) {
-          a += static_cast<float>(ld_cluster(&sh.octave[2 * lane], c));
-          b += static_cast<float>(ld_cluster(&sh.octave[2 * lane + 1], c));
-        }
-        float below = a + b;  // this lane's and all lower weights
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-          const float y = __shfl_down_sync(0xffffffffu, below, o);
-          if (lane + o < 32) below += y;
-        }
-        const float most = (1.f - set.top_p) * (1.f / 3.f) * __shfl_sync(0xffffffffu, below, 0);
-        const unsigned whole = __ballot_sync(0xffffffffu, below <= most), half = __ballot_sync(0xffffffffu, below - a <= most);
-        const int first = min(whole ? 2 * (__ffs(whole) - 1) : kOctaves, half ? 2 * (__ffs(half) - 1) + 1 : kOctaves);
-        if (lane == 0) sh.guess = fmaxf(sh.tau, sc.m - 0.5f * static_cast<float>(first) / sc.k_hi);
+        const float guess = maxima_bound<SP>(sh, sc, -(1.f - set.top_p) * (1.f / 3.f));
+        if (lane == 0) sh.guess = fmaxf(sh.tau, guess);
       }
       __syncthreads();
     }
@@ -1177,7 +1188,13 @@ __global__ void __launch_bounds__(kDrawThreads, 4) filtered_draw_kernel(const Dr
       tail = ld_cluster(&sh.tail[attempt], 0);
       const float t = static_cast<float>(tail), h = static_cast<float>(ld_cluster(&sh.mass[attempt], 0));
       if (tau == sh.tau || t * 1.0001f <= (1.f - set.top_p) * (t + h)) break;  // every id that can stay is above tau
-      tau = sh.tau;
+      // too high: lower by what the maxima below it turned out to stand for; then the safe bound
+      if (attempt == 0 && warp == 0) {
+        const float next = maxima_bound<SP>(sh, sc, sh.below_guess * 0.4f * (1.f - set.top_p) * (t + h) / t);
+        if (lane == 0) sh.guess = fmaxf(sh.tau, fminf(next, tau));
+      }
+      __syncthreads();
+      tau = attempt == 0 && sh.guess < tau ? sh.guess : sh.tau;
     }
     const float scale = tau > -INFINITY && sc.m > tau ? static_cast<float>(kBins) / (sc.m - tau) * 0.9999f : 0.f;
     bool fits = n <= kListCap;
@@ -1282,8 +1299,8 @@ __global__ void __launch_bounds__(kDrawThreads, 4) filtered_draw_kernel(const Dr
               append<T>(sl, f, q, &left, sh.local + warp * kSeg, kSeg, [&](float x) { return x >= tau && wanted(x); });
           });
         }
-        push(sh, left, 2);
-        n = gathered(sh, 2);
+        push(sh, left, 3);
+        n = gathered(sh, 3);
         fits = fits && n <= kListCap;
         if (!fits && n <= kListCap) {  // the border's bin decides the border
           if (part == 0) {
