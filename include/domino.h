@@ -281,9 +281,10 @@ enum domino_dtype { DOMINO_F32 = 0, DOMINO_BF16 = 1, DOMINO_F16 = 2 };
  *   exceeds u times the kept mass (u outside [0, 1), or NaN, is clamped to it).
  * T <= 0 or NaN draws the first id (argmax, equal values: the lowest id).  Ids of logit -inf or NaN are
  * never drawn; a row without any other gives id 0 and logp -inf; where logits are +inf, they share the
- * mass evenly.  Sums are exact integers of 2^-44 of the greatest weight: the draw does not depend on the
- * order in which they are formed, and borders (of top_p, of u) lie within about 1e-11 of the mass of
- * where exact arithmetic puts them.
+ * mass evenly.  The weights of the ids that can stay are integers of 2^-44 of the greatest, whose sums
+ * are exact in any order; under top_p the mass of the others is added up in fp32.  Borders (of top_p, of
+ * u) lie within about 1e-7 of the mass of where exact arithmetic puts them, and the same call gives the
+ * same draw.
  *   logits: device [rows, row_stride] of `dtype`, element-aligned; ids 0 .. V - 1 of a row are read,
  *     row_stride >= V.  V <= 524288 (the sum of the weights fits 63 bits).
  *   temperature, top_p, min_p (fp32) and top_k (int32): device [rows], or NULL (T = 1, filter off).
@@ -332,7 +333,7 @@ DOMINO_API int domino_verify_tree_filtered(const void* target_logits, int dtype,
  * of weight 0 has loss and gradient 0, whatever its logits hold; a row whose logits are all -inf has
  * loss +inf (0 where it is weighted 0, or teaches nothing).  Sums in fp32, in a fixed order.
  *   logits: device [rows, row_stride] of `dtype`, element-aligned, finite or -inf; row_stride >= V;
- *     V <= 8 * 49152.  teacher_ids int32 [rows, kt], teacher_scores fp32 [rows, kt] (finite or -inf),
+ *     V <= 524288.  teacher_ids int32 [rows, kt], teacher_scores fp32 [rows, kt] (finite or -inf),
  *     1 <= kt <= 256.  weights fp32 [rows] or NULL (1); grad_loss fp32 [rows] or NULL (1): the upstream
  *     gradient of the row's loss.  temperature > 0 with 1 / T finite in fp32.
  * Outputs (device): loss fp32 [rows]; lse fp32 [rows, 2]: the log-sum-exp of z over every id and over

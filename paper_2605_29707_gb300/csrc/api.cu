@@ -938,11 +938,11 @@ namespace {
 bool aligned(const void* p, size_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
 
 // What every entry point on rows of logits asks of them; `rows` CTA clusters are launched.
-int check_rows(const void* logits, int dtype, int64_t stride, long long rows, int V, int max_v) {
+int check_rows(const void* logits, int dtype, int64_t stride, long long rows, int V) {
   if (!logits || rows < 1 || V < 1 || stride < V) return DOMINO_ERR_INVALID_ARG;
   if (rows > 0x7fffffffLL / 8) return DOMINO_ERR_INVALID_ARG;
   if (dtype != DOMINO_F32 && dtype != DOMINO_BF16 && dtype != DOMINO_F16) return DOMINO_ERR_UNSUPPORTED;
-  if (V > max_v) return DOMINO_ERR_UNSUPPORTED;
+  if (V > dm::kMaxRowVocab) return DOMINO_ERR_UNSUPPORTED;
   const size_t size = dtype == DOMINO_F32 ? 4 : 2;
   // the last row's end stays addressable
   if (stride > static_cast<int64_t>((1LL << 62) / size) / rows) return DOMINO_ERR_INVALID_ARG;
@@ -967,7 +967,7 @@ int enqueue_draw(const dm::DrawParams& d, int dtype, long long rows, cudaStream_
 int run_distill(const void* logits, int dtype, int64_t row_stride, const int32_t* teacher_ids,
                 const float* teacher_scores, const float* weights, const float* grad_loss, float temperature, int mode,
                 int rows, int V, int kt, float* loss, float* lse, void* dlogits, int64_t grad_stride, void* stream) {
-  int rc = check_rows(logits, dtype, row_stride, rows, V, dm::kMaxDistillVocab);
+  int rc = check_rows(logits, dtype, row_stride, rows, V);
   if (rc != DOMINO_OK) return rc;
   if (!teacher_ids || !teacher_scores || kt < 1) return DOMINO_ERR_INVALID_ARG;
   if (!aligned(teacher_ids, 4) || !aligned(teacher_scores, 4) || !aligned(weights, 4) || !aligned(grad_loss, 4) ||
@@ -978,7 +978,7 @@ int run_distill(const void* logits, int dtype, int64_t row_stride, const int32_t
   if (mode != DOMINO_DISTILL_RENORM && mode != DOMINO_DISTILL_TAIL) return DOMINO_ERR_INVALID_ARG;
   if (kt > dm::kMaxTeacher) return DOMINO_ERR_UNSUPPORTED;
   if (dlogits) {
-    rc = check_rows(dlogits, dtype, grad_stride, rows, V, dm::kMaxDistillVocab);
+    rc = check_rows(dlogits, dtype, grad_stride, rows, V);
     if (rc != DOMINO_OK) return rc;
     if (dlogits == logits && grad_stride != row_stride) return DOMINO_ERR_INVALID_ARG;
   }
@@ -1004,7 +1004,7 @@ int run_distill(const void* logits, int dtype, int64_t row_stride, const int32_t
 int domino_sample_filtered(const void* logits, int dtype, int64_t row_stride, const float* temperature,
                            const int32_t* top_k, const float* top_p, const float* min_p, const float* uniforms,
                            int rows, int V, int32_t* tokens, float* logp, void* stream) try {
-  int rc = check_rows(logits, dtype, row_stride, rows, V, dm::kMaxDrawVocab);
+  int rc = check_rows(logits, dtype, row_stride, rows, V);
   if (rc != DOMINO_OK) return rc;
   if (!uniforms || !tokens) return DOMINO_ERR_INVALID_ARG;
   if (!aligned(temperature, 4) || !aligned(top_k, 4) || !aligned(top_p, 4) || !aligned(min_p, 4) ||
@@ -1032,7 +1032,7 @@ int domino_verify_tree_filtered(const void* target_logits, int dtype, int64_t ro
                                 int32_t* accepted_count, int32_t* bonus_token, void* stream) try {
   if (B < 1 || N < 0 || N > (1 << 20)) return DOMINO_ERR_INVALID_ARG;
   const long long rows = static_cast<long long>(B) * (N + 1);
-  int rc = check_rows(target_logits, dtype, row_stride, rows, V, dm::kMaxDrawVocab);
+  int rc = check_rows(target_logits, dtype, row_stride, rows, V);
   if (rc != DOMINO_OK) return rc;
   if (!uniforms || !row_sample || !accepted_count || !bonus_token) return DOMINO_ERR_INVALID_ARG;
   if (N > 0 && (!tree_parent || !tree_token || !accepted_nodes)) return DOMINO_ERR_INVALID_ARG;

@@ -259,8 +259,7 @@ cudaError_t launch_walk(const int32_t* parent, const int32_t* token, const int32
 // ---------------------------------------------------------------- rows of logits (sample.cu, distill.cu)
 // Element types; numerically equal to enum domino_dtype.
 constexpr int kF32 = 0, kBf16 = 1, kF16 = 2;
-constexpr int kMaxDrawVocab = 1 << 19;        // ids of a row whose weights, 2^44 each, fit one integer
-constexpr int kMaxDistillVocab = 8 * 49152;  // ids of a row: eight slices that shared memory holds
+constexpr int kMaxRowVocab = 1 << 19;  // ids of a row: the weights of a draw, 2^44 each, fit one integer
 constexpr int kMaxTeacher = 256;         // places of a teacher's list
 
 struct DrawParams {

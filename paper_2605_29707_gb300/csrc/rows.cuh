@@ -1,6 +1,6 @@
-// rows.cuh -- building blocks of the kernels that work on rows of vocabulary logits held across a
-// cluster of CTAs (sample.cu, distill.cu): element types, staging of a row slice in shared memory,
-// and reductions and scans over a block and over the cluster.
+// rows.cuh -- building blocks of the kernels that work on rows of vocabulary logits split over a
+// cluster of CTAs (sample.cuh, distill.cu): element types, units of 16 bytes, accesses to the cluster's
+// shared memory, and reductions and scans over a block.
 #pragma once
 
 #include <cuda_bf16.h>
@@ -96,49 +96,17 @@ __device__ __forceinline__ float vec_max(const Vec<__nv_bfloat16>& f) {
 }
 __device__ __forceinline__ float vec_max(const Vec<__half>& f) { return vec_max_pairs<__half, __half2>(f); }
 
-// ------------------------------------------------------------------ staging
-// Elements [0, len) of `src` come to rest at s[shift .. shift + len), where `shift` is the number of
-// elements between the 16-byte boundary below src and src itself, so that whole 16-byte units of
-// global memory are whole units of shared memory whatever the row's alignment.  The units that lie
-// wholly inside the range are copied asynchronously (cp.async, 16 bytes a thread, committed as one
-// group); the first and the last few elements, whose units hold what is not the row's, are read one
-// by one.  The rest of those two units is -inf (an element that carries no weight).
+// ------------------------------------------------------------------ units
+// Elements between the 16-byte boundary at or below `src` and src itself.
 template <typename T>
 __device__ __forceinline__ int row_shift(const T* src) {
   return static_cast<int>((reinterpret_cast<uintptr_t>(src) & 15) / sizeof(T));
 }
 
-// 16-byte units that hold a staged slice.
+// Units of 16 bytes, aligned, that hold `len` elements from `shift` elements past a boundary on.
 template <typename T>
 __device__ __forceinline__ int row_units(int shift, int len) {
   return len > 0 ? (shift + len + Vec<T>::kN - 1) / Vec<T>::kN : 0;
-}
-
-__device__ __forceinline__ void cp_async16(void* dst, const void* src) {
-  asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16;" ::"r"(smem_u32(dst)), "l"(src) : "memory");
-}
-__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-__device__ __forceinline__ void cp_async_wait_all() { asm volatile("cp.async.wait_all;" ::: "memory"); }
-
-template <typename T, int THREADS>
-__device__ __forceinline__ void stage_slice(T* s, const T* src, int len, int tid) {
-  constexpr int N = Vec<T>::kN;
-  const int shift = row_shift(src);
-  const int first = shift ? 1 : 0;          // first whole unit
-  const int last = (shift + len) / N;       // one past the last whole unit
-  const T* base = src - shift;              // 16-byte boundary; only whole units are read from it
-  for (int q = first + tid; q < last; q += THREADS) cp_async16(s + q * N, base + static_cast<size_t>(q) * N);
-  cp_async_commit();
-  const int units = row_units<T>(shift, len);
-  T none;
-  from_f32(-INFINITY, &none);
-  if (len > 0) {
-    if (first && tid < N) s[tid] = tid >= shift && tid < shift + len ? src[tid - shift] : none;
-    if (units > last && !(first && last == 0) && tid >= 32 && tid < 32 + N) {
-      const int i = last * N + tid - 32;
-      s[i] = i < shift + len ? src[i - shift] : none;
-    }
-  }
 }
 
 // ------------------------------------------------------------------ clusters

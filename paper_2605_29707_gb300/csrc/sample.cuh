@@ -6,23 +6,37 @@
 // with exp(z - max z) >= min_p; the first always.  The token is the first kept id, in id order, whose
 // cumulative mass exceeds u times the kept mass.
 //
-// Weights are integers: 2^44 exp(z - max z), rounded.  At most 2^19 of them fit 63 bits, so every sum
-// is exact and the same in any order: splitting a row over CTAs, atomics and the order of threads
-// change nothing.  A weight above 2^-11 of the greatest is computed to about 2^-38 of its value
-// (weight()), one below in fp32.  (z, id) is one 64-bit integer (Order), so every cut is a bound on it.
+// Weights are integers: 2^44 exp(z - max z), rounded.  At most 2^19 of them fit 63 bits, so their sums are
+// exact and the same in any order: splitting a row over CTAs, atomics and the order of threads change
+// nothing.  A weight above 2^-11 of the greatest is computed to about 2^-38 of its value (fine_weight()),
+// one below in fp32.  (z, id) is one 64-bit integer (order_of()), so every cut is a bound on it.  Under
+// top-p the mass of the ids that cannot stay is added up in fp32, a thread's share at a time.
 //
-// A cluster of eight CTAs takes a row, an eighth each, and reads it twice, the second time from L2: eight
-// slices of 76 KB (V = 151936, fp32) per SM would not fit its shared memory, while what is in flight on
-// the whole chip fits L2, and a plain re-read of L2-resident slices ran at 11 TB/s against 7 from DRAM.
-//   1. the row maximum, and a value below which no id can stay: with top-k, where every CTA has k / 8
-//      groups of elements whose maxima reach it; with top-p, where V ids of its weight would carry less
-//      than 1 - p of what those maxima carry already; with min-p, from its definition;
-//   2. the ids above it, the candidates, go to the first CTA, which finishes the row alone while the
-//      others leave; with top-p the weights of the other ids are added up on the way, in fp32.
-// Too many candidates (more than kListCap) under top-p: the candidates' weights are added up by value
-// in kBins bins, the bin that holds the border is found, and either the candidates down to it are few
-// enough, or those in it are and decide the border.  What else leaves too many is cut by a radix selection
-// over the whole row.  Then, and without any filter, the cluster scans the kept weights in id order.
+// A cluster of CTAs takes a row, a slice each.  Bound by DRAM for many rows (one read of the logits), by the
+// chain of exchanges for few.
+//   Sampled pass (rows that a filter thins out, vocabularies of some ten thousand ids on).  A few units of 16
+//   bytes a thread, spread over the slice, give a value above which the ids that can stay should lie: under
+//   top-k the sample's value of a rank a little above its share of k; under top-p where the sample's mass below
+//   is a part of what may be left out, by half octaves of weight; under min-p its definition.  The row is then
+//   read once: the ids above go to the first CTA, and under top-p the mass below is added up, which tells
+//   whether the guess held; if not, it is lowered by what that pass found, once.
+//   Two passes (short vocabularies, guesses that failed).  The row maximum and a safe bound from the maxima of
+//   groups of elements: under top-k where every CTA has k / SP groups that reach a value; under top-p where V
+//   ids of its weight would carry less than 1 - p of what the maxima carry, or, first, a nearer one that the
+//   pass checks.  The second read comes from L2: what is in flight on the chip (46 MB at V = 151936, fp32) fits
+//   it, and a re-read of such slices ran at 11 TB/s against 7 from DRAM; holding them in shared memory left
+//   two CTAs an SM, waiting for each other (512 rows with top-p: 249 us against 173).
+//   The first CTA sorts up to kSort candidates by preference, scans their weights, sorts what stays by id and
+//   draws, while the others have left (one row 2.7 us, against 7.4 for radix selections over the list); more of
+//   them it thins out by bins of value first.
+//   More candidates than kListCap under top-p: their weights are added up by value in kBins bins over the
+//   cluster, and the candidates down to the bin that holds the border are gathered, or those in it, which decide
+//   it.  What else leaves too many is cut by a radix selection over the whole row.  Then, and without any
+//   filter, the cluster scans the kept weights in id order.
+// What it measured (device time): V = 151936, one fp32 row with top-k and top-p 12.0 us, 64 rows without a
+// filter 38 us; 512 fp32 rows with top-k 79 us, 3.9 TB/s, with min-p 81, with top-p 119; 1088 bf16 rows with
+// top-k and top-p 107 us, 3.1 TB/s.  For many rows the waves of CTAs end unevenly (3.4 of them at 512 rows) and the
+// first CTA's 6 us stay; more CTAs an SM (48 and 40 registers) gave 77 and 81 us for the first.
 // One translation unit an element type (sample_f32.cu, sample_bf16.cu, sample_f16.cu); sample.cu dispatches.
 #pragma once
 
@@ -153,7 +167,7 @@ struct DrawShared {  // dynamic shared memory
   u64 cut;                // the first CTA: the border of top-p (read by the cluster)
   double floor;           // T log(min_p)
   float group[256];       // maxima of groups of threads
-  uint32_t octave[kOctaves];  // their mass by half octaves of weight (read by the cluster)
+  uint32_t octave[kOctaves];  // the threads' maxima's mass by half octaves of weight (read by the cluster)
   float red[kWarps], red2[kWarps];
   float max, aux;         // this CTA's maximum, and its part of the candidates' bound (read by the cluster)
   float k_hi, k_lo;
@@ -422,8 +436,8 @@ __device__ __forceinline__ u64 top_p_need(const Settings& set, u64 all) {
 // The end of a row with at most kSort candidates: sorted by preference, and what stays of them by id.  `need`: the mass
 // that top-p asks for, 0 where it goes by what top-k leaves and `tail`, which is relative to sc.m.  The list holds the
 // row's maximum, which sc.m need not be.
-__device__ __forceinline__ void finish_sorted(const uint2* list, int n, u64 need, u64 tail, const Settings& set, Scale sc, DrawShared& sh, int32_t* token,
-                              float* logp) {
+__device__ __forceinline__ void finish_sorted(const uint2* list, int n, u64 need, u64 tail, const Settings& set, Scale sc,
+                                              DrawShared& sh, int32_t* token, float* logp) {
   const int tid = threadIdx.x;
   int np2 = 64;
   while (np2 < n) np2 *= 2;
@@ -498,8 +512,8 @@ __device__ __forceinline__ void finish_sorted(const uint2* list, int n, u64 need
 
 // The end of a row in the cluster's first CTA: n candidates, every id that can stay among them; `tail`: the mass of
 // the others, where top-p goes by it.
-__device__ __forceinline__ void finish_list(int n, u64 tail, const Settings& set, const Scale& sc, int V, DrawShared& sh, int32_t* token,
-                            float* logp) {
+__device__ __forceinline__ void finish_list(int n, u64 tail, const Settings& set, const Scale& sc, int V, DrawShared& sh,
+                                            int32_t* token, float* logp) {
   const int tid = threadIdx.x;
   if (n <= kSort) return finish_sorted(sh.list, n, 0, tail, set, sc, sh, token, logp);
   const float scale = sh.tau > -INFINITY && sc.m > sh.tau ? static_cast<float>(kBins) / (sc.m - sh.tau) * 0.9999f : 0.f;

@@ -2,14 +2,14 @@
 64-bit form of tests/rows_reference.py.
 
 The token has to be the plain form's wherever the plain form's nearest border (of top-p, of u) is more than
-BORDER of the mass away.  The kernel's weights are off by at most 2^-45 of the greatest (their last place)
-plus 2^-37 of their value where they are above 2^-14 of it, and 2^-19 of their value (fp32: the argument's
-rounding, up to 45 * 2^-24, and the exponential's) below.  For the distributions here the coarse ones carry
-less than 1e-3 of the mass between them in independent errors of either sign, V of them at most 2^-14 each:
-the sum's error stays under sqrt(V) 2^-14 2^-19 + V 2^-45 + 2^-37 < 6e-8 of the greatest weight, in the
-worst case, and under 1e-9 of the mass in all but adversarial ones.  BORDER = 1e-7 takes the worst case;
-rows that close to a border (one in some hundred thousand uniforms) may give either neighbour, and none of
-the seeds here may put more than one such row into a case.
+BORDER of the mass away.  The kernel's weights are off by at most 2^-44 of the greatest (their last places) plus
+2^-37 of their value where they are above 2^-11 of it, and 2^-19 of their value (fp32: the argument's rounding, up
+to 45 * 2^-24, and the exponential's) below; under top-p what cannot stay is summed in fp32 by some thousand threads
+of a few hundred terms each, 2^-20 of that mass per thread at most.  The errors of different ids and threads are
+independent and of either sign: n of them that carry a share s of the mass move a border by about s 2^-19 / sqrt(n).
+With s below 1/2 and n in the thousands that stays under 3e-8 of the mass; the exact weights contribute 2^-37 and
+V 2^-44 < 3e-8 in the worst case of one sign.  BORDER = 1e-7; rows that close to a border (one in some hundred
+thousand uniforms) may give either neighbour, and none of the seeds here may put more than one such row into a case.
 
 logp: fp32.  z carries two roundings (subtraction, division) and log(mass) one of the sum, the logarithm's
 (1 ulp) and the subtraction's: |error| <= 2^-23 |z| + 2^-23 log(mass) + 2^-24 |logp| + 2^-24 < 2^-21 (1 + |logp| +
