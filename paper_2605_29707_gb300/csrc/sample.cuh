@@ -743,8 +743,22 @@ __device__ u64 radix_cut(const Slice<T>& sl, u64 need, u64 old, const Scale& sc,
       for (int i = 0; i < Vec<T>::kN; ++i) {
         const float x = to_f32(f.e[i]);
         const uint32_t k = value_key(x);
-        if ((k & mask) == prefix && sl.holds(q, i) && order_of(k, sl.id(q, i)) >= old)
-          atomicAdd(&hist[(k >> bit) & 255], WEIGHTED ? weight(x, sc, sh.pow2) : 1ull);
+        const bool in = (k & mask) == prefix && sl.holds(q, i) && order_of(k, sl.id(q, i)) >= old;
+        const uint32_t digit = (k >> bit) & 255;
+        const u64 amount = !in ? 0ull : (WEIGHTED ? weight(x, sc, sh.pow2) : 1ull);
+        // where the warp's elements share a digit (rows of equal values do throughout), one addition for all of them
+        const unsigned who = __ballot_sync(0xffffffffu, in);
+        if (!who) continue;
+        const int one = __ffs(who) - 1;
+        const uint32_t shared = __shfl_sync(0xffffffffu, digit, one);
+        if (__all_sync(0xffffffffu, !in || digit == shared)) {
+          u64 sum = amount;
+#pragma unroll
+          for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+          if ((tid & 31) == one) atomicAdd(&hist[digit], sum);
+        } else if (in) {
+          atomicAdd(&hist[digit], amount);
+        }
       }
     });
     cluster_sync();  // every CTA's histogram is in place
