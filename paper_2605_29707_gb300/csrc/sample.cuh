@@ -52,7 +52,7 @@ constexpr int kWarps = kDrawThreads / 32;
 constexpr int kDrawBatch = 4;       // 16-byte loads a thread has in flight
 constexpr int kLocalCap = 2048;     // candidates a CTA holds, a segment of them a warp
 constexpr int kSeg = kLocalCap / kWarps;
-constexpr int kListCap = 3072;      // candidates the cluster's first CTA can take
+constexpr int kListCap = 3040;      // candidates the cluster's first CTA can take
 constexpr int kMaxSteps = 264;      // of 32 units that a warp has of a slice
 constexpr int kBins = 512;          // of values, or of ids
 constexpr int kSubCap = 256;        // entries of one bin that are ranked against each other

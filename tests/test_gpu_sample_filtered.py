@@ -166,6 +166,26 @@ def test_draw_sorted_rows(order, rule):
     run_and_check(x, F32, u, **RULES[rule])
 
 
+@pytest.mark.parametrize("rule", ["topk", "topp", "minp", "all"])
+@pytest.mark.parametrize("dtype,V", [(F32, 151936), (BF16, 151935)])
+def test_draw_rows_that_a_sample_misjudges(rule, dtype, V):
+    """Long rows whose sample says little: sorted ones (all candidates in a few warps' ids), one token far above the
+    rest, a few finite logits among -inf and NaN, a run of high logits, two levels only, a plateau under a peak."""
+    x = logits(6, V, dtype, 31, std=3.0)
+    x[0] = x[0].sort().values
+    x[1] = x[1].sort(descending=True).values
+    x[2, 77777] = 60.0
+    x[3] = -math.inf
+    x[3, [5, 77777, V - 1]] = torch.tensor([1.0, 2.0, 1.5], device=DEV).to(TYPES[dtype])
+    x[3, 100:200] = math.nan
+    x[4] = x[4].clamp(max=4.0)
+    x[4, 40000:46000] = 9.0  # more equal candidates than any list holds
+    x[5] = 0.0
+    x[5, ::3] = 1.0
+    u = uniforms(6, 31)
+    run_and_check(x, dtype, u, **RULES[rule])
+
+
 def test_draw_masked_and_infinite_logits():
     """-inf, NaN and the type's lowest value in masked places, rows without any logit, +inf."""
     V = 3001
