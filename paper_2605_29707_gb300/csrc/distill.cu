@@ -88,13 +88,13 @@ __device__ __forceinline__ Place teacher_place(const DistillParams& p, size_t ro
   } else {
     t *= p.inv_t;
     const float top = block_max<THREADS>(t, s_red, tid);
-    e.q = t > -INFINITY ? expf(t - top) : 0.f;
+    e.q = t > -INFINITY || isnan(t) ? expf(t - top) : 0.f;  // (a NaN score shows)
   }
   const float sum = block_sum<THREADS>(e.q, s_red, tid);
   if (p.tail) {
     *rest = fmaxf(0.f, 1.f - sum);
   } else {
-    e.q = sum > 0.f ? e.q / sum : 0.f;
+    e.q = sum == 0.f ? 0.f : e.q / sum;
     *rest = 0.f;
   }
   if (tid < p.kt) {
@@ -265,7 +265,7 @@ __global__ void __launch_bounds__(kDistillThreads, 5) distill_kernel(const Disti
     if (p.tail) rest = fmaxf(0.f, 1.f - sum);
 #pragma unroll
     for (int i = 0; i < kLanePlaces; ++i)
-      if (32 * i + lane < p.kt) s_q[32 * i + lane] = p.tail ? t[i] : (sum > 0.f ? t[i] / sum : 0.f);
+      if (32 * i + lane < p.kt) s_q[32 * i + lane] = p.tail ? t[i] : (sum == 0.f ? 0.f : t[i] / sum);  // (NaN shows)
   }
   __syncthreads();
 

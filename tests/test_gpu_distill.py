@@ -199,6 +199,20 @@ def test_distill_nan_shows():
 
 
 @pytest.mark.parametrize("mode", [RENORM, TAIL])
+def test_distill_nan_scores_show(mode):
+    """A NaN among the teacher's scores makes the row's loss NaN, and its gradient by every entry point."""
+    x = logits(3, 1000, F32, 28)
+    ids, scores = lists(x, 4, mode, 1.0, 28)
+    scores[0, 1] = math.nan
+    scores[1] = math.nan
+    loss, lse, dx = run("both", x, F32, ids, scores, 1.0, mode)
+    _, _, dx2 = run("grad", x, F32, ids, scores, 1.0, mode, lse=lse)
+    assert np.isnan(loss[:2]).all() and np.isfinite(loss[2])
+    for d in (dx, dx2):
+        assert torch.isnan(d[:2]).any(1).all() and torch.isfinite(d[2]).all()
+
+
+@pytest.mark.parametrize("mode", [RENORM, TAIL])
 def test_distill_gradient_is_the_loss_difference(mode):
     """Central differences of the loss that the GPU returns: step h = 2^-5, error of the quotient h^2 / 6 times the
     third derivative (at most 1 for a softmax at T >= 1, both terms: 2) plus two losses' rounding (E each) over 2 h."""
