@@ -276,10 +276,11 @@ enum domino_dtype { DOMINO_F32 = 0, DOMINO_BF16 = 1, DOMINO_F16 = 2 };
  *   top_k: the first k stay (k < 1 or k >= V: all);
  *   top_p: of those, the ones before which less than top_p of their mass lies (top_p >= 1 or NaN: all);
  *   min_p: of those, the ones whose probability is at least min_p times the greatest (min_p <= 0 or
- *          NaN: all);
+ *          NaN: all; above 1 counts as 1);
  *   the first id always stays.  The token is the first kept id, in id order, whose cumulative mass
  *   exceeds u times the kept mass (u outside [0, 1), or NaN, is clamped to it).
- * T <= 0 or NaN draws the first id (argmax, equal values: the lowest id).  Ids of logit -inf or NaN are
+ * T <= 0 or NaN draws the first id (argmax, equal values: the lowest id); T = inf makes all ids equally
+ * likely, in the order of their logits.  Ids of logit -inf or NaN are
  * never drawn; a row without any other gives id 0 and logp -inf; where logits are +inf, they share the
  * mass evenly.  The weights of the ids that can stay are integers of 2^-44 of the greatest, whose sums
  * are exact in any order; under top_p the mass of the others is added up in fp32.  Borders (of top_p, of

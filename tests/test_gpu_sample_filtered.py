@@ -232,6 +232,23 @@ def test_draw_extreme_settings():
     assert (one == top).all()
 
 
+@pytest.mark.parametrize("dtype,V", [(F32, 151935), (BF16, 151935), (F32, 901), (F16, 40003)])
+def test_draw_infinitely_hot_rows_with_masked_ids(dtype, V):
+    """T = inf makes the ids that are not masked equally likely; -inf, whose product with 1 / T has no value, stays out
+    of the draw and out of the mass that top-p goes by."""
+    x = logits(6, V, dtype, 32)
+    x[0, ::2] = -math.inf
+    x[1, V // 3:] = -math.inf
+    x[2, : V // 3] = -math.inf
+    x[3, 7] = -math.inf
+    x[4, ::3] = math.nan
+    u = uniforms(6, 32)
+    T = [math.inf] * 6
+    for a in (dict(), dict(p=[0.9, 0.3, 0.99, 0.5, 0.05, 0.7]), dict(k=[50] * 6, p=[0.71] * 6), dict(k=[50] * 6),
+              dict(m=[0.5] * 6), dict(p=[0.63] * 6, m=[0.5] * 6)):
+        run_and_check(x, dtype, u, T=T, **a)
+
+
 def test_draw_interval_ends():
     """u on the borders of four equal ids, at the ends of [0, 1), and outside."""
     x = torch.zeros((9, 4), device=DEV)
