@@ -336,7 +336,8 @@ DOMINO_API int domino_verify_tree_filtered(const void* target_logits, int dtype,
  *   logits: device [rows, row_stride] of `dtype`, element-aligned, finite or -inf; row_stride >= V;
  *     V <= 524288.  teacher_ids int32 [rows, kt], teacher_scores fp32 [rows, kt] (finite or -inf),
  *     1 <= kt <= 256.  weights fp32 [rows] or NULL (1); grad_loss fp32 [rows] or NULL (1): the upstream
- *     gradient of the row's loss.  temperature > 0 with 1 / T finite in fp32.
+ *     gradient of the row's loss.  temperature > 0 with log2(e) / T finite in fp32; a logit over T beyond
+ *     fp32 gives infinities or NaN.
  * Outputs (device): loss fp32 [rows]; lse fp32 [rows, 2]: the log-sum-exp of z over every id and over
  *   the ids not listed (-inf where there is none); dlogits [rows, grad_stride] of `dtype`,
  *   grad_stride >= V, every id written, one rounding of the fp32 gradient; it may be the logits' own memory

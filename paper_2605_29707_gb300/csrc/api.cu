@@ -974,7 +974,8 @@ int run_distill(const void* logits, int dtype, int64_t row_stride, const int32_t
       !aligned(loss, 4) || !aligned(lse, 4))
     return DOMINO_ERR_INVALID_ARG;
   const float inv_t = 1.0f / temperature;
-  if (!(temperature > 0.f) || !std::isfinite(temperature) || !std::isfinite(inv_t)) return DOMINO_ERR_INVALID_ARG;
+  const float k2 = static_cast<float>(1.4426950408889634 / static_cast<double>(temperature));
+  if (!(temperature > 0.f) || !std::isfinite(temperature) || !std::isfinite(k2)) return DOMINO_ERR_INVALID_ARG;
   if (mode != DOMINO_DISTILL_RENORM && mode != DOMINO_DISTILL_TAIL) return DOMINO_ERR_INVALID_ARG;
   if (kt > dm::kMaxTeacher) return DOMINO_ERR_UNSUPPORTED;
   if (dlogits) {
@@ -989,7 +990,7 @@ int run_distill(const void* logits, int dtype, int64_t row_stride, const int32_t
   d.V = V; d.kt = kt;
   d.ids = teacher_ids; d.scores = teacher_scores; d.weights = weights; d.grad_loss = grad_loss;
   d.inv_t = inv_t;
-  d.k2 = static_cast<float>(1.4426950408889634 / static_cast<double>(temperature));
+  d.k2 = k2;
   d.tail = mode == DOMINO_DISTILL_TAIL;
   d.loss = loss; d.lse = lse;
   d.dlogits = dlogits; d.grad_stride = grad_stride;

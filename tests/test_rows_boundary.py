@@ -79,3 +79,9 @@ def test_distill_output_refusals():
         assert _distill(part, dlogits=P + 2) == BAD
         assert _distill(part, dlogits=P, grad_stride=104) == BAD  # in place, with another stride
     assert _distill("grad", lse=None) == BAD
+
+
+@pytest.mark.parametrize("part", ["loss", "grad", "both"])
+def test_distill_refuses_temperatures_whose_base_2_scale_overflows(part):
+    """1 / 3.5e-39 is finite in fp32, log2(e) / 3.5e-39 is not."""
+    assert _distill(part, temperature=3.5e-39) == BAD
