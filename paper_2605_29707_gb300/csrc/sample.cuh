@@ -1227,7 +1227,7 @@ __global__ void __launch_bounds__(kDrawThreads, 4) filtered_draw_kernel(const Dr
     const float scale = tau > -INFINITY && sc.m > tau ? static_cast<float>(kBins) / (sc.m - tau) * 0.9999f : 0.f;
     bool fits = n <= kListCap;
     if (!fits && with_tail) {
-          const int n_own = sh.n_warp[warp];
+      const int n_own = sh.n_warp[warp];
       const bool listed = __syncthreads_and(n_own <= kSeg);  // the local list has them all
       // the candidates' weights by value (from the list, or from the slice where it has more than the list holds)
       for (int i = tid; i < kBins; i += kDrawThreads) sh.bins[i] = make_uint4(0, 0, 0, 0);
