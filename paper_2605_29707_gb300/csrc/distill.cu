@@ -226,6 +226,7 @@ __global__ void __launch_bounds__(kDistillThreads, 5) distill_kernel(const Disti
   const unsigned row = blockIdx.x / SP;
   const uint32_t part = SP > 1 ? cluster_ctarank() : 0;  // == blockIdx.x % SP
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (SP > 1) cluster_arrive();  // this CTA runs: the others may store into its shared memory
   const int lo = min(p.V, static_cast<int>(part) * p.slice);
   const int len = min(p.V, lo + p.slice) - lo;
   const T* x = static_cast<const T*>(p.logits) + row * static_cast<size_t>(p.stride);
@@ -297,6 +298,7 @@ __global__ void __launch_bounds__(kDistillThreads, 5) distill_kernel(const Disti
   mine = warp_join(mine, p.k2);
   if (lane == 0) s_warp[warp] = mine;
   __syncthreads();
+  if (SP > 1) cluster_wait();  // every CTA of the cluster runs (what was read since the arrival hides the wait)
   if (warp == 0) {
     MaxSum all = s_warp[0];
 #pragma unroll
