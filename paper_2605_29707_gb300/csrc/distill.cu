@@ -8,6 +8,12 @@
 //   loss     = w [ sum_j q_j (log q_j - z_j + log Z) + rest (log rest - log R + log Z) ]
 //   dx_v     = (g w / T) [ exp(z_v - log Z) - sum_{j: id_j = v} q_j ]                       v listed
 //            = (g w / T) exp(z_v - log R) [ R / Z - rest ]                                  v not listed
+// The loss's terms are of the size of log Z and cancel where the student agrees with the teacher, so it is formed as
+//   loss / w = sum_b q_b h(p_b / q_b - 1) + sum_b (q_b - p_b),   h(d) = d - log(1 + d) >= 0,
+// b over the distinct listed ids (q_b: the sum of their places' q_j) and, with a tail, the rest; places that share an id
+// add q_j log(q_j / q_b).  The second sum is 0 where a rest is left (everything on both sides), R / Z under renorm and
+// sum q - 1 + R / Z without a rest.  Relative error of the loss of 151936 ids, T = 4, eight places: 1e-6; of the terms
+// added as they stand 2e-3.
 // The sum over the ids not listed is taken directly, with its own maximum: 1 - sum p_j would lose it where
 // the student agrees with the teacher.  Terms with q = 0 or rest = 0 are 0; a row of weight 0 has loss and
 // gradient 0 whatever its logits hold.
@@ -86,9 +92,8 @@ __device__ __forceinline__ Place teacher_place(const DistillParams& p, size_t ro
   if (p.tail) {
     e.q = expf(t);
   } else {
-    t *= p.inv_t;
     const float top = block_max<THREADS>(t, s_red, tid);
-    e.q = t > -INFINITY || isnan(t) ? expf(t - top) : 0.f;  // (a NaN score shows)
+    e.q = t > -INFINITY || isnan(t) ? expf((t - top) * p.inv_t) : 0.f;  // (a NaN score shows)
   }
   const float sum = block_sum<THREADS>(e.q, s_red, tid);
   if (p.tail) {
@@ -147,6 +152,18 @@ __device__ __forceinline__ void unit_exp(const Vec<T>& f, float base, float k2, 
 #pragma unroll
     for (int i = 0; i < Vec<T>::kN; ++i) e[i] = ex2((x[i] - base) * k2);
   }
+}
+
+// q log(q / p) + p - q = q h(p / q - 1).  Near p = q by the series of log(1 + d) = 2 artanh(s), s = d / (2 + d): an error of
+// p then counts by p - q alone; up to a factor of two by log1p; further off by the logarithms, p's being `log_p`.
+__device__ __forceinline__ float excess(float q, float p, float log_p) {
+  if (q == 0.f) return p;
+  const float gap = p - q, d = gap / q;
+  if (fabsf(gap) <= 0.25f * q) {  // |s| <= 1 / 7: the series' next term is below 2^-28 of h
+    const float s = d / (2.f + d), s2 = s * s;
+    return q * (s * d - 2.f * s * s2 * fmaf(s2, fmaf(s2, fmaf(s2, 1.f / 9.f, 1.f / 7.f), 1.f / 5.f), 1.f / 3.f));
+  }
+  return gap - q * (p > 0.5f * q && p < 2.f * q ? log1pf(d) : log_p - logf(q));
 }
 
 constexpr int kLanePlaces = kMaxTeacher / 32;  // places of the list that a lane of the list's warp has
@@ -219,6 +236,7 @@ __global__ void __launch_bounds__(kDistillThreads, 5) distill_kernel(const Disti
   extern __shared__ __align__(16) unsigned char s_listed[];  // a byte a unit
   __shared__ int s_id[kMaxTeacher];
   __shared__ float s_q[kMaxTeacher], s_x[kMaxTeacher];  // later, in s_x, the listed ids' gradients
+  __shared__ float s_all[kMaxTeacher];                  // the sum of q over the places with the place's id
   __shared__ MaxSum s_warp[kDistillThreads / 32];
   __shared__ MaxSum s_part[SP];  // every CTA's ids that are not listed (written by the cluster)
   __shared__ float s_a, s_base;
@@ -238,10 +256,10 @@ __global__ void __launch_bounds__(kDistillThreads, 5) distill_kernel(const Disti
   const float w = p.weights ? __ldg(p.weights + row) : 1.f;
 
   // ---- the teacher's list, by warp 0: the student's logits, the teacher's probabilities, and what it leaves to the rest
-  float rest = 0.f;
+  float rest = 0.f, taught = 0.f;  // (warp 0's) the teacher's mass outside and inside the list
   const int places = (p.kt + 31) / 32;  // of a lane: 32 i + lane
   if (warp == 0) {
-    float t[kLanePlaces], top = -INFINITY, sum = 0.f;
+    float t[kLanePlaces], top = -INFINITY;
 #pragma unroll
     for (int i = 0; i < kLanePlaces; ++i) {
       const int j = 32 * i + lane;
@@ -253,20 +271,19 @@ __global__ void __launch_bounds__(kDistillThreads, 5) distill_kernel(const Disti
         s_id[j] = on ? id : -1;
         s_x[j] = on ? to_f32(x[id]) : -INFINITY;
       }
-      if (!p.tail) t[i] *= p.inv_t;
       top = fmaxf(top, t[i]);
     }
-    top = p.tail ? 0.f : warp_max(top);
+    top = warp_max(top);
 #pragma unroll
     for (int i = 0; i < kLanePlaces; ++i) {
-      t[i] = t[i] > -INFINITY || isnan(t[i]) ? expf(t[i] - top) : 0.f;
-      sum += t[i];
+      t[i] = t[i] > -INFINITY || isnan(t[i]) ? expf(p.tail ? t[i] : (t[i] - top) * p.inv_t) : 0.f;
+      taught += t[i];
     }
-    sum = warp_sum(sum);
-    if (p.tail) rest = fmaxf(0.f, 1.f - sum);
+    taught = warp_sum(taught);
+    if (p.tail) rest = fmaxf(0.f, 1.f - taught);
 #pragma unroll
     for (int i = 0; i < kLanePlaces; ++i)
-      if (32 * i + lane < p.kt) s_q[32 * i + lane] = p.tail ? t[i] : (sum == 0.f ? 0.f : t[i] / sum);  // (NaN shows)
+      if (32 * i + lane < p.kt) s_q[32 * i + lane] = p.tail ? t[i] : (taught == 0.f ? 0.f : t[i] / taught);  // (NaN shows)
   }
   __syncthreads();
 
@@ -317,15 +334,24 @@ __global__ void __launch_bounds__(kDistillThreads, 5) distill_kernel(const Disti
     MaxSum r = s_part[0];
 #pragma unroll
     for (int c = 1; c < SP; ++c) r = join(r, s_part[c], p.k2);
-    float top = r.m;
+    float top = r.m, loss = 0.f;
     int distinct = 0;
     unsigned firsts = 0;  // places whose id no earlier place has
     for (int i = 0; i < places; ++i) {
       const int j = 32 * i + lane;
       const int id = j < p.kt ? s_id[j] : -1;
       bool first = id >= 0;
-      if (first) top = fmaxf(top, s_x[j]);
-      for (int k = 0; first && k < j; ++k) first = s_id[k] != id;
+      if (first) {
+        top = fmaxf(top, s_x[j]);
+        float all = 0.f;
+        for (int k = 0; k < p.kt; ++k)
+          if (s_id[k] == id) {
+            all += s_q[k];
+            if (k < j) first = false;
+          }
+        s_all[j] = all;
+        if (s_q[j] > 0.f && s_q[j] != all) loss += s_q[j] * logf(s_q[j] / all);  // a shared id
+      }
       if (first) firsts |= 1u << i;
       distinct += __popc(__ballot_sync(0xffffffffu, first));
     }
@@ -341,6 +367,7 @@ __global__ void __launch_bounds__(kDistillThreads, 5) distill_kernel(const Disti
     const float r_top = r.s * ex2(m_top * p.k2);
     const float z = r_top + listed;
     const float inv_z = z == 0.f ? 0.f : 1.f / z;
+    const float log_z = logf(z), log_r = m_top * p.inv_t + logf(r.s);  // relative to ref
     float scale = 0.f;
     if (GRAD) {
       scale = w == 0.f ? 0.f : (p.grad_loss ? __ldg(p.grad_loss + row) : 1.f) * w * p.inv_t;
@@ -350,31 +377,29 @@ __global__ void __launch_bounds__(kDistillThreads, 5) distill_kernel(const Disti
         s_base = r.m > -INFINITY ? r.m : 0.f;
       }
     }
+    for (int i = 0; i < places; ++i) {  // each first place's part of the loss, and its gradient
+      const int j = 32 * i + lane;
+      if (!(firsts >> i & 1)) continue;
+      const float pj = ex2((s_x[j] - ref) * p.k2) * inv_z, q = s_all[j];
+      if (part == 0) loss += excess(q, pj, (s_x[j] - ref) * p.inv_t - log_z);
+      if (GRAD) s_x[j] = w == 0.f ? 0.f : scale * (pj - q);
+    }
     if (part == 0) {
-      const float log_z = logf(z), log_r = m_top * p.inv_t + logf(r.s);  // relative to ref
-      float l = 0.f;
-      for (int j = lane; j < p.kt; j += 32) {
-        const float q = s_q[j];
-        if (q > 0.f || isnan(q)) l += empty ? INFINITY : q * (logf(q) - ((s_x[j] - ref) * p.inv_t - log_z));
-      }
-      l = warp_sum(l);
+      loss = warp_sum(loss);
       if (lane == 0) {
-        if (rest > 0.f) l += empty ? INFINITY : rest * (logf(rest) - (log_r - log_z));
-        p.loss[row] = w == 0.f ? 0.f : w * l;
+        const float p_rest = r_top / z;
+        if (rest > 0.f) loss += excess(rest, p_rest, log_r - log_z);
+        else loss += p.tail ? taught - 1.f + p_rest : p_rest;
+        if (taught == 0.f && rest == 0.f) loss = 0.f;  // nothing is taught
+        else if (empty) loss = INFINITY;
+        p.loss[row] = w == 0.f ? 0.f : w * loss;
         if (p.lse) {
           p.lse[2 * static_cast<size_t>(row)] = empty ? -INFINITY : ref * p.inv_t + log_z;
           p.lse[2 * static_cast<size_t>(row) + 1] = ref * p.inv_t + log_r;
         }
       }
     }
-    if (GRAD) {  // each first place's gradient
-      for (int i = 0; i < places; ++i) {
-        const int j = 32 * i + lane;
-        if (!(firsts >> i & 1)) continue;
-        float q_all = 0.f;
-        for (int k = 0; k < p.kt; ++k) q_all += s_id[k] == s_id[j] ? s_q[k] : 0.f;
-        s_x[j] = w == 0.f ? 0.f : scale * (ex2((s_x[j] - ref) * p.k2) * inv_z - q_all);
-      }
+    if (GRAD) {
       __syncwarp();
       for (int i = 0; i < places; ++i)
         if (!(firsts >> i & 1) && 32 * i + lane < p.kt) s_id[32 * i + lane] = -1;
