@@ -12,7 +12,8 @@
 //   loss / w = sum_b q_b h(p_b / q_b - 1) + sum_b (q_b - p_b),   h(d) = d - log(1 + d) >= 0,
 // b over the distinct listed ids (q_b: the sum of their places' q_j) and, with a tail, the rest; places that share an id
 // add q_j log(q_j / q_b).  The second sum is 0 where a rest is left (everything on both sides), R / Z under renorm and
-// sum q - 1 + R / Z without a rest.  Relative error of the loss of 151936 ids, T = 4, eight places: 1e-6; of the terms
+// sum q - 1 + R / Z without a rest.  1 - sum q, which is small where the teacher is sure of an id, is -expm1(t) of the
+// list's greatest score less the q of the other places: good to its own size, not to that of 1.  Relative error of the loss of 151936 ids, T = 4, eight places: 1e-6; of the terms
 // added as they stand 2e-3.
 // The sum over the ids not listed is taken directly, with its own maximum: 1 - sum p_j would lose it where
 // the student agrees with the teacher.  Terms with q = 0 or rest = 0 are 0; a row of weight 0 has loss and
@@ -64,6 +65,10 @@ __device__ __forceinline__ float block_max(float v, float* s, int tid) {
   return all;
 }
 
+// What a list of log-probabilities leaves, 1 - sum q (negative where the q add up to more): `top` the greatest score,
+// `others` the sum of q over all places but one that has it.
+__device__ __forceinline__ float unlisted_mass(float top, float others) { return -expm1f(top) - others; }
+
 // One place of the teacher's list, thread j's.
 struct Place {
   int id;       // -1: empty, or past the list
@@ -89,16 +94,16 @@ __device__ __forceinline__ Place teacher_place(const DistillParams& p, size_t ro
       if (id >= lo && id < hi) e.x = to_f32(x[id]);
     }
   }
+  const float top = block_max<THREADS>(t, s_red, tid);
   if (p.tail) {
     e.q = expf(t);
+    const int count = __syncthreads_count(t == top);
+    float others = block_sum<THREADS>(t == top ? 0.f : e.q, s_red, tid);
+    others += static_cast<float>(count - 1) * expf(top);
+    *rest = fmaxf(0.f, unlisted_mass(top, others));
   } else {
-    const float top = block_max<THREADS>(t, s_red, tid);
     e.q = t > -INFINITY || isnan(t) ? expf((t - top) * p.inv_t) : 0.f;  // (a NaN score shows)
-  }
-  const float sum = block_sum<THREADS>(e.q, s_red, tid);
-  if (p.tail) {
-    *rest = fmaxf(0.f, 1.f - sum);
-  } else {
+    const float sum = block_sum<THREADS>(e.q, s_red, tid);
     e.q = sum == 0.f ? 0.f : e.q / sum;
     *rest = 0.f;
   }
@@ -256,7 +261,7 @@ __global__ void __launch_bounds__(kDistillThreads, 5) distill_kernel(const Disti
   const float w = p.weights ? __ldg(p.weights + row) : 1.f;
 
   // ---- the teacher's list, by warp 0: the student's logits, the teacher's probabilities, and what it leaves to the rest
-  float rest = 0.f, taught = 0.f;  // (warp 0's) the teacher's mass outside and inside the list
+  float rest = 0.f, taught = 0.f, left = 0.f;  // (warp 0's) the teacher's mass outside and inside the list, 1 - inside
   const int places = (p.kt + 31) / 32;  // of a lane: 32 i + lane
   if (warp == 0) {
     float t[kLanePlaces], top = -INFINITY;
@@ -280,7 +285,18 @@ __global__ void __launch_bounds__(kDistillThreads, 5) distill_kernel(const Disti
       taught += t[i];
     }
     taught = warp_sum(taught);
-    if (p.tail) rest = fmaxf(0.f, 1.f - taught);
+    if (p.tail) {
+      const float q_top = expf(top);
+      float others = 0.f;
+      int count = 0;
+#pragma unroll
+      for (int i = 0; i < kLanePlaces; ++i) {
+        others += t[i] == q_top ? 0.f : t[i];
+        count += __popc(__ballot_sync(0xffffffffu, t[i] == q_top));
+      }
+      left = unlisted_mass(top, warp_sum(others) + static_cast<float>(count - 1) * q_top);
+      rest = fmaxf(0.f, left);
+    }
 #pragma unroll
     for (int i = 0; i < kLanePlaces; ++i)
       if (32 * i + lane < p.kt) s_q[32 * i + lane] = p.tail ? t[i] : (taught == 0.f ? 0.f : t[i] / taught);  // (NaN shows)
@@ -389,7 +405,7 @@ __global__ void __launch_bounds__(kDistillThreads, 5) distill_kernel(const Disti
       if (lane == 0) {
         const float p_rest = r_top / z;
         if (rest > 0.f) loss += excess(rest, p_rest, log_r - log_z);
-        else loss += p.tail ? taught - 1.f + p_rest : p_rest;
+        else loss += p.tail ? p_rest - left : p_rest;
         if (taught == 0.f && rest == 0.f) loss = 0.f;  // nothing is taught
         else if (empty) loss = INFINITY;
         p.loss[row] = w == 0.f ? 0.f : w * loss;
