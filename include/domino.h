@@ -327,9 +327,11 @@ DOMINO_API int domino_verify_tree_filtered(const void* target_logits, int dtype,
  *   DOMINO_DISTILL_TAIL: scores are the teacher's log-probabilities at temperature T; q_j = exp(score_j),
  *     and rest = max(0, 1 - sum_j q_j) belongs to all other ids together (0 where there is none):
  *     loss = weight * (sum_j q_j (log q_j - log p[id_j]) + rest (log rest - log sum_{v not listed} p[v])).
- *   gradient: d loss / d logits[v] * grad_loss = grad_loss weight / T * (p[v] - sum_{j: id_j = v} q_j)
- *     for a listed v (and for every v without a tail), grad_loss weight / T * p[v] (1 - rest /
- *     sum_{v' not listed} p[v']) for the others with one.  The loss is not scaled by T^2.
+ *   gradient: d loss / d logits[v] * grad_loss = grad_loss weight / T * (Q p[v] - sum_{j: id_j = v} q_j)
+ *     for a listed v (and for every v without a tail), grad_loss weight / T * p[v] (Q - rest /
+ *     sum_{v' not listed} p[v']) for the others with one, Q = sum_j q_j + rest.  Q is 1, but 0 for a
+ *     list that teaches nothing under DOMINO_DISTILL_RENORM (loss and gradient 0), and sum_j q_j under
+ *     DOMINO_DISTILL_TAIL where that is above 1 or every id is listed.  The loss is not scaled by T^2.
  * Places of the list whose id lies outside [0, V) are empty; an id may stand in several places.  A row
  * of weight 0 has loss and gradient 0, whatever its logits hold; a row whose logits are all -inf has
  * loss +inf (0 where it is weighted 0, or teaches nothing).  Sums in fp32, in a fixed order.

@@ -4,10 +4,11 @@
 // Mathematics.  Row x[V], temperature T, z = x / T, list (id_j, t_j), j < kt (a negative id is an empty
 // place), weight w, upstream gradient g.  p = softmax(z); q_j = softmax(t / T) over the list, and nothing
 // for the other ids ("renorm"), or q_j = exp(t_j) and rest = max(0, 1 - sum q) for all other ids together
-// ("tail").  With log Z the log-sum-exp of z over every id, log R over the ids not listed:
+// ("tail").  With log Z the log-sum-exp of z over every id, log R over the ids not listed, Q = sum q + rest (1, but where
+// the list teaches nothing, its probabilities add up to more, or every id is listed and they add up to less):
 //   loss     = w [ sum_j q_j (log q_j - z_j + log Z) + rest (log rest - log R + log Z) ]
-//   dx_v     = (g w / T) [ exp(z_v - log Z) - sum_{j: id_j = v} q_j ]                       v listed
-//            = (g w / T) exp(z_v - log R) [ R / Z - rest ]                                  v not listed
+//   dx_v     = (g w / T) [ Q exp(z_v - log Z) - sum_{j: id_j = v} q_j ]                     v listed
+//            = (g w / T) exp(z_v - log R) [ Q R / Z - rest ]                                v not listed
 // The loss's terms are of the size of log Z and cancel where the student agrees with the teacher, so it is formed as
 //   loss / w = sum_b q_b h(p_b / q_b - 1) + sum_b (q_b - p_b),   h(d) = d - log(1 + d) >= 0,
 // b over the distinct listed ids (q_b: the sum of their places' q_j) and, with a tail, the rest; places that share an id
@@ -65,6 +66,12 @@ __device__ __forceinline__ float block_max(float v, float* s, int tid) {
   return all;
 }
 
+// Q, from the sum of the list's weights (as exponentials: their quotients by it are q under renorm).  A NaN shows.
+__device__ __forceinline__ float teacher_mass(int tail, float sum, float rest) {
+  if (tail) return rest > 0.f ? 1.f : sum;
+  return sum == 0.f ? 0.f : sum / sum;
+}
+
 // What a list of log-probabilities leaves, 1 - sum q (negative where the q add up to more): `top` the greatest score,
 // `others` the sum of q over all places but one that has it.
 __device__ __forceinline__ float unlisted_mass(float top, float others) { return -expm1f(top) - others; }
@@ -79,10 +86,10 @@ struct Place {
 };
 
 // Reads the row's list (thread j < kt: place j; the logits of ids in [lo, hi) alone) and gives the
-// teacher's mass outside it.  s_id, s_q: [kt].
+// teacher's mass outside it, and all of it.  s_id, s_q: [kt].
 template <typename T, int THREADS>
 __device__ __forceinline__ Place teacher_place(const DistillParams& p, size_t row, const T* x, int lo, int hi, int* s_id,
-                                               float* s_q, float* s_red, float* rest) {
+                                               float* s_q, float* s_red, float* rest, float* mass) {
   const int tid = threadIdx.x;
   Place e{-1, -INFINITY, 0.f, false, 0.f};
   float t = -INFINITY;
@@ -95,15 +102,17 @@ __device__ __forceinline__ Place teacher_place(const DistillParams& p, size_t ro
     }
   }
   const float top = block_max<THREADS>(t, s_red, tid);
+  float sum;
   if (p.tail) {
     e.q = expf(t);
     const int count = __syncthreads_count(t == top);
     float others = block_sum<THREADS>(t == top ? 0.f : e.q, s_red, tid);
     others += static_cast<float>(count - 1) * expf(top);
+    sum = others + expf(top);
     *rest = fmaxf(0.f, unlisted_mass(top, others));
   } else {
     e.q = t > -INFINITY || isnan(t) ? expf((t - top) * p.inv_t) : 0.f;  // (a NaN score shows)
-    const float sum = block_sum<THREADS>(e.q, s_red, tid);
+    sum = block_sum<THREADS>(e.q, s_red, tid);
     e.q = sum == 0.f ? 0.f : e.q / sum;
     *rest = 0.f;
   }
@@ -121,6 +130,7 @@ __device__ __forceinline__ Place teacher_place(const DistillParams& p, size_t ro
     }
   }
   if (p.tail && p.kt >= p.V && __syncthreads_count(e.first) == p.V) *rest = 0.f;  // every id is listed
+  *mass = teacher_mass(p.tail, sum, *rest);
   return e;
 }
 
@@ -385,11 +395,12 @@ __global__ void __launch_bounds__(kDistillThreads, 5) distill_kernel(const Disti
     const float inv_z = z == 0.f ? 0.f : 1.f / z;
     const float log_z = logf(z), log_r = m_top * p.inv_t + logf(r.s);  // relative to ref
     float scale = 0.f;
+    const float mass = teacher_mass(p.tail, taught, rest);
     if (GRAD) {
       scale = w == 0.f ? 0.f : (p.grad_loss ? __ldg(p.grad_loss + row) : 1.f) * w * p.inv_t;
       if (lane == 0) {
-        // exp(z_v - log R) (R / Z - rest), with 2^((x - base) k2) = exp(z_v - log R) R
-        s_a = r.s == 0.f ? 0.f : scale * (r_top * inv_z - rest) / r.s;
+        // exp(z_v - log R) (Q R / Z - rest), with 2^((x - base) k2) = exp(z_v - log R) R
+        s_a = r.s == 0.f ? 0.f : scale * (mass * r_top * inv_z - rest) / r.s;
         s_base = r.m > -INFINITY ? r.m : 0.f;
       }
     }
@@ -398,7 +409,7 @@ __global__ void __launch_bounds__(kDistillThreads, 5) distill_kernel(const Disti
       if (!(firsts >> i & 1)) continue;
       const float pj = ex2((s_x[j] - ref) * p.k2) * inv_z, q = s_all[j];
       if (part == 0) loss += excess(q, pj, (s_x[j] - ref) * p.inv_t - log_z);
-      if (GRAD) s_x[j] = w == 0.f ? 0.f : scale * (pj - q);
+      if (GRAD) s_x[j] = w == 0.f ? 0.f : scale * (mass * pj - q);
     }
     if (part == 0) {
       loss = warp_sum(loss);
@@ -483,13 +494,13 @@ __global__ void __launch_bounds__(kGradThreads) distill_grad_kernel(const Distil
     for (int i = tid; i < len; i += kGradThreads) dx[i] = none;
     return;
   }
-  float rest;
-  const Place e = teacher_place<T, kGradThreads>(p, row, x, lo, lo + len, s_id, s_q, s_red, &rest);
+  float rest, mass;
+  const Place e = teacher_place<T, kGradThreads>(p, row, x, lo, lo + len, s_id, s_q, s_red, &rest, &mass);
   __syncthreads();  // the listed logits are read before any gradient is written (they may share memory)
   const float lse = p.lse[2 * row], lse_rest = p.lse[2 * row + 1];
   const float scale = (p.grad_loss ? __ldg(p.grad_loss + row) : 1.f) * w * p.inv_t;
   const bool some = lse_rest > -INFINITY || isnan(lse_rest);
-  const float a = some ? scale * (expf(lse_rest - lse) - rest) : 0.f;
+  const float a = some ? scale * (mass * expf(lse_rest - lse) - rest) : 0.f;
   const float base = some ? lse_rest : 0.f;
   auto grad = [&](T xv) {
     T g;
@@ -519,7 +530,7 @@ __global__ void __launch_bounds__(kGradThreads) distill_grad_kernel(const Distil
   if (e.first && e.id >= lo && e.id < lo + len) {
     const float pv = lse > -INFINITY || isnan(lse) ? expf(fmaf(e.x, p.inv_t, -lse)) : 0.f;
     T g;
-    from_f32(scale * (pv - e.q_all), &g);
+    from_f32(scale * (mass * pv - e.q_all), &g);
     dx[e.id - lo] = g;
   }
 }

@@ -96,7 +96,8 @@ def distill(x, ids, scores, T=1.0, tail=False, weight=1.0, up=1.0):
                 loss += rest * (np.log(rest) - (z_rest - z_all))
         p = np.exp(z - z_all)
         p_in_rest = np.exp(z - z_rest) if z_rest > -np.inf else np.zeros(V)
-    g = p - q_of - np.where(listed, 0.0, rest * p_in_rest)
+    with np.errstate(invalid="ignore"):  # (listed ids: not the rest's, whatever their share of it would be)
+        g = (q.sum() + rest) * p - q_of - np.where(listed, 0.0, rest * p_in_rest)
     if weight == 0:
         return 0.0, z_all, z_rest, np.zeros(V)
     return weight * loss, z_all, z_rest, g * (weight * up / T)
