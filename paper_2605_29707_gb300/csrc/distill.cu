@@ -152,21 +152,29 @@ __device__ __forceinline__ MaxSum warp_join(MaxSum v, float k2) {
   return v;
 }
 
-// 2^((x - base) k2) of a unit's elements.  fp32 logits: the difference first, which keeps the argument to 2.5 roundings
-// of itself.  16-bit logits: one multiply-add with -base k2, one instruction less of ten; the argument is then off by up
-// to a rounding of |base k2|, 2^-24 of some tens, which is far below what 8 or 11 bits of logit leave.
+// 2^((x - base) k2) of a unit's elements, but for a factor that all of them share, exp_factor(base, k2).  fp32 logits: the
+// difference first, which keeps the argument to 2.5 roundings of itself; the factor is 1.  16-bit logits: one multiply-add
+// with -base k2 rounded, one instruction less of ten.  What that rounding adds to every argument is known exactly, and the
+// factor takes it out where the terms have been added up.  Beyond kFusedMost (a row of masked places alone: -1e10 times k2 is
+// rounded by hundreds) the difference first, as for fp32; the rounding is 2^-9 at most below it.
+constexpr float kFusedMost = 65536.f;
 template <typename T>
 __device__ __forceinline__ void unit_exp(const Vec<T>& f, float base, float k2, float (&e)[Vec<T>::kN]) {
   float x[Vec<T>::kN];
   unpack(f, x);
   const float c = -base * k2;
-  if (sizeof(T) == 2 && fabsf(c) < 1e30f) {
+  if (sizeof(T) == 2 && fabsf(c) < kFusedMost) {
 #pragma unroll
     for (int i = 0; i < Vec<T>::kN; ++i) e[i] = ex2(fmaf(x[i], k2, c));
-  } else {  // (also where all the thread has is a mask's lowest value, whose product would overflow)
+  } else {
 #pragma unroll
     for (int i = 0; i < Vec<T>::kN; ++i) e[i] = ex2((x[i] - base) * k2);
   }
+}
+template <typename T>
+__device__ __forceinline__ float exp_factor(float base, float k2) {
+  const float c = -base * k2;
+  return sizeof(T) == 2 && fabsf(c) < kFusedMost ? ex2(-fmaf(base, k2, c)) : 1.f;
 }
 
 // q log(q / p) + p - q = q h(p / q - 1).  Near p = q by the series of log(1 + d) = 2 artanh(s), s = d / (2 + d): an error of
@@ -324,18 +332,20 @@ __global__ void __launch_bounds__(kDistillThreads, 5) distill_kernel(const Disti
   }
   __syncthreads();
   MaxSum mine{-INFINITY, 0.f};
+  float factor = 1.f;  // mine.m's
   auto take = [&](const Vec<T>& f, int) {
     const float top = vec_max(f);
     if (top > mine.m) {
       mine.s *= mine.m > -INFINITY ? ex2((mine.m - top) * p.k2) : 1.f;  // (nothing but a NaN sum yet)
       mine.m = top;
+      factor = exp_factor<T>(top, p.k2);
     }
     float e2[N];
     unit_exp(f, mine.m > -INFINITY ? mine.m : 0.f, p.k2, e2);
     float sum = 0.f;
 #pragma unroll
     for (int i = 0; i < N; ++i) sum += e2[i];
-    mine.s += sum;
+    mine.s = fmaf(sum, factor, mine.s);
   };
   slice.each(take, take);
   mine = warp_join(mine, p.k2);
@@ -434,7 +444,7 @@ __global__ void __launch_bounds__(kDistillThreads, 5) distill_kernel(const Disti
   }
   if (GRAD) {
     __syncthreads();
-    const float a = s_a, base = s_base;
+    const float base = s_base, a = s_a * exp_factor<T>(base, p.k2);
     T* dx = static_cast<T*>(p.dlogits) + row * static_cast<size_t>(p.grad_stride) + lo;
     const bool zero = w == 0.f;
     auto grads = [&](const Vec<T>& f) {
