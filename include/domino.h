@@ -345,8 +345,9 @@ DOMINO_API int domino_verify_tree_filtered(const void* target_logits, int dtype,
  *   grad_stride >= V, every id written, one rounding of the fp32 gradient; it may be the logits' own memory
  *   with the same stride.
  *   domino_distill_loss writes loss and lse (lse may be NULL); domino_distill_grad reads that lse and
- *   writes dlogits; domino_distill_loss_grad writes all three in one pass over the logits (lse may be
- *   NULL).
+ *   writes dlogits (the gradients carry lse's rounding, 2^-24 |lse| of their p; a row with an lse beyond
+ *   1024 in size, as where every id that is not listed is masked with a finite value, is summed anew);
+ *   domino_distill_loss_grad writes all three in one pass over the logits (lse may be NULL).
  * One kernel on `stream`, no workspace; the tensors and the stream belong to the current device.
  * Returns DOMINO_OK once enqueued, DOMINO_ERR_UNSUPPORTED for a larger V or kt or another dtype, or
  * another negative code (bad sizes, pointers, temperature or mode, logits of another device) with

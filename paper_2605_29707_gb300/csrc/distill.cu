@@ -25,7 +25,7 @@
 // the cluster join such pairs.  The teacher's list is one warp's work; the ids that it names are marked in shared
 // memory, a bit an element, and pass for -inf on the way through.  The gradient reads the slice again, from L2:
 // what is in flight on the chip (58 MB at most) fits it.  The gradient alone, from the two sums that the loss
-// left, is one pass without a cluster.
+// left, is one pass without a cluster, but for rows whose sums are too far from zero to tell their logits apart.
 // What it measured (device time): loss and gradient of 4096 bf16 rows, V = 151936, 517 us, 4.8 TB/s; with the slices
 // held in shared memory, 38 KB and five CTAs an SM, 568 us, for there they could not be longer.  Slices from 64 KB on;
 // from 32 KB 657 us, from 128 KB, which no longer fit L2, 636.  Gradient alone of 512 fp32 rows 98 us, 6.4 TB/s, 0.94 of
@@ -85,21 +85,18 @@ struct Place {
   float q_all;  // first: the sum of q over the places with this id
 };
 
-// Reads the row's list (thread j < kt: place j; the logits of ids in [lo, hi) alone) and gives the
-// teacher's mass outside it, and all of it.  s_id, s_q: [kt].
+// The row's list, place j (thread j < kt) with what it holds; gives the teacher's mass outside it, and all of it.  The
+// logits of ids in [lo, hi) alone are read.  s_id, s_q: [kt].
 template <typename T, int THREADS>
-__device__ __forceinline__ Place teacher_place(const DistillParams& p, size_t row, const T* x, int lo, int hi, int* s_id,
-                                               float* s_q, float* s_red, float* rest, float* mass) {
+__device__ __forceinline__ Place teacher_place(const DistillParams& p, int id, float score, const T* x, int lo, int hi,
+                                               int* s_id, float* s_q, float* s_red, float* rest, float* mass) {
   const int tid = threadIdx.x;
   Place e{-1, -INFINITY, 0.f, false, 0.f};
   float t = -INFINITY;
-  if (tid < p.kt) {
-    const int id = __ldg(p.ids + row * p.kt + tid);
-    if (id >= 0 && id < p.V) {
-      e.id = id;
-      t = __ldg(p.scores + row * p.kt + tid);
-      if (id >= lo && id < hi) e.x = to_f32(x[id]);
-    }
+  if (id >= 0 && id < p.V) {
+    e.id = id;
+    t = score;
+    if (id >= lo && id < hi) e.x = to_f32(x[id]);
   }
   const float top = block_max<THREADS>(t, s_red, tid);
   float sum;
@@ -484,9 +481,76 @@ __global__ void __launch_bounds__(kDistillThreads, 5) distill_kernel(const Disti
   }
 }
 
+// A stored log-sum-exp beyond this does not tell the row's logits apart any more: half its last place is more than 2^-14
+// (of -1e10, where every id that is not listed is masked so: hundreds).
+constexpr float kFarSum = 1024.f;
+__device__ __forceinline__ bool far_sum(float lse) { return fabsf(lse) > kFarSum && fabsf(lse) < INFINITY; }
+
+// Join over the block; `s` holds one pair a warp.
+__device__ __forceinline__ MaxSum block_join(MaxSum v, float k2, MaxSum* s, int tid) {
+  v = warp_join(v, k2);
+  __syncthreads();
+  if ((tid & 31) == 0) s[tid >> 5] = v;
+  __syncthreads();
+  MaxSum all = s[0];
+#pragma unroll
+  for (int w = 1; w < kGradThreads / 32; ++w) all = join(all, s[w], k2);
+  return all;
+}
+
+// The gradient of a whole row, by one CTA, with sums of its own, as distill_kernel takes them: they lie relative to the
+// logits that they are sums of.  Rows like that are few, so this reads element by element (one row of 151936 fp32 ids:
+// 250 us; 512 of them 630).  The logits and the gradient may share memory: everything is read before anything is written.
+template <typename T>
+__device__ __noinline__ void far_row(const DistillParams& p, size_t row, int id, float score, const T* x, T* dx, float w,
+                                     int* s_id, float* s_q, float* s_red) {
+  __shared__ uint32_t s_mark[kGradChunk / 32];  // the listed ids of a chunk, a bit each
+  __shared__ MaxSum s_pair[kGradThreads / 32];
+  const int tid = threadIdx.x;
+  float rest, mass;
+  const Place e = teacher_place<T, kGradThreads>(p, id, score, x, 0, p.V, s_id, s_q, s_red, &rest, &mass);
+  MaxSum mine{-INFINITY, 0.f};
+  for (int lo = 0; lo < p.V; lo += kGradChunk) {
+    __syncthreads();
+    for (int i = tid; i < kGradChunk / 32; i += kGradThreads) s_mark[i] = 0;
+    __syncthreads();
+    if (e.first && e.id >= lo && e.id - lo < kGradChunk) atomicOr(&s_mark[(e.id - lo) / 32], 1u << (e.id - lo) % 32);
+    __syncthreads();
+    const int end = min(p.V - lo, kGradChunk);
+    for (int i = tid; i < end; i += kGradThreads) {
+      const float v = to_f32(x[lo + i]);
+      if (s_mark[i / 32] >> i % 32 & 1 || v == -INFINITY) continue;
+      if (v > mine.m) {
+        mine.s *= mine.m > -INFINITY ? ex2((mine.m - v) * p.k2) : 1.f;  // (nothing but a NaN sum yet)
+        mine.m = v;
+      }
+      mine.s += ex2((v - mine.m) * p.k2);
+    }
+  }
+  const MaxSum r = block_join(mine, p.k2, s_pair, tid);
+  const MaxSum l = block_join(MaxSum{e.first ? e.x : -INFINITY, e.first && e.x != -INFINITY ? 1.f : 0.f}, p.k2, s_pair, tid);
+  const MaxSum all = join(r, l, p.k2);
+  const float scale = (p.grad_loss ? __ldg(p.grad_loss + row) : 1.f) * w * p.inv_t;
+  const float inv_z = all.s == 0.f ? 0.f : 1.f / all.s;
+  const float r_top = r.m > -INFINITY ? r.s * ex2((r.m - all.m) * p.k2) : r.s;
+  const float a = r.s == 0.f ? 0.f : scale * (mass * r_top * inv_z - rest) / r.s;
+  const float base = r.m > -INFINITY ? r.m : 0.f;
+  for (int i = tid; i < p.V; i += kGradThreads) {
+    T g;
+    from_f32(a * ex2((to_f32(x[i]) - base) * p.k2), &g);
+    dx[i] = g;
+  }
+  __syncthreads();  // the listed ids' places are written again
+  if (e.first) {
+    T g;
+    from_f32(scale * (mass * (e.x > -INFINITY || isnan(e.x) ? ex2((e.x - all.m) * p.k2) * inv_z : 0.f) - e.q_all), &g);
+    dx[e.id] = g;
+  }
+}
+
 // The gradient from the sums that the loss left: one CTA per chunk of a row.
 template <typename T>
-__global__ void __launch_bounds__(kGradThreads) distill_grad_kernel(const DistillParams p, int chunks) {
+__global__ void __launch_bounds__(kGradThreads) distill_grad_kernel(const __grid_constant__ DistillParams p, int chunks) {
   __shared__ int s_id[kMaxTeacher];
   __shared__ float s_q[kMaxTeacher];
   __shared__ float s_red[kGradThreads / 32];
@@ -498,16 +562,22 @@ __global__ void __launch_bounds__(kGradThreads) distill_grad_kernel(const Distil
   const T* x = static_cast<const T*>(p.logits) + row * static_cast<size_t>(p.stride);
   T* dx = static_cast<T*>(p.dlogits) + row * static_cast<size_t>(p.grad_stride) + lo;
   const float w = p.weights ? __ldg(p.weights + row) : 1.f;
+  const float lse = p.lse[2 * row], lse_rest = p.lse[2 * row + 1];
+  const int id = tid < p.kt ? __ldg(p.ids + row * p.kt + tid) : -1;  // (on the way before anything is asked of the others)
+  const float score = tid < p.kt ? __ldg(p.scores + row * p.kt + tid) : -INFINITY;
   if (w == 0.f) {
     T none;
     from_f32(0.f, &none);
     for (int i = tid; i < len; i += kGradThreads) dx[i] = none;
     return;
   }
+  if (far_sum(lse) || far_sum(lse_rest)) {
+    if (lo == 0) far_row(p, row, id, score, x, dx, w, s_id, s_q, s_red);
+    return;
+  }
   float rest, mass;
-  const Place e = teacher_place<T, kGradThreads>(p, row, x, lo, lo + len, s_id, s_q, s_red, &rest, &mass);
+  const Place e = teacher_place<T, kGradThreads>(p, id, score, x, lo, lo + len, s_id, s_q, s_red, &rest, &mass);
   __syncthreads();  // the listed logits are read before any gradient is written (they may share memory)
-  const float lse = p.lse[2 * row], lse_rest = p.lse[2 * row + 1];
   const float scale = (p.grad_loss ? __ldg(p.grad_loss + row) : 1.f) * w * p.inv_t;
   const bool some = lse_rest > -INFINITY || isnan(lse_rest);
   const float a = some ? scale * (mass * expf(lse_rest - lse) - rest) : 0.f;
