@@ -117,6 +117,14 @@ __device__ __forceinline__ u64 weight(float x, const Scale& sc, const u64* pow2)
   return fine_weight(x, sc.m, sc.k_hi, sc.k_lo, pow2);
 }
 
+// log(w / all) of the element x, whose weight w is.  More than half of the mass: by what the others have, so that a
+// log-probability near 0 is good to its own size; less: by the logit, of which more digits are there than of a small weight.
+static __device__ __noinline__ float log_prob(float x, u64 w, u64 all, const Scale& sc, float temp) {
+  const u64 others = all - w;
+  if (w > others) return -log1pf(static_cast<float>(others) / static_cast<float>(w));
+  return (sc.inf ? 0.f : (x - sc.m) / temp) - logf(static_cast<float>(all) * 0x1p-44f);
+}
+
 // The order of preference as integers: greater value, greater key (-0 as +0, NaN last); equal values: the lower id.
 __device__ __forceinline__ uint32_t value_key(float x) { return x != x ? 0u : f32_ord(x + 0.f); }
 __device__ __forceinline__ float key_value(uint32_t k) {
@@ -501,10 +509,7 @@ __device__ __forceinline__ void finish_sorted(const uint2* list, int n, u64 need
     if (at <= goal && goal < at + w[i]) {
       const uint32_t y = ~static_cast<uint32_t>(o[i] >> 32);
       *token = static_cast<int32_t>(y);
-      if (logp) {
-        const float x = sh.value[static_cast<uint32_t>(o[i])];
-        *logp = (sc.inf ? 0.f : (x - sc.m) / set.temp) - logf(static_cast<float>(all) * 0x1p-44f);
-      }
+      if (logp) *logp = log_prob(sh.value[static_cast<uint32_t>(o[i])], w[i], all, sc, set.temp);
     }
     at += w[i];
   }
@@ -595,8 +600,10 @@ __device__ __forceinline__ void finish_list(int n, u64 tail, const Settings& set
   for (int e = tid; e < n; e += kDrawThreads)
     if (sh.list[e].y == y) {
       *token = static_cast<int32_t>(y);
-      if (logp)
-        *logp = (sc.inf ? 0.f : (__uint_as_float(sh.list[e].x) - sc.m) / set.temp) - logf(static_cast<float>(all) * 0x1p-44f);
+      if (logp) {
+        const float x = __uint_as_float(sh.list[e].x);
+        *logp = log_prob(x, weight(x, sc, sh.pow2), all, sc, set.temp);
+      }
     }
 }
 
@@ -1388,7 +1395,7 @@ __global__ void __launch_bounds__(kDrawThreads, 4) filtered_draw_kernel(const Dr
   if (before <= goal && goal < before + own)
     slice_locate(sl, goal - before, sh, kept_weight, [&](float x, uint32_t id) {
       p.tokens[row] = static_cast<int32_t>(id);
-      if (logp) *logp = (sc.inf ? 0.f : (x - sc.m) / set.temp) - logf(static_cast<float>(all) * 0x1p-44f);
+      if (logp) *logp = log_prob(x, weight(x, sc, sh.pow2), all, sc, set.temp);
     });
   cluster_wait();
 }
