@@ -53,7 +53,8 @@ constexpr int kDrawBatch = 4;       // 16-byte loads a thread has in flight
 constexpr int kLocalCap = 2048;     // candidates a CTA holds, a segment of them a warp
 constexpr int kSeg = kLocalCap / kWarps;
 constexpr int kListCap = 3040;      // candidates the cluster's first CTA can take
-constexpr int kMaxSteps = 264;      // of 32 units that a warp has of a slice
+constexpr int kMaxSliceBytes = 256 << 10;  // the launch's rule: 524288 fp32 ids over eight CTAs, and no more by any halving
+constexpr int kMaxSteps = ((kMaxSliceBytes / 16 + 1 + kWarps - 1) / kWarps + 31) / 32;  // of 32 units, a warp's of a slice
 constexpr int kBins = 512;          // of values, or of ids
 constexpr int kSubCap = 256;        // entries of one bin that are ranked against each other
 constexpr int kSort = 512;          // entries that are sorted, two a thread
