@@ -282,8 +282,9 @@ enum domino_dtype { DOMINO_F32 = 0, DOMINO_BF16 = 1, DOMINO_F16 = 2 };
  * T <= 0 or NaN draws the first id (argmax, equal values: the lowest id); T = inf makes all ids equally
  * likely, in the order of their logits.  Ids of logit -inf or NaN are
  * never drawn; a row without any other gives id 0 and logp -inf; where logits are +inf, they share the
- * mass evenly.  The weights of the ids that can stay are integers of 2^-44 of the greatest, whose sums
- * are exact in any order; under top_p the mass of the others is added up in fp32.  Borders (of top_p, of
+ * mass evenly.  The weights of the ids that can stay are integers of 2^-44 of the greatest (good to 2^-38
+ * of their value, below 2^-11 of the greatest to fp32's), whose sums are exact in any order; under top_p
+ * the mass of the others is added up in fp32.  Borders (of top_p, of
  * u) lie within about 1e-7 of the mass of where exact arithmetic puts them, and the same call gives the
  * same draw.
  *   logits: device [rows, row_stride] of `dtype`, element-aligned; ids 0 .. V - 1 of a row are read,
@@ -291,7 +292,7 @@ enum domino_dtype { DOMINO_F32 = 0, DOMINO_BF16 = 1, DOMINO_F16 = 2 };
  *   temperature, top_p, min_p (fp32) and top_k (int32): device [rows], or NULL (T = 1, filter off).
  *   uniforms: device fp32 [rows].
  * Outputs (device): tokens int32 [rows]; logp fp32 [rows] or NULL: the token's log-probability among
- *   the kept ids.
+ *   the kept ids (near 0 good to its own size).
  * One kernel on `stream`, no workspace; the tensors and the stream belong to the current device.
  * Returns DOMINO_OK once enqueued, DOMINO_ERR_UNSUPPORTED for a larger V or another dtype, or another
  * negative code (bad sizes or pointers, logits of another device) with nothing enqueued. */

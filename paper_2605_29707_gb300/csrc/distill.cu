@@ -11,25 +11,32 @@
 //            = (g w / T) exp(z_v - log R) [ Q R / Z - rest ]                                v not listed
 // The loss's terms are of the size of log Z and cancel where the student agrees with the teacher, so it is formed as
 //   loss / w = sum_b q_b h(p_b / q_b - 1) + sum_b (q_b - p_b),   h(d) = d - log(1 + d) >= 0,
-// b over the distinct listed ids (q_b: the sum of their places' q_j) and, with a tail, the rest; places that share an id
-// add q_j log(q_j / q_b).  The second sum is 0 where a rest is left (everything on both sides), R / Z under renorm and
-// sum q - 1 + R / Z without a rest.  1 - sum q, which is small where the teacher is sure of an id, is -expm1(t) of the
-// list's greatest score less the q of the other places: good to its own size, not to that of 1.  Relative error of the loss of 151936 ids, T = 4, eight places: 1e-6; of the terms
-// added as they stand 2e-3.
+// b over the distinct listed ids (q_b: the sum of their places' q_j) and, with a tail, the rest; places that share an
+// id add q_j log(q_j / q_b).  The second sum is 0 where a rest is left (everything on both sides), R / Z under renorm
+// and sum q - 1 + R / Z without a rest.  1 - sum q, which is small where the teacher is sure of an id, is -expm1(t)
+// of the list's greatest score less the q of the other places: good to its own size, not to that of 1.  Relative
+// error of the loss of 151936 ids, T = 4, eight places: 1e-6; of the terms added as they stand 2e-3.
 // The sum over the ids not listed is taken directly, with its own maximum: 1 - sum p_j would lose it where
 // the student agrees with the teacher.  Terms with q = 0 or rest = 0 are 0; a row of weight 0 has loss and
 // gradient 0 whatever its logits hold.
 //
-// Bound by DRAM.  For the loss, and for loss and gradient together, a cluster of CTAs takes a row, a slice each.
+// The gradient alone is bound by DRAM; with the loss, many rows are bound by DRAM at six tenths of its rate and by the barriers
+// around the list and the exchange, few rows by the chain of one.
+// For the loss, and for loss and gradient together, a cluster of CTAs takes a row, a slice each.
 // A thread keeps the maximum of what it reads and the sum relative to it; warps, the CTA and, with one exchange,
 // the cluster join such pairs.  The teacher's list is one warp's work; the ids that it names are marked in shared
 // memory, a bit an element, and pass for -inf on the way through.  The gradient reads the slice again, from L2:
-// what is in flight on the chip (58 MB at most) fits it.  The gradient alone, from the two sums that the loss
+// what is in flight on the chip (58 MB at V = 151936, bf16) fits it.  The gradient alone, from the two sums that the loss
 // left, is one pass without a cluster, but for rows whose sums are too far from zero to tell their logits apart.
-// What it measured (device time): loss and gradient of 4096 bf16 rows, V = 151936, 517 us, 4.8 TB/s; with the slices
-// held in shared memory, 38 KB and five CTAs an SM, 568 us, for there they could not be longer.  Slices from 64 KB on;
-// from 32 KB 657 us, from 128 KB, which no longer fit L2, 636.  Gradient alone of 512 fp32 rows 98 us, 6.4 TB/s, 0.94 of
-// the measured copy rate; loss of 1023 fp16 rows, V = 41511, 30.5 us; loss of 16 bf16 rows 7.4 us.
+// What it measured (device time): loss and gradient of 4096 bf16 rows, V = 151936, 530 us, 4.7 TB/s (522 with the
+// rest as 1 - sum q); with the slices held in shared memory, 38 KB and five CTAs an SM, 568 us, for there they could
+// not be longer.  Slices from 64 KB on; from 32 KB 657 us, from 128 KB, which no longer fit L2, 636.  Vocabularies
+// just below a power of two have the longest, up to 128 KB, 100 MB in flight: as many bytes at V = 65535, 131071 or
+// 262143 take 615 us (540 at 140000).  Gradient alone of 512 fp32 rows 96.7 us, 6.4 TB/s, 0.95 of the measured copy
+// rate, of 512 bf16 rows 61; loss of 1023 fp16 rows, V = 41511, 30.7 us; loss of 16 bf16 rows 8.1 us.  Gradient rows
+// of another 16-byte alignment than the logits' are written element by element: 165 us for the 512 fp32 rows, and 390
+// instead of 145 for loss and gradient of 1024 bf16 rows.  A list of 64 places costs 10 us in 90 (512 bf16 rows), of
+// 256, where every place looks at every other, 97 in 177.
 #include <math.h>
 
 #include "kernels.h"
@@ -149,11 +156,12 @@ __device__ __forceinline__ MaxSum warp_join(MaxSum v, float k2) {
   return v;
 }
 
-// 2^((x - base) k2) of a unit's elements, but for a factor that all of them share, exp_factor(base, k2).  fp32 logits: the
-// difference first, which keeps the argument to 2.5 roundings of itself; the factor is 1.  16-bit logits: one multiply-add
-// with -base k2 rounded, one instruction less of ten.  What that rounding adds to every argument is known exactly, and the
-// factor takes it out where the terms have been added up.  Beyond kFusedMost (a row of masked places alone: -1e10 times k2 is
-// rounded by hundreds) the difference first, as for fp32; the rounding is 2^-9 at most below it.
+// 2^((x - base) k2) of a unit's elements, but for a factor that all of them share, exp_factor(base, k2).  fp32
+// logits: the difference first, which keeps the argument to 2.5 roundings of itself; the factor is 1.  16-bit logits:
+// one multiply-add with -base k2 rounded, one instruction less of ten.  What that rounding adds to every argument is
+// known exactly, and the factor takes it out where the terms have been added up.  Beyond kFusedMost (a row of masked
+// places alone: -1e10 times k2 is rounded by hundreds) the difference first, as for fp32; the rounding is 2^-9 at
+// most below it.
 constexpr float kFusedMost = 65536.f;
 template <typename T>
 __device__ __forceinline__ void unit_exp(const Vec<T>& f, float base, float k2, float (&e)[Vec<T>::kN]) {

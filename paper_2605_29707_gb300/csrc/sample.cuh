@@ -23,9 +23,9 @@
 //   Two passes (short vocabularies, guesses that failed).  The row maximum and a safe bound from the maxima of
 //   groups of elements: under top-k where every CTA has k / SP groups that reach a value; under top-p where V
 //   ids of its weight would carry less than 1 - p of what the maxima carry, or, first, a nearer one that the
-//   pass checks.  The second read comes from L2: what is in flight on the chip (46 MB at V = 151936, fp32) fits
-//   it, and a re-read of such slices ran at 11 TB/s against 7 from DRAM; holding them in shared memory left
-//   two CTAs an SM, waiting for each other (512 rows with top-p: 249 us against 173).
+//   pass checks.  The second read comes from L2: what is in flight on the chip (at V = 151936, fp32, 46 MB with eight
+//   CTAs a row, 92 MB with four) fits it, and a re-read of such slices ran at 11 TB/s against 7 from DRAM; holding
+//   them in shared memory left two CTAs an SM, waiting for each other (512 rows with top-p: 249 us against 173).
 //   The first CTA sorts up to kSort candidates by preference, scans their weights, sorts what stays by id and
 //   draws, while the others have left (one row 2.7 us, against 7.4 for radix selections over the list); more of
 //   them it thins out by bins of value first.
@@ -33,10 +33,11 @@
 //   cluster, and the candidates down to the bin that holds the border are gathered, or those in it, which decide
 //   it.  What else leaves too many is cut by a radix selection over the whole row.  Then, and without any
 //   filter, the cluster scans the kept weights in id order.
-// What it measured (device time): V = 151936, one fp32 row with top-k and top-p 12.0 us, 64 rows without a
-// filter 38 us; 512 fp32 rows with top-k 79 us, 3.9 TB/s, with min-p 81, with top-p 119; 1088 bf16 rows with
-// top-k and top-p 107 us, 3.1 TB/s.  For many rows the waves of CTAs end unevenly (3.4 of them at 512 rows) and the
-// first CTA's 6 us stay; more CTAs an SM (48 and 40 registers) gave 77 and 81 us for the first.
+// What it measured (device time): V = 151936, one fp32 row with top-k and top-p 12.0 us; 512 fp32 rows with top-k 80
+// us, 3.9 TB/s, with min-p 81, with top-p 120; 1088 bf16 rows with top-k and top-p 107 us, 3.1 TB/s; temperature
+// alone, which reads the row twice and weighs every element, 64 fp32 rows 38 us, 512 of them 199.  For many rows the
+// waves of CTAs end unevenly (3.4 of them at 512 rows) and the first CTA's 6 us stay; more CTAs an SM (48 and 40
+// registers) gave 77 and 81 us for the first.
 // One translation unit an element type (sample_f32.cu, sample_bf16.cu, sample_f16.cu); sample.cu dispatches.
 #pragma once
 
@@ -384,7 +385,7 @@ __device__ u64 find_border(const ListView& l, u64 need, float top, float scale, 
     }
     if (pairs) before += __shfl_xor_sync(0xffffffffu, before, 1);
     if (e < c && before < want && want <= before + sh.sub_amount[e]) sh.result = o;
-  } else {  // one bit of the order at a time: the greatest order from which on the amounts reach `need`
+  } else {  // hundreds of equal values: one bit of the order at a time, the greatest order from which on the amounts reach `need`
     u64 prefix = 0;
     for (int bit = BY_ID ? 31 : 63; bit >= 0; --bit) {
       const u64 c2 = prefix | (1ull << bit);
@@ -569,7 +570,7 @@ __device__ __forceinline__ void finish_list(int n, u64 tail, const Settings& set
     return finish_sorted(sh.local, sh.n_sub, set.use_k ? 0 : need, 0, set, sc, sh, token, logp);
   }
 
-  // still more: border by border
+  // still more (top-k of several hundreds, min-p on a flat row): border by border
   ListView l{sh.list, n, 0, sc, sh.pow2};
   auto kept = [&] {  // the mass from the cut on
     u64 mass = 0;
