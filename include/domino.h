@@ -56,7 +56,8 @@ enum domino_status {
                                   Ds > 2048, V >= 2^22, or not an sm_103 device */
   DOMINO_ERR_CUDA = -3,        /* a CUDA runtime call or kernel launch failed */
   DOMINO_ERR_TIMEOUT = -4,     /* device: a bounded wait (pipeline barrier, grid barrier) ran out */
-  DOMINO_ERR_BAD_TOKEN = -5    /* device: a prefix id outside [0, V) */
+  DOMINO_ERR_BAD_TOKEN = -5,   /* device: a prefix id outside [0, V) */
+  DOMINO_ERR_BAD_PAGE = -6     /* device: a key's page outside [0, pages) of its cache */
 };
 
 /* The Domino head's weights (section 4.1.2), all device pointers to bf16.
@@ -319,6 +320,118 @@ DOMINO_API int domino_verify_tree_filtered(const void* target_logits, int dtype,
                                            int32_t* row_sample, float* row_logp, int32_t* accepted_nodes,
                                            int32_t* accepted_count, int32_t* bonus_token, void* stream);
 
+/* A target's (or a draft backbone's) cache of keys and values in pages, and a batch of new tokens on it: what the
+ * four entry points below share.  Places 0 .. kv_len[b] - 1 of sequence b hold its keys and values; its new tokens are
+ * the last of them.  With n = start[b + 1] - start[b], new token i of the sequence is row start[b] + i of the token
+ * tensors and has place kv_len[b] - n + i.  Place t lies in page table[b][t / page] at t % page; element d of head h
+ * there at k + page_index page_stride + (t % page) token_stride + h head_stride + d, and the same from v.
+ *   k, v: device, of `dtype`, element-aligned; pages, page, heads and head_dim >= 1, head_dim <= 256.  Strides in
+ *     elements, each at least head_dim (one whose extent is 1 is not looked at): any order of page, token and head.
+ *   table: device int32 [B, table_stride], table_width entries a sequence; pages in any order, shared ones too where
+ *     they are only read.  kv_len [B], start [B + 1] (from 0 on, not falling): device int32, the sequences of a batch
+ *     one after another; n may be 0.  Rows from start[B] on are left as they are.
+ * The structures are host memory and may be freed after the call.  What the device finds out of range is cut off:
+ * start at the token tensors' ends, kv_len at table_width page; nothing outside the tensors is touched. */
+typedef struct domino_kv_cache {
+  void* k;
+  void* v;
+  int64_t page_stride, token_stride, head_stride;
+  int pages, page, heads, head_dim;
+  int dtype; /* DOMINO_F32, DOMINO_BF16 or DOMINO_F16 */
+} domino_kv_cache;
+typedef struct domino_kv_batch {
+  const int32_t* table;
+  int64_t table_stride;
+  int table_width;
+  const int32_t* kv_len;
+  const int32_t* start;
+  int B;
+} domino_kv_batch;
+
+/* Rotary positions: y = R(position) x, the first `rot` elements of every head turned in pairs and the others copied.
+ * Pair i < rot / 2 of a token at position p turns by the angle a = p freq[i]:
+ *   (y0, y1) = amplitude (x0 cos a - x1 sin a, x1 cos a + x0 sin a);
+ *   DOMINO_ROPE_HALF: the pair is (x[i], x[i + rot / 2]);  DOMINO_ROPE_PAIRS: (x[2 i], x[2 i + 1]).
+ * freq and amplitude carry any stretching for long contexts (positions divided by a factor, speeds blended by
+ * frequency, amplitudes scaled with its logarithm).  gradient != 0 turns back, by -a: applied to the gradient by y it
+ * gives the gradient by x.  The angle is taken modulo a turn exactly, at any position; cos, sin and the products in
+ * fp32, one rounding to dtype.
+ *   x, y: device of `dtype`, element-aligned, [tokens][heads][head_dim] with strides in elements between tokens and
+ *     between heads (each at least head_dim; one whose extent is 1 is not looked at); y may be x with the same strides,
+ *     and shares no memory with it otherwise.  positions: device int32 [tokens], any sign.  freq: device fp32
+ *     [rot / 2], radians a position, finite and at most 1024 in size.  amplitude finite.  rot even, 0 <= rot <= head_dim <= 256.
+ * One kernel on `stream`, no workspace.  Returns DOMINO_OK once enqueued, DOMINO_ERR_UNSUPPORTED for another dtype or
+ * a larger head_dim, or another negative code (bad sizes, pointers, layout, tensors of another device) with nothing
+ * enqueued. */
+enum domino_rope_layout { DOMINO_ROPE_HALF = 0, DOMINO_ROPE_PAIRS = 1 };
+DOMINO_API int domino_rope(const void* x, int dtype, int64_t x_token_stride, int64_t x_head_stride,
+                           const int32_t* positions, const float* freq, float amplitude, int layout, int gradient,
+                           int tokens, int heads, int head_dim, int rot, void* y, int64_t y_token_stride,
+                           int64_t y_head_stride, void* stream);
+
+/* New tokens' queries turned, and their keys, turned, and values written to their places in the cache: domino_rope on
+ * q and k with every token's position, one pass over all three.
+ *   q [tokens][q_heads][head_dim], k and v [tokens][heads][head_dim], of the cache's dtype: heads contiguous, token
+ *     strides in elements (parts of one projection's output, say).  q_out [tokens][q_heads][head_dim] with its stride;
+ *     it may be q itself with the same stride.
+ *   positions: device int32 [tokens], or NULL: a token's position is its place; with tree_depth (device int32 [B, N] as
+ *     domino_draft_step writes it) token 0, the anchor, keeps its place and token i <= N has the anchor's place plus
+ *     tree_depth[b][i - 1].  Not both.
+ *   q and q_out NULL with q_heads 0: keys and values alone.
+ * A token whose place is negative or past the table, or whose page lies outside [0, pages), is turned but not written
+ * to the cache (a negative page thus leaves padding out).  Two tokens must not have the same place in the same page.
+ * One kernel on `stream`, no workspace.  Returns as domino_rope. */
+DOMINO_API int domino_rope_append(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
+                                  int64_t v_stride, const int32_t* positions, const int32_t* tree_depth, int N,
+                                  const float* freq, float amplitude, int layout, int rot, int q_heads, int tokens,
+                                  void* q_out, int64_t q_out_stride, const domino_kv_cache* cache,
+                                  const domino_kv_batch* batch, void* stream);
+
+/* Attention of a batch's new tokens over the cache: for every token and query head h, over the keys j that it sees
+ * (of head h / (q_heads / heads), which the query heads of a group share),
+ *   w_j = exp(scale q . k_j - lse),  lse = log sum_j exp(scale q . k_j),  out = sum_j w_j v_j.
+ * Token i of sequence b, with n new tokens, sees
+ *   DOMINO_MASK_CAUSAL: places up to its own (a token alone: all of them);
+ *   DOMINO_MASK_FULL: all kv_len[b] places (a draft block: what was there and all of the block);
+ *   DOMINO_MASK_TREE: the kv_len[b] - n places before the new ones, itself and its ancestors: token 0 is the anchor,
+ *     token i >= 1 tree node i - 1, whose parent is tree_parent[b][i - 1] (device int32 [B, N] as domino_draft_step
+ *     writes it: -1 the anchor, otherwise an earlier node; anything else counts as -1).  Tokens i > N see nothing.
+ * A row that sees nothing has out 0 and lse -inf.  What a row does not see, places behind kv_len and free pages
+ * included, does not reach it, NaN and infinities neither.
+ *   q [tokens][q_heads][head_dim] of the cache's dtype, heads contiguous, with its token stride; out likewise (it may be q with
+ *     the same stride); lse fp32 [tokens][q_heads] or NULL.  q_heads a multiple of heads, at most 128 times as many.
+ *     scale > 0, finite, with scale log2(e) normal in fp32.
+ * bf16 and fp16 products run on the tensor cores where head_dim <= 128 and page are multiples of 8 and pointers and
+ * strides multiples of 16 bytes: scores, maxima, sums and accumulators in fp32, the weights of the second product
+ * rounded to dtype, one rounding at the end.  Everything else takes a plain kernel, in fp32 throughout, a warp a row:
+ * right, and slow on long caches.
+ * workspace: device memory of domino_attend_workspace_bytes(...) bytes, 256-byte aligned, of one call at a time; what
+ *   it holds before does not matter.  Its first int32 receives the device status (DOMINO_OK, DOMINO_ERR_BAD_PAGE where
+ *   a page of a sequence's keys lies outside [0, pages): the rows of that sequence are not specified,
+ *   DOMINO_ERR_TIMEOUT; domino_check_status reads it).  domino_attend_workspace_bytes depends on the current device
+ *   (0 without one, or for sizes that are refused), not on lengths.
+ * Deterministic: the same call gives the same bits.  Two kernels on `stream`.  Returns as domino_rope. */
+enum domino_mask { DOMINO_MASK_CAUSAL = 0, DOMINO_MASK_FULL = 1, DOMINO_MASK_TREE = 2 };
+DOMINO_API size_t domino_attend_workspace_bytes(int tokens, int q_heads, const domino_kv_cache* cache);
+DOMINO_API int domino_attend_paged(const void* q, int64_t q_stride, int tokens, int q_heads,
+                                   const domino_kv_cache* cache, const domino_kv_batch* batch, float scale, int mask,
+                                   const int32_t* tree_parent, int N, void* out, int64_t out_stride, float* lse,
+                                   void* workspace, size_t workspace_bytes, void* stream);
+
+/* After verification, the accepted nodes' keys and values moved to the places right after the anchor, in all layers:
+ * in layer l (keys at k + l layer_stride, values likewise) of sequence b, whose n new tokens are the anchor and the tree's
+ * nodes 0 .. n - 2, node accepted_nodes[b][j] moves to where node j lies, for j < accepted_count[b].
+ *   accepted_nodes [B, N], accepted_count [B]: as domino_verify_tree_* write them (each entry above the one before).
+ *   layer_stride: elements between layers, not looked at for one layer.  N <= 1048576.
+ * Output: new_len int32 [B] = kv_len[b] - (n - 1) + accepted_count[b], the next step's length without its new tokens
+ *   (n = 0 and none accepted: kv_len[b]); it may not be kv_len itself.  A sequence whose list is not rising, names a node
+ *   outside the tree, whose places lie outside the table or in pages outside [0, pages), or whose count is out of range is
+ *   left as it is, with new_len -1.
+ * One kernel on `stream`, no workspace.  Returns as domino_rope. */
+DOMINO_API int domino_cache_commit(const domino_kv_cache* cache, const domino_kv_batch* batch, int layers,
+                                   int64_t layer_stride, const int32_t* accepted_nodes, const int32_t* accepted_count,
+                                   int N, int32_t* new_len, void* stream);
+
 /* Distillation of a teacher's top logits into rows of student logits, e.g. of the target's best kt
  * tokens per draft position (the form of domino_draft_step's topk_ids / topk_logp) into the draft's
  * final or base logits; the row weight carries the position decay exp(-k / gamma) of section 4.2 and
@@ -487,7 +600,10 @@ enum domino_kernel_kind {
                                      tree walk */
   DOMINO_KERNEL_SAMPLE = 9,       /* domino_sample_filtered, and domino_verify_tree_filtered with its walk */
   DOMINO_KERNEL_DISTILL = 10,     /* domino_distill_* */
-  DOMINO_KERNEL_KINDS = 11
+  DOMINO_KERNEL_ROPE = 11,        /* domino_rope, domino_rope_append */
+  DOMINO_KERNEL_ATTEND = 12,      /* domino_attend_paged: both kernels */
+  DOMINO_KERNEL_COMMIT = 13,      /* domino_cache_commit */
+  DOMINO_KERNEL_KINDS = 14
 };
 DOMINO_API int domino_timing_begin(int max_launches);
 DOMINO_API int domino_timing_end(float* total_ms, int* launches, int nkinds);

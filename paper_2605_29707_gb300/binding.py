@@ -19,6 +19,7 @@ DOMINO_ERR_UNSUPPORTED = -2
 DOMINO_ERR_CUDA = -3
 DOMINO_ERR_TIMEOUT = -4
 DOMINO_ERR_BAD_TOKEN = -5
+DOMINO_ERR_BAD_PAGE = -6
 
 # every entry point declared in include/domino.h
 SYMBOLS = ("domino_workspace_bytes", "domino_draft_step", "domino_workspace_bytes_host",
@@ -28,11 +29,13 @@ SYMBOLS = ("domino_workspace_bytes", "domino_draft_step", "domino_workspace_byte
            "domino_rollout_greedy", "domino_rollout_sample", "domino_input_table_bytes",
            "domino_build_input_table", "domino_launches_per_step_table", "domino_debug_hold",
            "domino_verify_tree_sample", "domino_rollout_sample_gumbel", "domino_sample_filtered",
-           "domino_verify_tree_filtered", "domino_distill_loss", "domino_distill_grad", "domino_distill_loss_grad")
+           "domino_verify_tree_filtered", "domino_distill_loss", "domino_distill_grad", "domino_distill_loss_grad",
+           "domino_rope", "domino_rope_append", "domino_attend_workspace_bytes", "domino_attend_paged",
+           "domino_cache_commit")
 
 DOMINO_STATIC_SCRATCH_BYTES = 16 << 20
 
-# element types of logits (domino_sample_filtered, domino_verify_tree_filtered, domino_distill_*)
+# element types of logits (domino_sample_filtered, domino_verify_tree_filtered, domino_distill_*) and of caches
 DOMINO_F32 = 0
 DOMINO_BF16 = 1
 DOMINO_F16 = 2
@@ -41,6 +44,15 @@ DOMINO_F16 = 2
 DOMINO_DISTILL_RENORM = 0
 DOMINO_DISTILL_TAIL = 1
 
+# domino_rope, domino_rope_append: which elements of a head form a pair
+DOMINO_ROPE_HALF = 0
+DOMINO_ROPE_PAIRS = 1
+
+# domino_attend_paged: which of its sequence's keys a new token sees
+DOMINO_MASK_CAUSAL = 0
+DOMINO_MASK_FULL = 1
+DOMINO_MASK_TREE = 2
+
 # domino_debug_hold: what a GRU CTA withholds (a failure-detection test hook)
 DOMINO_HOLD_OFF = 0
 DOMINO_HOLD_STATE = 1
@@ -48,13 +60,25 @@ DOMINO_HOLD_CLEAR_BARRIER = 2
 DOMINO_HOLD_ROW_COPY = 3
 
 KERNEL_KINDS = ("gather", "gru_input_proj", "w1_hidden_proj", "gru", "vocab_gemm_softmax_topk", "merge_tree",
-                "rollout_base_gemm", "rollout_steps", "tree_verify", "sample_filtered", "distill")
+                "rollout_base_gemm", "rollout_steps", "tree_verify", "sample_filtered", "distill",
+                "rope", "attend", "cache_commit")
 
 
 class domino_head_weights(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in
                 ("emb", "w_ih", "w_hh", "b_ih", "b_hh", "w1", "b1", "w2", "b2")] + \
                [("Ds", ctypes.c_int), ("R", ctypes.c_int), ("x_table", ctypes.c_void_p)]
+
+
+class domino_kv_cache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p)] + \
+               [(n, ctypes.c_int64) for n in ("page_stride", "token_stride", "head_stride")] + \
+               [(n, ctypes.c_int) for n in ("pages", "page", "heads", "head_dim", "dtype")]
+
+
+class domino_kv_batch(ctypes.Structure):
+    _fields_ = [("table", ctypes.c_void_p), ("table_stride", ctypes.c_int64), ("table_width", ctypes.c_int),
+                ("kv_len", ctypes.c_void_p), ("start", ctypes.c_void_p), ("B", ctypes.c_int)]
 
 
 class DominoError(RuntimeError):
@@ -134,6 +158,17 @@ def load():
     lib.domino_distill_grad.restype = I
     lib.domino_distill_loss_grad.argtypes = [P, I, L, P, P, P, P, F, I, I, I, I, P, P, P, L, P]
     lib.domino_distill_loss_grad.restype = I
+    cache, batch = ctypes.POINTER(domino_kv_cache), ctypes.POINTER(domino_kv_batch)
+    lib.domino_rope.argtypes = [P, I, L, L, P, P, F, I, I, I, I, I, I, P, L, L, P]
+    lib.domino_rope.restype = I
+    lib.domino_rope_append.argtypes = [P, L, P, L, P, L, P, P, I, P, F, I, I, I, I, P, L, cache, batch, P]
+    lib.domino_rope_append.restype = I
+    lib.domino_attend_workspace_bytes.argtypes = [I, I, cache]
+    lib.domino_attend_workspace_bytes.restype = S
+    lib.domino_attend_paged.argtypes = [P, L, I, I, cache, batch, F, I, P, I, P, L, P, P, S, P]
+    lib.domino_attend_paged.restype = I
+    lib.domino_cache_commit.argtypes = [cache, batch, I, L, P, P, I, P, P]
+    lib.domino_cache_commit.restype = I
     _lib = lib
     return lib
 
@@ -311,6 +346,59 @@ def domino_distill_loss_grad(logits, dtype, row_stride, teacher_ids, teacher_sco
                                                _addr(teacher_scores), _addr(weights), _addr(grad_loss),
                                                float(temperature), int(mode), rows, V, kt, _addr(loss), _addr(lse),
                                                _addr(dlogits), int(grad_stride), _stream(stream)))
+
+
+def make_cache(k, v, page_stride, token_stride, head_stride, pages, page, heads, head_dim, dtype) -> domino_kv_cache:
+    """A paged cache of keys and values (strides in elements).  The structure holds addresses: keep the tensors."""
+    return domino_kv_cache(_addr(k), _addr(v), int(page_stride), int(token_stride), int(head_stride), int(pages),
+                           int(page), int(heads), int(head_dim), int(dtype))
+
+
+def make_batch(table, table_stride, table_width, kv_len, start, B) -> domino_kv_batch:
+    """New tokens of B sequences on a paged cache.  The structure holds addresses: keep the tensors."""
+    return domino_kv_batch(_addr(table), int(table_stride), int(table_width), _addr(kv_len), _addr(start), int(B))
+
+
+def _ref(x):
+    return ctypes.byref(x) if x is not None else None
+
+
+def domino_rope(x, dtype, x_token_stride, x_head_stride, positions, freq, amplitude, layout, gradient, tokens, heads,
+                head_dim, rot, y, y_token_stride, y_head_stride, stream=None) -> int:
+    """y = rotary positions applied to x [tokens][heads][head_dim]; gradient: turned back (device)."""
+    return int(load().domino_rope(_addr(x), int(dtype), int(x_token_stride), int(x_head_stride), _addr(positions),
+                                  _addr(freq), float(amplitude), int(layout), int(gradient), tokens, heads, head_dim,
+                                  rot, _addr(y), int(y_token_stride), int(y_head_stride), _stream(stream)))
+
+
+def domino_rope_append(q, q_stride, k, k_stride, v, v_stride, positions, tree_depth, N, freq, amplitude, layout, rot,
+                       q_heads, tokens, q_out, q_out_stride, cache, batch, stream=None) -> int:
+    """New tokens' queries turned into q_out; their keys, turned, and values written to the paged cache (device)."""
+    return int(load().domino_rope_append(_addr(q), int(q_stride), _addr(k), int(k_stride), _addr(v), int(v_stride),
+                                         _addr(positions), _addr(tree_depth), int(N), _addr(freq), float(amplitude),
+                                         int(layout), rot, q_heads, tokens, _addr(q_out), int(q_out_stride),
+                                         _ref(cache), _ref(batch), _stream(stream)))
+
+
+def domino_attend_workspace_bytes(tokens, q_heads, cache) -> int:
+    return int(load().domino_attend_workspace_bytes(tokens, q_heads, _ref(cache)))
+
+
+def domino_attend_paged(q, q_stride, tokens, q_heads, cache, batch, scale, mask, tree_parent, N, out, out_stride, lse,
+                        workspace, workspace_bytes, stream=None) -> int:
+    """Attention of a batch's new tokens over the paged cache: out, and lse fp32 [tokens][q_heads] or None (device)."""
+    return int(load().domino_attend_paged(_addr(q), int(q_stride), tokens, q_heads, _ref(cache), _ref(batch),
+                                          float(scale), int(mask), _addr(tree_parent), int(N), _addr(out),
+                                          int(out_stride), _addr(lse), _addr(workspace), int(workspace_bytes),
+                                          _stream(stream)))
+
+
+def domino_cache_commit(cache, batch, layers, layer_stride, accepted_nodes, accepted_count, N, new_len,
+                        stream=None) -> int:
+    """The accepted nodes' keys and values moved behind the anchor in all layers; new_len [B] (device)."""
+    return int(load().domino_cache_commit(_ref(cache), _ref(batch), int(layers), int(layer_stride),
+                                          _addr(accepted_nodes), _addr(accepted_count), int(N), _addr(new_len),
+                                          _stream(stream)))
 
 
 def domino_rollout_workspace_bytes(B, K, H, V, Ds, R) -> int:

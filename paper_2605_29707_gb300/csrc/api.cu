@@ -839,6 +839,7 @@ const char* domino_status_string(int status) {
     case DOMINO_ERR_CUDA: return "DOMINO_ERR_CUDA";
     case DOMINO_ERR_TIMEOUT: return "DOMINO_ERR_TIMEOUT";
     case DOMINO_ERR_BAD_TOKEN: return "DOMINO_ERR_BAD_TOKEN";
+    case DOMINO_ERR_BAD_PAGE: return "DOMINO_ERR_BAD_PAGE";
     default: return "DOMINO_ERR_UNKNOWN";
   }
 }
@@ -1088,6 +1089,278 @@ int domino_distill_loss_grad(const void* logits, int dtype, int64_t row_stride, 
   if (!loss || !dlogits) return DOMINO_ERR_INVALID_ARG;
   return run_distill(logits, dtype, row_stride, teacher_ids, teacher_scores, weights, grad_loss, temperature, mode,
                      rows, V, kt, loss, lse, dlogits, grad_stride, stream);
+} catch (...) {
+  return DOMINO_ERR_CUDA;
+}
+
+// ---------------------------------------------------------------- a paged cache: rotary positions, attention, accepted nodes
+static_assert(dm::kMaskCausal == DOMINO_MASK_CAUSAL && dm::kMaskFull == DOMINO_MASK_FULL &&
+                  dm::kMaskTree == DOMINO_MASK_TREE,
+              "masks");
+
+namespace {
+constexpr int64_t kMaxElems = 1LL << 60;  // what any tensor's last element stays below: its address is formed in 64 bits
+
+size_t elem_bytes(int dtype) { return dtype == DOMINO_F32 ? 4 : 2; }
+
+// A stride between n slices of `least` elements and more.
+bool stride_ok(int64_t stride, int64_t n, int64_t least) {
+  return n == 1 || (stride >= least && stride <= kMaxElems / n);
+}
+
+// True where every slice of the tensor begins on a boundary of `bytes`.
+bool stride_aligned(int64_t stride, int64_t n, int dtype, size_t bytes) {
+  return n == 1 || stride % static_cast<int64_t>(bytes / elem_bytes(dtype)) == 0;
+}
+
+int check_dtype(int dtype) {
+  return dtype == DOMINO_F32 || dtype == DOMINO_BF16 || dtype == DOMINO_F16 ? DOMINO_OK : DOMINO_ERR_UNSUPPORTED;
+}
+
+int check_cache(const domino_kv_cache* c) {
+  if (!c || !c->k || !c->v || c->pages < 1 || c->page < 1 || c->heads < 1 || c->head_dim < 1) return DOMINO_ERR_INVALID_ARG;
+  const int rc = check_dtype(c->dtype);
+  if (rc != DOMINO_OK) return rc;
+  if (c->head_dim > dm::kMaxHeadDim || c->heads > (1 << 14)) return DOMINO_ERR_UNSUPPORTED;
+  if (!stride_ok(c->page_stride, c->pages, c->head_dim) || !stride_ok(c->token_stride, c->page, c->head_dim) ||
+      !stride_ok(c->head_stride, c->heads, c->head_dim))
+    return DOMINO_ERR_INVALID_ARG;
+  const size_t e = elem_bytes(c->dtype);
+  return aligned(c->k, e) && aligned(c->v, e) ? DOMINO_OK : DOMINO_ERR_INVALID_ARG;
+}
+
+int check_batch(const domino_kv_batch* b) {
+  if (!b || !b->table || !b->kv_len || !b->start || b->B < 1 || b->table_width < 1) return DOMINO_ERR_INVALID_ARG;
+  if (!stride_ok(b->table_stride, b->B, b->table_width)) return DOMINO_ERR_INVALID_ARG;
+  return aligned(b->table, 4) && aligned(b->kv_len, 4) && aligned(b->start, 4) ? DOMINO_OK : DOMINO_ERR_INVALID_ARG;
+}
+
+// Rows [tokens][heads][D] with contiguous heads.
+int check_heads(const void* x, int64_t stride, int tokens, int64_t heads, int D, int dtype) {
+  if (!x || !aligned(x, elem_bytes(dtype))) return DOMINO_ERR_INVALID_ARG;
+  return stride_ok(stride, tokens, heads * D) ? DOMINO_OK : DOMINO_ERR_INVALID_ARG;
+}
+
+// A cache's slices all begin on boundaries of `bytes`.
+bool cache_aligned(const domino_kv_cache& c, size_t bytes) {
+  return aligned(c.k, bytes) && aligned(c.v, bytes) && stride_aligned(c.page_stride, c.pages, c.dtype, bytes) &&
+         stride_aligned(c.token_stride, c.page, c.dtype, bytes) && stride_aligned(c.head_stride, c.heads, c.dtype, bytes);
+}
+
+dm::PagedCache paged_cache(const domino_kv_cache& c) {
+  dm::PagedCache d{};
+  d.k = c.k; d.v = c.v;
+  // a slice that is alone has no stride
+  d.page_stride = c.pages > 1 ? c.page_stride : 0;
+  d.token_stride = c.page > 1 ? c.token_stride : 0;
+  d.head_stride = c.heads > 1 ? c.head_stride : 0;
+  d.pages = c.pages; d.page = c.page; d.heads = c.heads; d.D = c.head_dim;
+  return d;
+}
+
+dm::PagedBatch paged_batch(const domino_kv_batch& b) {
+  dm::PagedBatch d{};
+  d.table = b.table;
+  d.table_stride = b.B > 1 ? b.table_stride : 0;
+  d.table_width = b.table_width;
+  d.kv_len = b.kv_len; d.start = b.start; d.B = b.B;
+  return d;
+}
+
+// What turns: freq, amplitude, layout and the heads' share.
+int check_rotation(const float* freq, float amplitude, int layout, int rot, int D) {
+  if (rot < 0 || rot > D || rot % 2 != 0 || !std::isfinite(amplitude)) return DOMINO_ERR_INVALID_ARG;
+  if (layout != DOMINO_ROPE_HALF && layout != DOMINO_ROPE_PAIRS) return DOMINO_ERR_INVALID_ARG;
+  return rot == 0 || (freq && aligned(freq, 4)) ? DOMINO_OK : DOMINO_ERR_INVALID_ARG;
+}
+
+int enqueue_rope(dm::RopeParams& r, int dtype, int layout, bool by16, bool by8, void* stream) {
+  int sms = 0, major = 0, minor = 0;
+  int rc = device_sms(&sms, &major, &minor);
+  if (rc != DOMINO_OK) return rc;
+  r.pairs = layout == DOMINO_ROPE_PAIRS;
+  const int n16 = static_cast<int>(16 / elem_bytes(dtype)), n8 = n16 / 2;
+  const int unit = by16 && r.rot / 2 % n16 == 0 && r.D % n16 == 0 ? 16 : by8 && r.rot / 2 % n8 == 0 && r.D % n8 == 0 ? 8 : 0;
+  const long long blocks = (static_cast<long long>(r.tokens) * r.D + 255) / 256;  // the most that any unit takes
+  if (blocks > 0x7fffffffLL) return DOMINO_ERR_UNSUPPORTED;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const int ts = timing_open(DOMINO_KERNEL_ROPE, st);
+  rc = cuda_rc(dm::launch_rope(r, dtype, unit, sms, st));
+  timing_close(ts, st);
+  return rc;
+}
+}  // namespace
+
+int domino_rope(const void* x, int dtype, int64_t x_token_stride, int64_t x_head_stride, const int32_t* positions,
+                const float* freq, float amplitude, int layout, int gradient, int tokens, int heads, int head_dim, int rot,
+                void* y, int64_t y_token_stride, int64_t y_head_stride, void* stream) try {
+  if (!x || !y || !positions || tokens < 1 || heads < 1 || head_dim < 1) return DOMINO_ERR_INVALID_ARG;
+  int rc = check_dtype(dtype);
+  if (rc != DOMINO_OK) return rc;
+  if (head_dim > dm::kMaxHeadDim || heads > (1 << 14)) return DOMINO_ERR_UNSUPPORTED;
+  rc = check_rotation(freq, amplitude, layout, rot, head_dim);
+  if (rc != DOMINO_OK) return rc;
+  if (!stride_ok(x_token_stride, tokens, head_dim) || !stride_ok(x_head_stride, heads, head_dim) ||
+      !stride_ok(y_token_stride, tokens, head_dim) || !stride_ok(y_head_stride, heads, head_dim))
+    return DOMINO_ERR_INVALID_ARG;
+  const size_t e = elem_bytes(dtype);
+  if (!aligned(x, e) || !aligned(y, e) || !aligned(positions, 4)) return DOMINO_ERR_INVALID_ARG;
+  if (x == y && ((tokens > 1 && x_token_stride != y_token_stride) || (heads > 1 && x_head_stride != y_head_stride)))
+    return DOMINO_ERR_INVALID_ARG;
+  rc = check_device(x);
+  if (rc != DOMINO_OK) return rc;
+  dm::RopeParams r{};
+  r.x = x; r.x_token = tokens > 1 ? x_token_stride : 0; r.x_head = heads > 1 ? x_head_stride : 0;
+  r.y = y; r.y_token = tokens > 1 ? y_token_stride : 0; r.y_head = heads > 1 ? y_head_stride : 0;
+  r.heads = heads;
+  r.positions = positions;
+  r.freq = freq; r.amplitude = amplitude;
+  r.back = gradient != 0;
+  r.tokens = tokens; r.D = head_dim; r.rot = rot;
+  auto by = [&](size_t n) {
+    return aligned(x, n) && aligned(y, n) && stride_aligned(x_token_stride, tokens, dtype, n) &&
+           stride_aligned(y_token_stride, tokens, dtype, n) && stride_aligned(x_head_stride, heads, dtype, n) &&
+           stride_aligned(y_head_stride, heads, dtype, n);
+  };
+  return enqueue_rope(r, dtype, layout, by(16), by(8), stream);
+} catch (...) {
+  return DOMINO_ERR_CUDA;
+}
+
+int domino_rope_append(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                       const int32_t* positions, const int32_t* tree_depth, int N, const float* freq, float amplitude,
+                       int layout, int rot, int q_heads, int tokens, void* q_out, int64_t q_out_stride,
+                       const domino_kv_cache* cache, const domino_kv_batch* batch, void* stream) try {
+  int rc = check_cache(cache);
+  if (rc == DOMINO_OK) rc = check_batch(batch);
+  if (rc != DOMINO_OK) return rc;
+  const int D = cache->head_dim, dtype = cache->dtype;
+  if (tokens < 1 || q_heads < 0 || N < 0 || (positions && tree_depth)) return DOMINO_ERR_INVALID_ARG;
+  if (q_heads > (1 << 14)) return DOMINO_ERR_UNSUPPORTED;
+  rc = check_rotation(freq, amplitude, layout, rot, D);
+  if (rc == DOMINO_OK) rc = check_heads(k, k_stride, tokens, cache->heads, D, dtype);
+  if (rc == DOMINO_OK) rc = check_heads(v, v_stride, tokens, cache->heads, D, dtype);
+  if (rc == DOMINO_OK && q_heads > 0) rc = check_heads(q, q_stride, tokens, q_heads, D, dtype);
+  if (rc == DOMINO_OK && q_heads > 0) rc = check_heads(q_out, q_out_stride, tokens, q_heads, D, dtype);
+  if (rc != DOMINO_OK) return rc;
+  if (q_heads > 0 && q == q_out && tokens > 1 && q_stride != q_out_stride) return DOMINO_ERR_INVALID_ARG;
+  if (!aligned(positions, 4) || !aligned(tree_depth, 4)) return DOMINO_ERR_INVALID_ARG;
+  rc = check_device(cache->k);
+  if (rc == DOMINO_OK) rc = check_device(k);
+  if (rc != DOMINO_OK) return rc;
+  dm::RopeParams r{};
+  if (q_heads > 0) {
+    r.x = q; r.x_token = tokens > 1 ? q_stride : 0; r.x_head = D;
+    r.y = q_out; r.y_token = tokens > 1 ? q_out_stride : 0; r.y_head = D;
+    r.heads = q_heads;
+  }
+  r.k = k; r.k_token = tokens > 1 ? k_stride : 0;
+  r.v = v; r.v_token = tokens > 1 ? v_stride : 0;
+  r.positions = positions;
+  r.depth = tree_depth; r.N = N;
+  r.freq = freq; r.amplitude = amplitude;
+  r.tokens = tokens; r.D = D; r.rot = rot;
+  r.cache = paged_cache(*cache);
+  r.batch = paged_batch(*batch);
+  auto by = [&](size_t n) {
+    const bool queries = q_heads == 0 || (aligned(q, n) && aligned(q_out, n) && stride_aligned(q_stride, tokens, dtype, n) &&
+                                          stride_aligned(q_out_stride, tokens, dtype, n));
+    return queries && aligned(k, n) && aligned(v, n) && stride_aligned(k_stride, tokens, dtype, n) &&
+           stride_aligned(v_stride, tokens, dtype, n) && cache_aligned(*cache, n);
+  };
+  return enqueue_rope(r, dtype, layout, by(16), by(8), stream);
+} catch (...) {
+  return DOMINO_ERR_CUDA;
+}
+
+namespace {
+int check_attend(int tokens, int q_heads, const domino_kv_cache* cache) {
+  const int rc = check_cache(cache);
+  if (rc != DOMINO_OK) return rc;
+  if (tokens < 1 || q_heads < 1 || q_heads % cache->heads != 0) return DOMINO_ERR_INVALID_ARG;
+  if (q_heads / cache->heads > 128 || q_heads > (1 << 14)) return DOMINO_ERR_UNSUPPORTED;
+  if (static_cast<long long>(tokens) * q_heads > 0x7fffffffLL) return DOMINO_ERR_UNSUPPORTED;
+  return DOMINO_OK;
+}
+}  // namespace
+
+size_t domino_attend_workspace_bytes(int tokens, int q_heads, const domino_kv_cache* cache) {
+  int sms = 0, major = 0, minor = 0;
+  if (check_attend(tokens, q_heads, cache) != DOMINO_OK || device_sms(&sms, &major, &minor) != DOMINO_OK) return 0;
+  return 256;
+}
+
+int domino_attend_paged(const void* q, int64_t q_stride, int tokens, int q_heads, const domino_kv_cache* cache,
+                        const domino_kv_batch* batch, float scale, int mask, const int32_t* tree_parent, int N, void* out,
+                        int64_t out_stride, float* lse, void* workspace, size_t workspace_bytes, void* stream) try {
+  int rc = check_attend(tokens, q_heads, cache);
+  if (rc == DOMINO_OK) rc = check_batch(batch);
+  if (rc != DOMINO_OK) return rc;
+  const int D = cache->head_dim, dtype = cache->dtype;
+  rc = check_heads(q, q_stride, tokens, q_heads, D, dtype);
+  if (rc == DOMINO_OK) rc = check_heads(out, out_stride, tokens, q_heads, D, dtype);
+  if (rc != DOMINO_OK) return rc;
+  if (q == out && tokens > 1 && q_stride != out_stride) return DOMINO_ERR_INVALID_ARG;
+  if (mask != DOMINO_MASK_CAUSAL && mask != DOMINO_MASK_FULL && mask != DOMINO_MASK_TREE) return DOMINO_ERR_INVALID_ARG;
+  if (N < 0 || (mask == DOMINO_MASK_TREE && N > 0 && !tree_parent)) return DOMINO_ERR_INVALID_ARG;
+  const float scale_log2 = static_cast<float>(static_cast<double>(scale) * 1.4426950408889634);
+  if (!(scale > 0.f) || !std::isfinite(scale) || !std::isnormal(scale_log2)) return DOMINO_ERR_INVALID_ARG;
+  if (!aligned(tree_parent, 4) || !aligned(lse, 4) || !workspace || !aligned(workspace, 256)) return DOMINO_ERR_INVALID_ARG;
+  rc = check_device(cache->k);
+  if (rc == DOMINO_OK) rc = check_device(q);
+  if (rc != DOMINO_OK) return rc;
+  if (workspace_bytes < domino_attend_workspace_bytes(tokens, q_heads, cache)) return DOMINO_ERR_INVALID_ARG;
+  dm::AttendParams a{};
+  a.q = q; a.q_stride = tokens > 1 ? q_stride : 0;
+  a.tokens = tokens; a.hq = q_heads; a.group = q_heads / cache->heads;
+  a.cache = paged_cache(*cache);
+  a.batch = paged_batch(*batch);
+  a.scale = scale; a.scale_log2 = scale_log2;
+  a.mask = mask;
+  a.parent = mask == DOMINO_MASK_TREE ? tree_parent : nullptr;
+  a.N = N;
+  a.out = out; a.out_stride = tokens > 1 ? out_stride : 0;
+  a.lse = lse;
+  a.status = static_cast<int*>(workspace);
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (cudaMemsetAsync(workspace, 0, sizeof(int), st) != cudaSuccess) return DOMINO_ERR_CUDA;
+  const bool vector = cache_aligned(*cache, 16) && D % static_cast<int>(16 / elem_bytes(dtype)) == 0;
+  const int ts = timing_open(DOMINO_KERNEL_ATTEND, st);
+  rc = cuda_rc(dm::launch_attend_rows(a, dtype, vector, st));
+  timing_close(ts, st);
+  return rc;
+} catch (...) {
+  return DOMINO_ERR_CUDA;
+}
+
+int domino_cache_commit(const domino_kv_cache* cache, const domino_kv_batch* batch, int layers, int64_t layer_stride,
+                        const int32_t* accepted_nodes, const int32_t* accepted_count, int N, int32_t* new_len,
+                        void* stream) try {
+  int rc = check_cache(cache);
+  if (rc == DOMINO_OK) rc = check_batch(batch);
+  if (rc != DOMINO_OK) return rc;
+  if (layers < 1 || N < 0 || N > (1 << 20) || !accepted_count || !new_len || (N > 0 && !accepted_nodes))
+    return DOMINO_ERR_INVALID_ARG;
+  if (layers > 32767) return DOMINO_ERR_UNSUPPORTED;
+  if (!stride_ok(layer_stride, layers, cache->head_dim) || new_len == batch->kv_len) return DOMINO_ERR_INVALID_ARG;
+  if (!aligned(accepted_nodes, 4) || !aligned(accepted_count, 4) || !aligned(new_len, 4)) return DOMINO_ERR_INVALID_ARG;
+  rc = check_device(cache->k);
+  if (rc != DOMINO_OK) return rc;
+  dm::CommitParams c{};
+  c.cache = paged_cache(*cache);
+  c.batch = paged_batch(*batch);
+  c.layers = layers;
+  c.layer_stride = layers > 1 ? layer_stride : 0;
+  c.nodes = accepted_nodes; c.count = accepted_count; c.N = N;
+  c.new_len = new_len;
+  const size_t e = elem_bytes(cache->dtype);
+  const bool vector = cache_aligned(*cache, 16) && stride_aligned(layer_stride, layers, cache->dtype, 16) &&
+                      cache->head_dim % static_cast<int>(16 / e) == 0;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const int ts = timing_open(DOMINO_KERNEL_COMMIT, st);
+  rc = cuda_rc(dm::launch_commit(c, static_cast<int>(e), vector, st));
+  timing_close(ts, st);
+  return rc;
 } catch (...) {
   return DOMINO_ERR_CUDA;
 }

@@ -300,4 +300,76 @@ struct DistillParams {
 };
 cudaError_t launch_distill(const DistillParams& p, int dtype, int rows, cudaStream_t stream);
 
+// ---------------------------------------------------------------- a paged cache (cache.cu, attend*.cu)
+constexpr int kMaxHeadDim = 256;
+
+struct PagedCache {
+  void *k, *v;
+  long long page_stride, token_stride, head_stride;  // elements
+  int pages, page, heads, D;
+};
+struct PagedBatch {
+  const int32_t* table;
+  long long table_stride;
+  int table_width;
+  const int32_t* kv_len;
+  const int32_t* start;
+  int B;
+};
+
+struct RopeParams {
+  const void* x;  // queries, or what domino_rope turns: [tokens][heads][D]
+  long long x_token, x_head;
+  void* y;
+  long long y_token, y_head;
+  int heads;  // of x (0: none)
+  const void *k, *v;  // append: new keys and values, heads contiguous; nullptr: none
+  long long k_token, v_token;
+  const int32_t* positions;  // [tokens]; nullptr: by place (and depth)
+  const int32_t* depth;      // [B][N] or nullptr
+  int N;
+  const float* freq;
+  float amplitude;
+  int pairs;  // pairs of neighbours instead of halves
+  int back;
+  int tokens, D, rot;
+  PagedCache cache;
+  PagedBatch batch;
+};
+// unit_bytes: 16 or 8 where every pointer and stride, rot / 2 and D are whole units; otherwise anything else
+cudaError_t launch_rope(const RopeParams& p, int dtype, int unit_bytes, int sms, cudaStream_t stream);
+
+struct CommitParams {
+  PagedCache cache;
+  PagedBatch batch;
+  int layers;
+  long long layer_stride;
+  const int32_t* nodes;  // [B][N]
+  const int32_t* count;  // [B]
+  int N;
+  int32_t* new_len;
+};
+cudaError_t launch_commit(const CommitParams& p, int elem_bytes, bool vector, cudaStream_t stream);
+
+// Masks; numerically equal to enum domino_mask.
+constexpr int kMaskCausal = 0, kMaskFull = 1, kMaskTree = 2;
+
+struct AttendParams {
+  const void* q;
+  long long q_stride;
+  int tokens, hq, group;  // group: query heads a head of keys
+  PagedCache cache;
+  PagedBatch batch;
+  float scale, scale_log2;  // scale log2(e)
+  int mask;
+  const int32_t* parent;  // [B][N]
+  int N;
+  void* out;
+  long long out_stride;
+  float* lse;   // [tokens][hq] or nullptr
+  int* status;  // the workspace's first word
+};
+// Any type and layout: a warp a row.  Status already cleared.
+cudaError_t launch_attend_rows(const AttendParams& p, int dtype, bool vector, cudaStream_t stream);
+
 }  // namespace dm

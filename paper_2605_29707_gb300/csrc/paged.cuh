@@ -1,0 +1,49 @@
+// paged.cuh -- places of a paged cache and the sequences of a batch, as the device reads them.
+#pragma once
+
+#include "kernels.h"
+
+namespace dm {
+
+// The places that the table holds, in int range.
+__device__ __forceinline__ int table_places(const PagedCache& c, const PagedBatch& b) {
+  const long long n = static_cast<long long>(b.table_width) * c.page;
+  return n > 0x7fffffffLL ? 0x7fffffff : static_cast<int>(n);
+}
+
+struct Sequence {
+  int row;  // its first new token's row
+  int n;    // new tokens
+  int kv;   // keys, the new ones among them
+};
+
+// What the batch says of sequence b, cut off at the tensors' ends.
+__device__ __forceinline__ Sequence load_sequence(const PagedCache& c, const PagedBatch& b, int tokens, int seq) {
+  const int s0 = b.start[seq], s1 = b.start[seq + 1], kv = b.kv_len[seq];
+  Sequence s;
+  s.row = min(max(s0, 0), tokens);
+  s.n = min(max(s1, s.row), tokens) - s.row;
+  s.kv = min(max(kv, 0), table_places(c, b));
+  return s;
+}
+
+// The sequence that row `token` belongs to, or -1.
+__device__ __forceinline__ int find_sequence(const PagedBatch& b, int token) {
+  int lo = 0, hi = b.B;  // start[lo] <= token < start[hi]
+  if (token < b.start[0] || token >= b.start[hi]) return -1;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (b.start[mid] <= token) lo = mid; else hi = mid;
+  }
+  return lo;
+}
+
+// Element offset of (place, head 0), or -1 where the place has no page.
+__device__ __forceinline__ long long place_offset(const PagedCache& c, const PagedBatch& b, int seq, int place) {
+  if (place < 0 || place >= table_places(c, b)) return -1;
+  const int i = place / c.page, pg = b.table[seq * b.table_stride + i];
+  if (pg < 0 || pg >= c.pages) return -1;
+  return pg * c.page_stride + (place - i * c.page) * c.token_stride;
+}
+
+}  // namespace dm

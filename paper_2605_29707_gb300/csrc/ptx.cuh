@@ -15,6 +15,7 @@ namespace dm {
 constexpr int kStatusUnsupported = -2;
 constexpr int kStatusTimeout = -4;
 constexpr int kStatusBadToken = -5;
+constexpr int kStatusBadPage = -6;
 
 constexpr long long kWaitCycles = 2000000000LL;  // ~1 s at the GB300 SM clock
 
@@ -106,6 +107,16 @@ __device__ __forceinline__ void tma_load_2d(void* dst, const CUtensorMap* tm, ui
       "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint"
       " [%0], [%1, {%3, %4}], [%2], %5;" ::"r"(smem_u32(dst)),
       "l"(reinterpret_cast<uint64_t>(tm)), "r"(smem_u32(bar)), "r"(x), "r"(y), "l"(policy)
+      : "memory");
+}
+
+// The same for a 4-D tensor: coordinates outside it read as zero.
+__device__ __forceinline__ void tma_load_4d(void* dst, const CUtensorMap* tm, uint64_t* bar, int x, int y, int z, int w,
+                                            uint64_t policy) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint"
+      " [%0], [%1, {%3, %4, %5, %6}], [%2], %7;" ::"r"(smem_u32(dst)),
+      "l"(reinterpret_cast<uint64_t>(tm)), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z), "r"(w), "l"(policy)
       : "memory");
 }
 
@@ -235,11 +246,23 @@ __device__ __forceinline__ uint64_t smem_desc_sw128(uint32_t saddr) {
   return d;
 }
 
+// The same for an MN-major operand: rows along K, 64 elements of MN (128 B) each, 8-row atoms 1024 B apart
+// (stride byte offset); the next 64 elements of MN lie `block` bytes on (leading byte offset).  Stepping K by 16 rows
+// adds 2048 bytes to the address.
+__device__ __forceinline__ uint64_t smem_desc_sw128_mn(uint32_t saddr, uint32_t block) {
+  return (smem_desc_sw128(saddr) & ~(static_cast<uint64_t>(0x3FFF) << 16)) | (static_cast<uint64_t>(block >> 4) << 16);
+}
+
 // Instruction descriptor of kind::f16: D fp32 (bits 4-5 = 1), A and B bf16 (bits 7-9 and
 // 10-12 = 1), both K-major (bits 15, 16 = 0), N >> 3 in bits 17-22, M >> 4 in bits 24-28.
 __host__ __device__ constexpr uint32_t idesc_bf16_f32(int M, int N) {
   return (1u << 4) | (1u << 7) | (1u << 10) | (static_cast<uint32_t>(N >> 3) << 17) |
          (static_cast<uint32_t>(M >> 4) << 24);
+}
+
+// The same for f16 operands (format 0), or for bf16 ones; b_mn: B is MN-major.
+__host__ __device__ constexpr uint32_t idesc_16_f32(bool bf16, int M, int N, bool b_mn) {
+  return (idesc_bf16_f32(M, N) & (bf16 ? ~0u : ~((7u << 7) | (7u << 10)))) | (b_mn ? 1u << 16 : 0u);
 }
 
 // ------------------------------------------------------------------ tcgen05, CTA pairs
