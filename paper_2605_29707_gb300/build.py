@@ -20,7 +20,7 @@ LIB = os.path.join(PKG, "libdomino.so")
 SOURCES = ["api.cu", "tc_softmax.cu", "tc_softmax_k8.cu", "tc_store.cu", "gru.cu", "tree.cu", "verify.cu", "rollout.cu",
            "rollout_race.cu", "rollout_resident_fast.cu", "rollout_resident_three.cu", "rollout_resident_race_fast.cu",
            "rollout_resident_race_three.cu", "sample.cu", "sample_f32.cu",
-           "sample_bf16.cu", "sample_f16.cu", "distill.cu", "cache.cu", "attend_rows.cu"]
+           "sample_bf16.cu", "sample_f16.cu", "distill.cu", "cache.cu", "attend.cu", "attend_rows.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 

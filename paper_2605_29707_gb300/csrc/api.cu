@@ -1284,10 +1284,96 @@ int check_attend(int tokens, int q_heads, const domino_kv_cache* cache) {
 }
 }  // namespace
 
+namespace {
+// The tensor cores take this cache's element type, heads and pages (pointers and strides apart).
+bool attend_tc_shape(const domino_kv_cache& c) {
+  return c.dtype != DOMINO_F32 && c.head_dim <= 128 && c.head_dim % 8 == 0 && c.page % 8 == 0;
+}
+
+struct AttendPlan {
+  int tile_tokens, slot_rows;
+  size_t off_codes, off_tails, off_norms, off_parts, total;
+};
+
+AttendPlan plan_attend(int tokens, int q_heads, const domino_kv_cache& c, int sms) {
+  AttendPlan p{};
+  size_t off = 0;
+  auto take = [&](size_t bytes) {
+    const size_t o = off;
+    off = align_up(off + bytes);
+    return o;
+  };
+  take(sizeof(int));  // the status
+  if (!attend_tc_shape(c)) {
+    p.total = off;
+    return p;
+  }
+  const int group = q_heads / c.heads;
+  p.tile_tokens = dm::kAttendRows / group;
+  // two tiles' rows, or those of the few tokens that one tile holds
+  p.slot_rows = tokens > p.tile_tokens ? 2 * dm::kAttendRows : (tokens * group + 31) / 32 * 32;
+  p.off_codes = take(sizeof(int) * sms);
+  p.off_tails = take(sizeof(dm::AttendTail) * sms);
+  p.off_norms = take(sizeof(float) * 2 * sms * 2 * p.slot_rows);
+  p.off_parts = take(sizeof(float) * 2 * sms * c.head_dim * p.slot_rows);
+  p.total = off;
+  return p;
+}
+
+// The cache as (element, token, head, page): boxes of 64 elements and `piece` tokens, 128-byte swizzling; what lies outside
+// reads as zero.
+bool make_cache_map(CUtensorMap* m, const void* base, const domino_kv_cache& c, uint32_t piece) {
+  auto fn = encode_fn();
+  if (!fn) return false;
+  // a slice that is alone has any stride
+  auto stride = [](int64_t s, int n) { return static_cast<cuuint64_t>(n > 1 ? 2 * s : 256); };
+  cuuint64_t dims[4] = {static_cast<cuuint64_t>(c.head_dim), static_cast<cuuint64_t>(c.page),
+                        static_cast<cuuint64_t>(c.heads), static_cast<cuuint64_t>(c.pages)};
+  cuuint64_t strides[3] = {stride(c.token_stride, c.page), stride(c.head_stride, c.heads), stride(c.page_stride, c.pages)};
+  cuuint32_t box[4] = {64, piece, 1, 1};
+  cuuint32_t estr[4] = {1, 1, 1, 1};
+  return fn(m, c.dtype == DOMINO_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4,
+            const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// A launch of at most kAttendSeqs sequences after the other.
+int enqueue_attend_tc(const dm::AttendParams& a, const domino_kv_cache& c, int sms, uint8_t* ws, cudaStream_t st) {
+  const AttendPlan plan = plan_attend(a.tokens, a.hq, c, sms);
+  dm::AttendSplit s{};
+  s.piece = std::min(dm::kAttendKeys, c.page & -c.page);
+  s.tile_tokens = plan.tile_tokens;
+  s.slot_rows = plan.slot_rows;
+  s.codes = reinterpret_cast<int*>(ws + plan.off_codes);
+  s.tails = reinterpret_cast<dm::AttendTail*>(ws + plan.off_tails);
+  s.norms = reinterpret_cast<float*>(ws + plan.off_norms);
+  s.parts = reinterpret_cast<float*>(ws + plan.off_parts);
+  CUtensorMap keys, values;
+  if (!make_cache_map(&keys, c.k, c, s.piece) || !make_cache_map(&values, c.v, c, s.piece)) return DOMINO_ERR_CUDA;
+  const int all = a.batch.B;
+  for (int b = 0; b < all; b += dm::kAttendSeqs) {
+    dm::AttendParams part = a;
+    part.batch.B = std::min(dm::kAttendSeqs, all - b);
+    part.batch.table += b * a.batch.table_stride;
+    part.batch.kv_len += b;
+    part.batch.start += b;
+    if (a.parent) part.parent += static_cast<long long>(b) * a.N;
+    s.first = b == 0;
+    // at most this much work: fewer CTAs where there is less of it than SMs
+    const long long groups = a.tokens / (2 * plan.tile_tokens) + part.batch.B;
+    const long long tiles = static_cast<long long>(a.batch.table_width) * c.page / dm::kAttendKeys + 1;
+    const double units = static_cast<double>(groups) * tiles * c.heads;
+    const int rc = cuda_rc(dm::launch_attend_tc(keys, values, part, s, c.dtype, units < sms ? static_cast<int>(units) : sms, st));
+    if (rc != DOMINO_OK) return rc;
+  }
+  return DOMINO_OK;
+}
+}  // namespace
+
 size_t domino_attend_workspace_bytes(int tokens, int q_heads, const domino_kv_cache* cache) {
   int sms = 0, major = 0, minor = 0;
   if (check_attend(tokens, q_heads, cache) != DOMINO_OK || device_sms(&sms, &major, &minor) != DOMINO_OK) return 0;
-  return 256;
+  return plan_attend(tokens, q_heads, *cache, sms).total;
 }
 
 int domino_attend_paged(const void* q, int64_t q_stride, int tokens, int q_heads, const domino_kv_cache* cache,
@@ -1309,7 +1395,10 @@ int domino_attend_paged(const void* q, int64_t q_stride, int tokens, int q_heads
   rc = check_device(cache->k);
   if (rc == DOMINO_OK) rc = check_device(q);
   if (rc != DOMINO_OK) return rc;
-  if (workspace_bytes < domino_attend_workspace_bytes(tokens, q_heads, cache)) return DOMINO_ERR_INVALID_ARG;
+  int sms = 0, major = 0, minor = 0;
+  rc = device_sms(&sms, &major, &minor);
+  if (rc != DOMINO_OK) return rc;
+  if (workspace_bytes < plan_attend(tokens, q_heads, *cache, sms).total) return DOMINO_ERR_INVALID_ARG;
   dm::AttendParams a{};
   a.q = q; a.q_stride = tokens > 1 ? q_stride : 0;
   a.tokens = tokens; a.hq = q_heads; a.group = q_heads / cache->heads;
@@ -1323,10 +1412,15 @@ int domino_attend_paged(const void* q, int64_t q_stride, int tokens, int q_heads
   a.lse = lse;
   a.status = static_cast<int*>(workspace);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  if (cudaMemsetAsync(workspace, 0, sizeof(int), st) != cudaSuccess) return DOMINO_ERR_CUDA;
-  const bool vector = cache_aligned(*cache, 16) && D % static_cast<int>(16 / elem_bytes(dtype)) == 0;
+  const bool whole = cache_aligned(*cache, 16);
+  const bool tc = attend_tc_shape(*cache) && whole && aligned(q, 16) && aligned(out, 16) &&
+                  stride_aligned(q_stride, tokens, dtype, 16) && stride_aligned(out_stride, tokens, dtype, 16);
+  if (!tc && cudaMemsetAsync(workspace, 0, sizeof(int), st) != cudaSuccess) return DOMINO_ERR_CUDA;
   const int ts = timing_open(DOMINO_KERNEL_ATTEND, st);
-  rc = cuda_rc(dm::launch_attend_rows(a, dtype, vector, st));
+  if (tc)
+    rc = enqueue_attend_tc(a, *cache, sms, static_cast<uint8_t*>(workspace), st);
+  else
+    rc = cuda_rc(dm::launch_attend_rows(a, dtype, whole && D % static_cast<int>(16 / elem_bytes(dtype)) == 0, st));
   timing_close(ts, st);
   return rc;
 } catch (...) {

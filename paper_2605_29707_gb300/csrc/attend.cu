@@ -1,0 +1,807 @@
+// attend.cu -- attention of new tokens over a paged cache on the tensor cores, bf16 and fp16.
+//
+// Mathematics.  Query x of a row, keys k_j and values v_j that it sees:  s_j = x . k_j,  out = sum_j 2^(c (s_j - m)) v_j /
+// sum_j 2^(c (s_j - m)),  lse = scale m + log of that sum, with c = scale log2(e) and any m; one pass over the keys, 128 at
+// a time, with m the running maximum.
+//
+// The query heads of a group share their keys, so a tile of 128 rows holds 128 / group tokens with all of the group's heads,
+// and a group of queries (a sequence's tokens, one head of keys) has one or two tiles.  Each of two warpgroups owns an S and an
+// O accumulator in tensor memory, and keeps one row a thread: with two tiles of queries each has its own and both take
+// every tile of keys; with one, the warpgroups take the tiles of keys in turn and add up at the end.  S = X K^T runs
+// with both operands in shared memory; the weights replace S in tensor memory and are the first operand of O += W V
+// there.  While one warpgroup takes its exponentials, the tensor core works for the other.  O is scaled down only where
+// the maximum has grown by more than 2^8 since m was set: the weights stay below 2^8, whose sums fp32 holds.
+//
+// Work is the line of all (sequence, head, group of queries, tile of keys), cut into equal stretches, one a CTA (one an SM):
+// whatever the lengths, which the host does not know, no SM idles.  A stretch that begins or ends inside a group leaves its
+// unnormalised sums, maxima and masses in the workspace, two slots a CTA; a second kernel joins them in order.
+//
+// Masks only touch tiles that reach past the first key that some row does not see.  There the weights' 0 would meet
+// values nobody vouches for (places behind the last key, tokens of other branches), so in such tiles whatever is not
+// finite, or lies behind the last key, is set to 0 in shared memory, and rows that do see such a value get it added at the
+// end from the cache.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <math.h>
+
+#include <type_traits>
+
+#include "kernels.h"
+#include "paged.cuh"
+#include "ptx.cuh"
+#include "rows.cuh"
+
+namespace dm {
+namespace {
+
+constexpr int kStages = 4;          // tiles of keys or values in flight
+constexpr int kHalfBytes = 16384;   // 128 rows of 64 elements
+constexpr int kTileBytes = 2 * kHalfBytes;
+constexpr int kSoftThreads = 256;
+constexpr int kThreads = kSoftThreads + 128;  // and a warp that loads, one that multiplies, two that make up a warpgroup
+// Registers a thread: 168 at launch (384 threads share 65536); rows of 128 scores take more, the other warps less:
+// 2 x 128 x 216 + 128 x 72 = 384 x 168.
+constexpr int kSoftRegs = 216, kOtherRegs = 72;
+constexpr int kS = 0, kO = 256;     // tensor memory columns: S of warpgroup w at 128 w, O at 256 + 128 w
+constexpr float kGrowth = 8.f;      // log2 of what a maximum may grow before O is scaled
+
+struct Shared {
+  uint64_t full[kStages], empty[kStages], s_full[2], w_ready[2], o_done[2], q_ready;
+  uint32_t tmem;
+  int abort, code;
+  int odd[2];  // by the segment's parity: a value that is not finite in a masked tile
+  float norm[2][2][kAttendRows];  // warpgroup: maximum, sum
+  long long before[kAttendSeqs + 1];  // units of work before a sequence
+  Sequence seq[kAttendSeqs];
+};
+constexpr size_t kSharedBytes = 1024 + static_cast<size_t>(2 + kStages) * kTileBytes + sizeof(Shared);
+
+// D[tmem] (+)= A[tmem] * B[smem]: A's rows lie on the TMEM lanes, two 16-bit elements of K a column.
+__device__ __forceinline__ void tc_mma_f16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc,
+                                              uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem),
+      "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+
+// Each thread of the warp writes 16 / 32 consecutive 32-bit columns of its TMEM lane.
+__device__ __forceinline__ void tc_st_x16(uint32_t taddr, const float (&v)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
+      "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(taddr),
+      "r"(__float_as_uint(v[0])), "r"(__float_as_uint(v[1])), "r"(__float_as_uint(v[2])), "r"(__float_as_uint(v[3])),
+      "r"(__float_as_uint(v[4])), "r"(__float_as_uint(v[5])), "r"(__float_as_uint(v[6])), "r"(__float_as_uint(v[7])),
+      "r"(__float_as_uint(v[8])), "r"(__float_as_uint(v[9])), "r"(__float_as_uint(v[10])), "r"(__float_as_uint(v[11])),
+      "r"(__float_as_uint(v[12])), "r"(__float_as_uint(v[13])), "r"(__float_as_uint(v[14])), "r"(__float_as_uint(v[15]))
+      : "memory");
+}
+
+__device__ __forceinline__ void tc_st_x32(uint32_t taddr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+      "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,"
+      "%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(taddr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+      "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]),
+      "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]),
+      "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+      : "memory");
+}
+
+__device__ __forceinline__ void tc_wait_st() {
+  asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+}
+
+__device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+template <int N>
+__device__ __forceinline__ void regs_up() {
+  asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
+}
+template <int N>
+__device__ __forceinline__ void regs_down() {
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N));
+}
+
+__device__ __forceinline__ void fma2(float& x0, float& x1, float a, float b) {  // x = x a + b
+  asm("{\n\t.reg .b64 x, y, z;\n\t"
+      "mov.b64 x, {%0, %1};\n\tmov.b64 y, {%2, %2};\n\tmov.b64 z, {%3, %3};\n\t"
+      "fma.rn.f32x2 x, x, y, z;\n\tmov.b64 {%0, %1}, x;\n\t}"
+      : "+f"(x0), "+f"(x1)
+      : "f"(a), "f"(b));
+}
+__device__ __forceinline__ void add2(float& s0, float& s1, float x0, float x1) {
+  asm("{\n\t.reg .b64 x, y;\n\t"
+      "mov.b64 x, {%0, %1};\n\tmov.b64 y, {%2, %3};\n\t"
+      "add.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}"
+      : "+f"(s0), "+f"(s1)
+      : "f"(x0), "f"(x1));
+}
+
+__device__ __forceinline__ uint32_t pack2(float lo, float hi, __nv_bfloat16) {
+  const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ uint32_t pack2(float lo, float hi, __half) {
+  const __half2 h = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+// ---------------------------------------------------------------- the line of work
+// Keys that some token below `last` of a sequence sees, in tiles; a group that sees none still has one, for its rows'
+// zeros.
+__device__ __forceinline__ int key_tiles(int mask, const Sequence& s, int last) {
+  const long long seen = mask == kMaskCausal ? static_cast<long long>(s.kv) - s.n + last : s.kv;
+  const int k = static_cast<int>(min(max(seen, 0LL), static_cast<long long>(s.kv)));
+  return max(1, k / kAttendKeys + (k % kAttendKeys != 0));
+}
+
+struct Segment {
+  Sequence s;
+  int seq, head;
+  int tok0, tokens;    // the group's, in the sequence
+  int t0, t1, tiles;   // tiles of keys here, of all
+};
+
+struct Line {
+  long long at, end;
+  int seq, head, tok0, t;
+
+  __device__ __forceinline__ void begin(const Shared* sh, const AttendParams& p, const AttendSplit& sp, long long from,
+                                        long long to) {
+    at = from;
+    end = to;
+    if (at >= end) return;
+    int lo = 0, hi = p.batch.B;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (sh->before[mid] <= at) lo = mid; else hi = mid;
+    }
+    seq = lo;
+    const long long each = (sh->before[lo + 1] - sh->before[lo]) / p.cache.heads;
+    long long rest = at - sh->before[lo];
+    head = static_cast<int>(rest / each);
+    rest -= head * each;
+    const Sequence& s = sh->seq[seq];
+    const int step = 2 * sp.tile_tokens;
+    if (p.mask == kMaskCausal) {
+      for (tok0 = 0;; tok0 += step) {
+        const int n = key_tiles(p.mask, s, min(tok0 + step, s.n));
+        if (rest < n) break;
+        rest -= n;
+      }
+    } else {
+      const int n = key_tiles(p.mask, s, s.n);
+      tok0 = static_cast<int>(rest / n) * step;
+      rest %= n;
+    }
+    t = static_cast<int>(rest);
+  }
+
+  __device__ __forceinline__ bool next(const Shared* sh, const AttendParams& p, const AttendSplit& sp, Segment* g) {
+    if (at >= end) return false;
+    const int step = 2 * sp.tile_tokens;
+    while (sh->seq[seq].n == 0) ++seq;
+    g->s = sh->seq[seq];
+    g->seq = seq;
+    g->head = head;
+    g->tok0 = tok0;
+    g->tokens = min(step, g->s.n - tok0);
+    g->tiles = key_tiles(p.mask, g->s, tok0 + g->tokens);
+    g->t0 = t;
+    g->t1 = static_cast<int>(min(static_cast<long long>(g->tiles), t + (end - at)));
+    at += g->t1 - g->t0;
+    t = g->t1;
+    if (t == g->tiles) {
+      t = 0;
+      tok0 += step;
+      if (tok0 >= g->s.n) {
+        tok0 = 0;
+        if (++head == p.cache.heads) {
+          head = 0;
+          ++seq;
+        }
+      }
+    }
+    return true;
+  }
+};
+
+__device__ __forceinline__ long long sequence_units(const AttendParams& p, const AttendSplit& sp, const Sequence& s) {
+  const int step = 2 * sp.tile_tokens;
+  long long n = 0;
+  if (p.mask == kMaskCausal)
+    for (int t = 0; t < s.n; t += step) n += key_tiles(p.mask, s, min(t + step, s.n));
+  else
+    n = static_cast<long long>((s.n + step - 1) / step) * key_tiles(p.mask, s, s.n);
+  return n * p.cache.heads;
+}
+
+// The first key that some token from tok0 on may not see.
+__device__ __forceinline__ int masked_from(const AttendParams& p, const Sequence& s, int tok0) {
+  if (p.mask == kMaskFull) return s.kv;
+  const long long k = static_cast<long long>(s.kv) - s.n + (p.mask == kMaskCausal ? tok0 + 1 : 0);
+  return static_cast<int>(min(max(k, 0LL), static_cast<long long>(s.kv)));
+}
+
+// Which of 128 keys from key0 on token i sees, a bit each.
+__device__ __forceinline__ void seen_bits(const AttendParams& p, const Sequence& s, const int32_t* parent, int i, int key0,
+                                          uint32_t (&bits)[4]) {
+  const int first = s.kv - s.n;
+  int limit = s.kv;  // every key below it is seen
+  if (p.mask == kMaskCausal) limit = min(max(first + i + 1, 0), s.kv);
+  if (p.mask == kMaskTree) limit = i > p.N ? 0 : max(first, 0);
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const int n = limit - key0 - 32 * w;
+    bits[w] = n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1;
+  }
+  if (p.mask != kMaskTree || i > p.N) return;
+  for (int a = i;;) {
+    const int at = first + a - key0;
+    if (at < 0) break;
+    const uint32_t bit = 1u << (at & 31);
+#pragma unroll
+    for (int w = 0; w < 4; ++w)
+      if (at >> 5 == w) bits[w] |= bit;
+    if (a == 0) break;
+    a = tree_up(parent, a);
+  }
+}
+
+// A wait of its own limit for what is in flight when the others have given up.
+__device__ __forceinline__ void drain_wait(uint64_t* bar, uint32_t parity) {
+  const long long t0 = clock64();
+  while (!mbar_try_wait(bar, parity) && clock64() - t0 < kWaitCycles) {
+  }
+}
+
+// ---------------------------------------------------------------- warps
+// Tiles of a segment with n of them pass the ring as K_0 .. K_(a-1), then V_j and K_(j+a) in turn: the order in which the
+// products want them, a = 1 where both warpgroups take every tile, 2 where they alternate.
+__device__ __forceinline__ int value_place(int j, int n, int ahead) { return min(ahead, n) + j + min(j, max(0, n - ahead)); }
+
+__device__ void load_warp(Shared* sh, uint8_t* ring, const CUtensorMap* keys, const CUtensorMap* values,
+                          const AttendParams& p, const AttendSplit& sp, Line line) {
+  const int lane = threadIdx.x & 31;
+  const int halves = p.cache.D > 64 ? 2 : 1, pieces = kAttendKeys / sp.piece;
+  const bool mine = lane < pieces * halves;
+  const int piece = lane % pieces, half = lane / pieces;
+  const uint32_t offset = half * kHalfBytes + piece * sp.piece * 128;
+  const uint64_t policy = l2_policy_evict_normal();
+  unsigned it = 0;
+  Segment g;
+  bool ok = true;
+  while (ok && line.next(sh, p, sp, &g)) {
+    const bool two = g.tokens > sp.tile_tokens;
+    const int n = g.t1 - g.t0, ahead = two ? 1 : 2;
+    const int32_t* const table = p.batch.table + g.seq * p.batch.table_stride;
+    auto find = [&](int j, int* token) {  // this lane's page of tile j, past the last one where there is nothing
+      const int place = (g.t0 + j) * kAttendKeys + piece * sp.piece;
+      if (!mine || static_cast<unsigned>(place) >= static_cast<unsigned>(g.s.kv)) return p.cache.pages;
+      const int i = place / p.cache.page;
+      *token = place - i * p.cache.page;
+      const int page = table[i];
+      if (page >= 0 && page < p.cache.pages) return page;
+      sh->code = kStatusBadPage;
+      return p.cache.pages;
+    };
+    int next_k = 0, next_v = 0, token = 0, page = find(0, &token);
+    for (int c = 0; c < 2 * n; ++c, ++it) {
+      const bool value = next_k >= min(n, next_v + ahead);
+      if (value) ++next_v; else ++next_k;
+      // the page of the copy after this one is on its way while this one waits for room
+      int token_after = 0, page_after = 0;
+      if (c + 1 < 2 * n) page_after = find(next_k >= min(n, next_v + ahead) ? next_v : next_k, &token_after);
+      const int stage = it % kStages;
+      ok = it < kStages || mbar_wait(&sh->empty[stage], (it / kStages - 1) & 1, &sh->abort, &sh->code);
+      ok = __all_sync(~0u, ok);
+      if (!ok) break;
+      if (lane == 0) mbar_arrive_expect_tx(&sh->full[stage], halves * kHalfBytes);
+      __syncwarp();
+      if (mine)
+        tma_load_4d(ring + stage * kTileBytes + offset, value ? values : keys, &sh->full[stage], half * 64, token, g.head, page,
+                    policy);
+      token = token_after;
+      page = page_after;
+    }
+  }
+  if (!ok)  // nothing of ours stays in flight
+    for (unsigned i = it < kStages ? 0 : it - kStages; i < it; ++i) drain_wait(&sh->full[i % kStages], (i / kStages) & 1);
+}
+
+template <typename T>
+__device__ void multiply_thread(Shared* sh, uint32_t q_addr, uint32_t ring_addr, const AttendParams& p, const AttendSplit& sp,
+                                Line line) {
+  constexpr bool kBf = sizeof(T) == 2 && !std::is_same<T, __half>::value;
+  const int steps = (p.cache.D + 15) / 16;
+  const uint32_t tmem = sh->tmem;
+  const uint32_t qk = idesc_16_f32(kBf, kAttendRows, kAttendKeys, false), wv = idesc_16_f32(kBf, kAttendRows, 16 * steps, true);
+  unsigned it = 0, segment = 0, turns[2] = {0, 0};
+  Segment g;
+  auto take = [&]() {
+    const unsigned stage = it % kStages;
+    const bool ok = mbar_wait(&sh->full[stage], (it / kStages) & 1, &sh->abort, &sh->code);
+    ++it;
+    return ok ? static_cast<int>(stage) : -1;
+  };
+  auto scores = [&](int w, int tile, int stage) {
+    tc_fence_after();
+    const uint64_t a = smem_desc_sw128(q_addr + tile * kTileBytes), b = smem_desc_sw128(ring_addr + stage * kTileBytes);
+    for (int k = 0; k < steps; ++k) {
+      const uint64_t step = static_cast<uint64_t>((k >> 2) * (kHalfBytes >> 4) + (k & 3) * 2);
+      tc_mma_bf16(tmem + kS + 128 * w, a + step, b + step, qk, k > 0);
+    }
+    tc_commit(&sh->s_full[w]);
+  };
+  auto weigh = [&](int w, int stage, bool add) {
+    tc_fence_after();
+    const uint64_t b = smem_desc_sw128_mn(ring_addr + stage * kTileBytes, kHalfBytes);
+#pragma unroll
+    for (int k = 0; k < kAttendKeys / 16; ++k)
+      tc_mma_f16_ts(tmem + kO + 128 * w, tmem + kS + 128 * w + 8 * k, b + k * (2048 >> 4), wv, add || k > 0);
+    tc_commit(&sh->o_done[w]);
+  };
+  auto weights = [&](int w) { return mbar_wait(&sh->w_ready[w], turns[w]++ & 1, &sh->abort, &sh->code); };
+  while (line.next(sh, p, sp, &g)) {
+    if (!mbar_wait(&sh->q_ready, segment++ & 1, &sh->abort, &sh->code)) return;
+    const bool two = g.tokens > sp.tile_tokens;
+    const int n = g.t1 - g.t0;
+    if (two) {
+      int k = take();
+      if (k < 0) return;
+      scores(0, 0, k);
+      scores(1, 1, k);
+      tc_commit(&sh->empty[k]);
+      for (int j = 0; j < n; ++j) {
+        if (!weights(0)) return;
+        const int v = take();
+        if (v < 0) return;
+        weigh(0, v, j > 0);
+        if (j + 1 < n) {
+          k = take();
+          if (k < 0) return;
+          scores(0, 0, k);
+        }
+        if (!weights(1)) return;
+        weigh(1, v, j > 0);
+        tc_commit(&sh->empty[v]);
+        if (j + 1 < n) {
+          scores(1, 1, k);
+          tc_commit(&sh->empty[k]);
+        }
+      }
+    } else {
+      for (int w = 0; w < 2 && w < n; ++w) {
+        const int k = take();
+        if (k < 0) return;
+        scores(w, 0, k);
+        tc_commit(&sh->empty[k]);
+      }
+      for (int j = 0; j < n; ++j) {
+        const int w = j & 1;
+        if (!weights(w)) return;
+        const int v = take();
+        if (v < 0) return;
+        weigh(w, v, j >= 2);
+        tc_commit(&sh->empty[v]);
+        if (j + 2 < n) {
+          const int k = take();
+          if (k < 0) return;
+          scores(w, 0, k);
+          tc_commit(&sh->empty[k]);
+        }
+      }
+    }
+  }
+}
+
+// One warpgroup: queries into shared memory, a row's softmax, the end of a segment.
+template <typename T>
+__device__ void soft_group(Shared* sh, uint8_t* q_smem, uint8_t* ring, const AttendParams& p, const AttendSplit& sp, Line line) {
+  const int w = threadIdx.x >> 7, r = threadIdx.x & 127, lane_base = (threadIdx.x >> 5 & 3) * 32;
+  const int D = p.cache.D, G = p.group, steps = (D + 15) / 16;
+  const uint32_t tmem = sh->tmem + (static_cast<uint32_t>(lane_base) << 16);
+  const uint32_t s_col = tmem + kS + 128 * w, o_col = tmem + kO + 128 * w;
+  const float c = p.scale_log2;
+  const int tile_rows = sp.tile_tokens * G;
+  const int my_tok = r / G, my_head = r - my_tok * G;  // of a tile
+  unsigned segment = 0, turn = 0, base = 0;
+  Segment g;
+  for (; line.next(sh, p, sp, &g); ++segment, base += 2 * (g.t1 - g.t0)) {
+    const bool two = g.tokens > sp.tile_tokens;
+    const int n = g.t1 - g.t0, ahead = two ? 1 : 2;
+    const int tile = two ? w : 0;
+    named_bar_sync(1, kSoftThreads);  // the last segment's rows and accumulators are no longer read
+    if (threadIdx.x == 0) sh->odd[(segment + 1) & 1] = 0;
+
+    {  // queries: whole tiles of our own, or half of the one tile
+      const int rows = two ? kAttendRows : kAttendRows / 2, row0 = two ? 0 : w * rows;
+      const int units = 2 * steps;  // 16 bytes each, the last one zeros where D is not a multiple of 16
+      uint8_t* const dst = q_smem + tile * kTileBytes;
+#pragma unroll 4
+      for (int x = r; x < rows * units; x += 128) {
+        const int row = row0 + x / units, u = x % units;
+        const int tok = tile * sp.tile_tokens + row / G, h = row % G;
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (row < tile_rows && tok < g.tokens && 8 * u < D)
+          v = *reinterpret_cast<const uint4*>(static_cast<const T*>(p.q) + (g.s.row + g.tok0 + tok) * p.q_stride +
+                                              (g.head * G + h) * D + 8 * u);
+        *reinterpret_cast<uint4*>(dst + (u >> 3) * kHalfBytes + row * 128 + (((u & 7) ^ (row & 7)) << 4)) = v;
+      }
+      fence_async_smem();
+      mbar_arrive(&sh->q_ready);
+    }
+
+    const int tok = tile * sp.tile_tokens + my_tok;  // in the group
+    const bool valid = r < tile_rows && tok < g.tokens;
+    const int i = g.tok0 + tok;
+    const int32_t* const parent = p.mask == kMaskTree ? p.parent + static_cast<long long>(g.seq) * p.N : nullptr;
+    const int from = masked_from(p, g.s, g.tok0 + tile * sp.tile_tokens);
+    float m = -INFINITY, l = 0.f;
+    for (int j = two ? 0 : w; j < n; j += two ? 1 : 2, ++turn) {
+      const bool started = j >= (two ? 1 : 2);
+      const int key0 = (g.t0 + j) * kAttendKeys;
+      const bool masked = key0 + kAttendKeys > from;
+      mbar_wait(&sh->s_full[w], turn & 1, &sh->abort, &sh->code);
+      tc_fence_after();
+      float s[4][32];
+#pragma unroll
+      for (int x = 0; x < 4; ++x) tc_ld_x32(s_col + 32 * x, s[x]);
+      tc_wait_ld();
+      if (masked) {
+        uint32_t bits[4] = {0, 0, 0, 0};
+        if (valid) seen_bits(p, g.s, parent, i, key0, bits);
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+#pragma unroll
+          for (int y = 0; y < 32; ++y) s[x][y] = bits[x] >> y & 1 ? s[x][y] : -INFINITY;
+      }
+      float top[4];
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        top[x] = fmaxf(s[x][0], s[x][1]);
+#pragma unroll
+        for (int y = 2; y < 32; y += 2) top[x] = fmaxf(fmaxf(top[x], s[x][y]), s[x][y + 1]);
+      }
+      const float seen = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+      if (!started) {
+        m = seen;
+      } else {
+        const float up = fmaxf(m, seen);
+        if (__any_sync(~0u, (up - m) * c > kGrowth)) {
+          const float keep = m == up ? 1.f : ex2((m - up) * c);
+          mbar_wait(&sh->o_done[w], (turn - 1) & 1, &sh->abort, &sh->code);
+          tc_fence_after();
+          for (int d = 0; d < steps; ++d) {
+            float o[16];
+            tc_ld_x16(o_col + 16 * d, o);
+            tc_wait_ld();
+#pragma unroll
+            for (int x = 0; x < 16; ++x) o[x] *= keep;
+            tc_st_x16(o_col + 16 * d, o);
+          }
+          l *= keep;
+          m = up;
+        }
+      }
+      const float mc = m == -INFINITY ? 0.f : -m * c;
+      float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int x = 0; x < 4; x += 2) {
+        uint32_t pk[32];
+#pragma unroll
+        for (int y = 0; y < 64; y += 2) {
+          float a = s[x + y / 32][y % 32], b = s[x + y / 32][y % 32 + 1];
+          fma2(a, b, c, mc);
+          a = ex2(a);
+          b = ex2(b);
+          add2(sum[y & 2], sum[(y & 2) + 1], a, b);
+          pk[y / 2] = pack2(a, b, T());
+        }
+        tc_st_x32(s_col + 16 * x, pk);
+      }
+      l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+      if (masked) {  // values that weights of 0 must not meet
+        const unsigned place = base + value_place(j, n, ahead);
+        const int stage = place % kStages, key = key0 + r;
+        mbar_wait(&sh->full[stage], (place / kStages) & 1, &sh->abort, &sh->code);
+        if (key >= from) {
+          uint8_t* const row = ring + stage * kTileBytes + r * 128;
+          for (int u = 0; u < 2 * steps; ++u) {
+            uint4* const at = reinterpret_cast<uint4*>(row + (u >> 3) * kHalfBytes + (((u & 7) ^ (r & 7)) << 4));
+            if (key >= g.s.kv) {
+              *at = make_uint4(0, 0, 0, 0);
+            } else {
+              Vec<T> v;
+              v.raw = *at;
+              float f[8];
+              unpack(v, f);
+              bool odd = false;
+#pragma unroll
+              for (int x = 0; x < 8; ++x) odd = odd || !isfinite(f[x]);
+              if (odd) {
+                *reinterpret_cast<volatile int*>(&sh->odd[segment & 1]) = 1;
+                __threadfence_block();
+#pragma unroll
+                for (int x = 0; x < 8; ++x) f[x] = isfinite(f[x]) ? f[x] : 0.f;
+                pack(f, &v);
+                *at = v.raw;
+              }
+            }
+          }
+        }
+        fence_async_smem();
+      }
+      tc_wait_st();
+      tc_fence_before();
+      mbar_arrive(&sh->w_ready[w]);
+    }
+
+    // the segment's end: sums into the output, or into the workspace where the group's keys go on elsewhere
+    const bool any = n > (two ? 0 : w);
+    if (any) mbar_wait(&sh->o_done[w], (turn - 1) & 1, &sh->abort, &sh->code);
+    tc_fence_after();
+    float f0 = 1.f, f1 = 0.f;  // one tile of queries: the warpgroups' weights
+    if (!two) {
+      sh->norm[w][0][r] = m;
+      sh->norm[w][1][r] = l;
+      tc_fence_before();
+      named_bar_sync(1, kSoftThreads);
+      tc_fence_after();
+      const float m0 = sh->norm[0][0][r], m1 = sh->norm[1][0][r];
+      m = fmaxf(m0, m1);
+      f0 = m0 == -INFINITY ? 0.f : m0 == m ? 1.f : ex2((m0 - m) * c);
+      f1 = m1 == -INFINITY ? 0.f : m1 == m ? 1.f : ex2((m1 - m) * c);
+      l = sh->norm[0][1][r] * f0 + sh->norm[1][1][r] * f1;
+    }
+    const bool odd = *reinterpret_cast<volatile int*>(&sh->odd[segment & 1]) != 0;
+    const bool whole = g.t0 == 0 && g.t1 == g.tiles;
+    const long long row = g.s.row + i;
+    const int head = g.head * G + my_head;
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const int slot = 2 * blockIdx.x + (g.t0 == 0 ? 1 : 0), slot_row = tile * kAttendRows + r;
+    for (int d = two ? 0 : w; d < steps; d += two ? 1 : 2) {
+      float o[16];
+      if (two) {
+        tc_ld_x16(o_col + 16 * d, o);
+        tc_wait_ld();
+      } else {
+        float o1[16];
+        tc_ld_x16(tmem + kO + 16 * d, o);
+        tc_ld_x16(tmem + kO + 128 + 16 * d, o1);
+        tc_wait_ld();
+#pragma unroll
+        for (int x = 0; x < 16; ++x) o[x] = (f0 == 0.f ? 0.f : o[x] * f0) + (f1 == 0.f ? 0.f : o1[x] * f1);
+      }
+      if (!valid) continue;
+      if (odd) {  // what was left out of the products, where this row sees it
+        const int end = min(g.s.kv, g.t1 * kAttendKeys);
+        for (int key = max(masked_from(p, g.s, g.tok0), g.t0 * kAttendKeys); key < end; ++key) {
+          if (!sees(p.mask, parent, p.N, i, static_cast<long long>(g.s.kv) - g.s.n, key)) continue;
+          const long long off = place_offset(p.cache, p.batch, g.seq, key);
+          if (off < 0) continue;
+          const T* const v = static_cast<const T*>(p.cache.v) + off + g.head * p.cache.head_stride;
+#pragma unroll
+          for (int x = 0; x < 16; ++x) {
+            if (16 * d + x >= D) break;
+            const float f = to_f32(v[16 * d + x]);
+            if (!isfinite(f)) o[x] += f;
+          }
+        }
+      }
+      if (whole) {
+        T* const out = static_cast<T*>(p.out) + row * p.out_stride + static_cast<long long>(head) * D + 16 * d;
+#pragma unroll
+        for (int x = 0; x < 16; x += 8) {
+          if (16 * d + x >= D) break;
+          float y[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) y[e] = l == 0.f ? 0.f : o[x + e] * inv;
+          Vec<T> v;
+          pack(y, &v);
+          *reinterpret_cast<uint4*>(out + x) = v.raw;
+        }
+      } else {
+        float* const part = sp.parts + (static_cast<long long>(slot) * D + 16 * d) * sp.slot_rows + slot_row;
+#pragma unroll
+        for (int x = 0; x < 16; ++x)
+          if (16 * d + x < D) part[static_cast<long long>(x) * sp.slot_rows] = o[x];
+      }
+    }
+    if (valid && (two || w == 0)) {
+      if (!whole) {
+        float* const norm = sp.norms + static_cast<long long>(slot) * 2 * sp.slot_rows + slot_row;
+        norm[0] = m;
+        norm[sp.slot_rows] = l;
+      } else if (p.lse) {
+        p.lse[row * p.hq + head] = l == 0.f ? -INFINITY : fmaf(m, p.scale, logf(l));
+      }
+    }
+    tc_fence_before();
+  }
+}
+
+__device__ __forceinline__ long long stretch(long long units, int ctas) { return (units + ctas - 1) / ctas; }
+
+template <typename T>
+__global__ void __launch_bounds__(kThreads, 1)
+    attend_kernel(const __grid_constant__ CUtensorMap keys, const __grid_constant__ CUtensorMap values, const AttendParams p,
+                  const AttendSplit sp) {
+  extern __shared__ uint8_t raw[];
+  uint8_t* const tiles = raw + ((1024 - (smem_u32(raw) & 1023)) & 1023);  // queries, then the ring
+  uint8_t* const ring = tiles + 2 * kTileBytes;
+  Shared* const sh = reinterpret_cast<Shared*>(ring + kStages * kTileBytes);
+  const int tid = threadIdx.x, warp = tid >> 5;
+  if (tid == 0) {
+    for (int i = 0; i < kStages; ++i) {
+      mbar_init(&sh->full[i], 1);
+      mbar_init(&sh->empty[i], 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&sh->s_full[i], 1);
+      mbar_init(&sh->w_ready[i], 128);
+      mbar_init(&sh->o_done[i], 1);
+      sh->odd[i] = 0;
+    }
+    mbar_init(&sh->q_ready, kSoftThreads);
+    fence_mbar_init();
+    sh->abort = 0;
+    sh->code = 0;
+    tma_prefetch_desc(&keys);
+    tma_prefetch_desc(&values);
+  }
+  if (warp == kSoftThreads / 32) {
+    tmem_alloc(&sh->tmem, 512);
+    tmem_relinquish();
+  }
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  for (int b = tid; b < p.batch.B; b += kThreads) {
+    const Sequence s = load_sequence(p.cache, p.batch, p.tokens, b);
+    sh->seq[b] = s;
+    sh->before[b + 1] = sequence_units(p, sp, s);
+  }
+  if (tid == 0) sh->before[0] = 0;
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (warp == 0) {
+    long long carry = 0;
+    for (int b = 0; b < p.batch.B; b += 32) {
+      long long x = b + tid < p.batch.B ? sh->before[b + tid + 1] : 0;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const long long y = __shfl_up_sync(~0u, x, o);
+        if (tid >= o) x += y;
+      }
+      x += carry;
+      if (b + tid < p.batch.B) sh->before[b + tid + 1] = x;
+      carry = __shfl_sync(~0u, x, 31);
+    }
+  }
+  __syncthreads();
+  const long long units = sh->before[p.batch.B], each = stretch(units, gridDim.x);
+  Line line;
+  line.begin(sh, p, sp, min(units, blockIdx.x * each), min(units, (blockIdx.x + 1) * each));
+  if (tid < kSoftThreads) {
+    regs_up<kSoftRegs>();
+    soft_group<T>(sh, tiles, ring, p, sp, line);
+  } else {
+    regs_down<kOtherRegs>();
+    if (warp == kSoftThreads / 32) load_warp(sh, ring, &keys, &values, p, sp, line);
+    if (tid == kSoftThreads + 32) {
+      multiply_thread<T>(sh, smem_u32(tiles), smem_u32(ring), p, sp, line);
+      // the last group of this stretch that goes on: where, for the kernel that joins
+      AttendTail tail{-1, 0, 0, 0};
+      Segment g;
+      while (line.next(sh, p, sp, &g))
+        if (g.t0 == 0 && g.t1 < g.tiles)
+          tail = AttendTail{static_cast<int>((line.at + g.tiles - g.t1 - 1) / each), g.s.row + g.tok0, g.head, g.tokens};
+      sp.tails[blockIdx.x] = tail;
+      if (sh->abort) {  // products in flight read the tiles and write the accumulators: they take microseconds
+        const long long t0 = clock64();
+        while (clock64() - t0 < kWaitCycles / 1024) {
+        }
+      }
+    }
+  }
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  if (tid == 0) sp.codes[blockIdx.x] = sh->code;
+  if (warp == kSoftThreads / 32) {
+    tc_fence_after();
+    tmem_dealloc(sh->tmem, 512);
+  }
+}
+
+// ---------------------------------------------------------------- joining
+constexpr int kJoinThreads = 256;
+
+// The group that CTA blockIdx.x began and others went on with: its rows' sums over all of them, in their order.  A thread
+// takes eight elements of a row; rows lie side by side in the slots.
+template <typename T>
+__global__ void __launch_bounds__(kJoinThreads) join_kernel(const AttendParams p, const AttendSplit sp) {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x < 32) {
+    int code = 0;
+    for (unsigned i = threadIdx.x; i < gridDim.x; i += 32) {
+      const int x = sp.codes[i];
+      code = x != 0 ? x : code;
+    }
+    const unsigned bad = __ballot_sync(~0u, code != 0);
+    if (bad) code = __shfl_sync(~0u, code, __ffs(bad) - 1);
+    if (threadIdx.x == 0 && (sp.first || code != 0)) *p.status = code;
+  }
+  const AttendTail tail = sp.tails[blockIdx.x];
+  if (tail.last < 0) return;
+  const int D = p.cache.D, G = p.group, rows = tail.tokens * G, octets = D / 8, first = blockIdx.x;
+  const long long slot_rows = sp.slot_rows;
+  for (int x = blockIdx.y * kJoinThreads + threadIdx.x; x < rows * octets; x += gridDim.y * kJoinThreads) {
+    const int oct = x / rows, at = x - oct * rows, tok = at / G, h = at - tok * G;
+    const int slot_row = tok < sp.tile_tokens ? at : kAttendRows + at - sp.tile_tokens * G;
+    auto slot = [&](int i) { return static_cast<long long>(i == first ? 2 * i + 1 : 2 * i); };
+    float m = -INFINITY;
+#pragma unroll 4
+    for (int i = first; i <= tail.last; ++i) m = fmaxf(m, sp.norms[slot(i) * 2 * slot_rows + slot_row]);
+    float l = 0.f, o[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) o[e] = 0.f;
+#pragma unroll 4
+    for (int i = first; i <= tail.last; ++i) {
+      const float* const norm = sp.norms + slot(i) * 2 * slot_rows + slot_row;
+      const float* const part = sp.parts + (slot(i) * D + 8 * oct) * slot_rows + slot_row;
+      const float mi = norm[0];
+      const float f = mi == -INFINITY ? 0.f : mi == m ? 1.f : ex2((mi - m) * p.scale_log2);
+      l = fmaf(norm[slot_rows], f, l);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) o[e] = fmaf(part[e * slot_rows], f, o[e]);
+    }
+    const long long row = tail.row + tok;
+    const int head = tail.head * G + h;
+    const float inv = 1.f / l;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) o[e] = l == 0.f ? 0.f : o[e] * inv;
+    Vec<T> v;
+    pack(o, &v);
+    *reinterpret_cast<uint4*>(static_cast<T*>(p.out) + row * p.out_stride + static_cast<long long>(head) * D + 8 * oct) = v.raw;
+    if (p.lse && oct == 0) p.lse[row * p.hq + head] = l == 0.f ? -INFINITY : fmaf(m, p.scale, logf(l));
+  }
+}
+
+template <typename T>
+cudaError_t launch_tc_type(const CUtensorMap& keys, const CUtensorMap& values, const AttendParams& p, const AttendSplit& s,
+                           int grid, cudaStream_t stream) {
+  cudaError_t e = ensure_smem_attr(reinterpret_cast<const void*>(&attend_kernel<T>), kSharedBytes, false);
+  if (e != cudaSuccess) return e;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(grid);
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = kSharedBytes;
+  cfg.stream = stream;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  e = cudaLaunchKernelEx(&cfg, attend_kernel<T>, keys, values, p, s);
+  if (e != cudaSuccess) return e;
+  cfg.gridDim = dim3(grid, s.slot_rows > kAttendRows ? 8 : 1);
+  cfg.blockDim = dim3(kJoinThreads);
+  cfg.dynamicSmemBytes = 0;
+  return cudaLaunchKernelEx(&cfg, join_kernel<T>, p, s);
+}
+
+}  // namespace
+
+cudaError_t launch_attend_tc(const CUtensorMap& keys, const CUtensorMap& values, const AttendParams& p,
+                             const AttendSplit& s, int dtype, int grid, cudaStream_t stream) {
+  if (dtype == kBf16) return launch_tc_type<__nv_bfloat16>(keys, values, p, s, grid, stream);
+  return launch_tc_type<__half>(keys, values, p, s, grid, stream);
+}
+
+}  // namespace dm

@@ -16,21 +16,6 @@ namespace {
 constexpr int kRowWarps = 4;
 constexpr int kLaneElems = kMaxHeadDim / 32;
 
-// Whether token i of a sequence (keys of new tokens from `first` on) sees the key at `place`, below its kv.
-__device__ __forceinline__ bool sees(const AttendParams& p, const int32_t* parent, int i, long long first, int place) {
-  if (p.mask == kMaskFull) return true;
-  const long long t = place - first;  // the key's new token, or negative
-  if (p.mask == kMaskCausal) return t <= i;
-  if (i > p.N) return false;
-  if (t < 0) return true;
-  int a = i;
-  while (a > t && a > 0) {
-    const int up = parent[a - 1];
-    a = (up < -1 || up >= a - 1 ? -1 : up) + 1;  // a parent is an earlier node
-  }
-  return a == t;
-}
-
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(32 * kRowWarps) attend_rows_kernel(const AttendParams p) {
   __shared__ float s_q[kRowWarps][kMaxHeadDim];
@@ -61,7 +46,7 @@ __global__ void __launch_bounds__(32 * kRowWarps) attend_rows_kernel(const Atten
   for (long long j0 = 0; j0 < end; j0 += 32) {
     const int j = static_cast<int>(j0) + lane;
     long long off = -1;
-    if (j0 + lane < end && sees(p, parent, i, first, j)) {
+    if (j0 + lane < end && sees(p.mask, parent, p.N, i, first, j)) {
       const int pi = j / c.page, pg = table[pi];
       if (pg >= 0 && pg < c.pages) off = pg * c.page_stride + (j - pi * c.page) * c.token_stride;
       else set_status(p.status, kStatusBadPage);

@@ -369,6 +369,28 @@ struct AttendParams {
   float* lse;   // [tokens][hq] or nullptr
   int* status;  // the workspace's first word
 };
+// bf16 and fp16 on the tensor cores (D <= 128 and page multiples of 8, everything on 16-byte boundaries).
+constexpr int kAttendKeys = 128;   // keys a tile
+constexpr int kAttendRows = 128;   // queries a tile
+constexpr int kAttendSeqs = 1024;  // sequences a launch
+struct AttendTail {  // a group of queries whose keys go on behind the CTA that began them
+  int last;          // the CTA that ends them, -1: none
+  int row, head, tokens;
+};
+struct AttendSplit {
+  int piece;       // keys of a copy: the greatest power of two up to 128 that divides the page
+  int tile_tokens; // tokens of a tile of queries: 128 / group
+  int slot_rows;   // rows of a partial result
+  int first;       // the call's first launch: later ones keep an earlier error
+  int* codes;         // [grid] a CTA's status
+  AttendTail* tails;  // [grid]
+  float* norms;       // [2 grid][2][slot_rows] maximum and sum
+  float* parts;       // [2 grid][D][slot_rows]
+};
+// keys, values: tensor maps (element, token, head, page) with boxes of 64 elements and `piece` tokens.
+cudaError_t launch_attend_tc(const CUtensorMap& keys, const CUtensorMap& values, const AttendParams& p,
+                             const AttendSplit& s, int dtype, int grid, cudaStream_t stream);
+
 // Any type and layout: a warp a row.  Status already cleared.
 cudaError_t launch_attend_rows(const AttendParams& p, int dtype, bool vector, cudaStream_t stream);
 

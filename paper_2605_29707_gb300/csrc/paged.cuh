@@ -5,10 +5,10 @@
 
 namespace dm {
 
-// The places that the table holds, in int range.
+// The places that the table holds, cut off a tile below 2^31.
 __device__ __forceinline__ int table_places(const PagedCache& c, const PagedBatch& b) {
   const long long n = static_cast<long long>(b.table_width) * c.page;
-  return n > 0x7fffffffLL ? 0x7fffffff : static_cast<int>(n);
+  return n > 0x7fffff80LL ? 0x7fffff80 : static_cast<int>(n);
 }
 
 struct Sequence {
@@ -44,6 +44,24 @@ __device__ __forceinline__ long long place_offset(const PagedCache& c, const Pag
   const int i = place / c.page, pg = b.table[seq * b.table_stride + i];
   if (pg < 0 || pg >= c.pages) return -1;
   return pg * c.page_stride + (place - i * c.page) * c.token_stride;
+}
+
+// The token that token a > 0 of a sequence follows in its tree (parents given by node: token a is node a - 1).
+__device__ __forceinline__ int tree_up(const int32_t* parent, int a) {
+  const int up = parent[a - 1];
+  return up < -1 || up >= a - 1 ? 0 : up + 1;  // a parent is an earlier node, or the anchor
+}
+
+// Whether token i of a sequence (keys of new tokens from `first` on) sees the key at `place`, below its kv.
+__device__ __forceinline__ bool sees(int mask, const int32_t* parent, int N, int i, long long first, int place) {
+  if (mask == kMaskFull) return true;
+  const long long t = place - first;  // the key's new token, or negative
+  if (mask == kMaskCausal) return t <= i;
+  if (i > N) return false;
+  if (t < 0) return true;
+  int a = i;
+  while (a > t && a > 0) a = tree_up(parent, a);
+  return a == t;
 }
 
 }  // namespace dm
