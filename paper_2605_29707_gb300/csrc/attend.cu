@@ -24,6 +24,7 @@
 #include <cuda_fp16.h>
 #include <math.h>
 
+#include <algorithm>
 #include <type_traits>
 
 #include "kernels.h"
@@ -43,6 +44,7 @@ constexpr int kThreads = kSoftThreads + 128;  // and a warp that loads, one that
 // 2 x 128 x 216 + 128 x 72 = 384 x 168.
 constexpr int kSoftRegs = 216, kOtherRegs = 72;
 constexpr int kS = 0, kO = 256;     // tensor memory columns: S of warpgroup w at 128 w, O at 256 + 128 w
+constexpr int kGroupCost = 3;       // what a group's queries and its end cost, in tiles of keys
 constexpr float kGrowth = 8.f;      // log2 of what a maximum may grow before O is scaled
 
 struct Shared {
@@ -56,15 +58,40 @@ struct Shared {
 };
 constexpr size_t kSharedBytes = 1024 + static_cast<size_t>(2 + kStages) * kTileBytes + sizeof(Shared);
 
-// D[tmem] (+)= A[tmem] * B[smem]: A's rows lie on the TMEM lanes, two 16-bit elements of K a column.
-__device__ __forceinline__ void tc_mma_f16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc,
-                                              uint32_t accumulate) {
+// Descriptors of 128-byte swizzled tiles differ in their low word alone (start address and, MN-major, the distance of
+// blocks): 32-bit sums step them.
+constexpr uint32_t kDescHigh = (1024 >> 4) | (1u << 14) | (2u << 29);
+__device__ __forceinline__ uint32_t desc_low(uint32_t addr, uint32_t block) {
+  return ((addr & 0x3FFFFu) >> 4) | ((block >> 4) << 16);
+}
+
+// D[tmem] (+)= A[smem] B[smem]^T, and D[tmem] (+)= A[tmem] B[smem], 16-bit operands, by their low words.
+__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t add) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t.reg .b64 x, y;\n\t"
+      "mov.b64 x, {%1, %5};\n\tmov.b64 y, {%2, %5};\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %3, p;\n\t}" ::"r"(d),
+      "r"(a), "r"(b), "r"(idesc), "r"(add), "n"(kDescHigh)
+      : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t add) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t.reg .b64 y;\n\t"
+      "mov.b64 y, {%2, %5};\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], y, %3, p;\n\t}" ::"r"(d),
+      "r"(a), "r"(b), "r"(idesc), "r"(add), "n"(kDescHigh)
+      : "memory");
+}
+__device__ __forceinline__ bool elect_one() {
+  uint32_t yes;
   asm volatile(
       "{\n\t.reg .pred p;\n\t"
-      "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem),
-      "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
-      : "memory");
+      "elect.sync _|p, 0xffffffff;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(yes));
+  return yes != 0;
 }
 
 // Each thread of the warp writes 16 / 32 consecutive 32-bit columns of its TMEM lane.
@@ -146,9 +173,15 @@ struct Segment {
   int t0, t1, tiles;   // tiles of keys here, of all
 };
 
+__device__ __forceinline__ long long quotient(long long a, long long b) {
+  if (((a | b) >> 32) == 0) return static_cast<unsigned>(a) / static_cast<unsigned>(b);
+  return a / b;
+}
+
+// A CTA's stretch of the line.  A group of queries counts kGroupCost units and one a tile of keys.
 struct Line {
   long long at, end;
-  int seq, head, tok0, t;
+  int seq, head, tok0, t;  // t: the tile at `at`, negative in the units before the first
 
   __device__ __forceinline__ void begin(const Shared* sh, const AttendParams& p, const AttendSplit& sp, long long from,
                                         long long to) {
@@ -161,63 +194,79 @@ struct Line {
       if (sh->before[mid] <= at) lo = mid; else hi = mid;
     }
     seq = lo;
-    const long long each = (sh->before[lo + 1] - sh->before[lo]) / p.cache.heads;
+    const long long each = quotient(sh->before[lo + 1] - sh->before[lo], p.cache.heads);
     long long rest = at - sh->before[lo];
-    head = static_cast<int>(rest / each);
+    head = static_cast<int>(quotient(rest, each));
     rest -= head * each;
-    const Sequence& s = sh->seq[seq];
-    const int step = 2 * sp.tile_tokens;
+    const Sequence s = sh->seq[seq];
+    const int step = 2 * sp.tile_tokens, groups = (s.n + step - 1) / step;
+    int g = 0;
     if (p.mask == kMaskCausal) {
-      for (tok0 = 0;; tok0 += step) {
-        const int n = key_tiles(p.mask, s, min(tok0 + step, s.n));
-        if (rest < n) break;
-        rest -= n;
+      if (groups > 1) {  // every lane of the warp adds up a part of them; the one where `rest` lies goes through its own
+        const int lane = threadIdx.x & 31, share = (groups + 31) / 32;
+        const int mine = min(groups, lane * share), stop = min(groups, mine + share);
+        long long sum = 0;
+        for (int i = mine; i < stop; ++i) sum += kGroupCost + key_tiles(p.mask, s, min((i + 1) * step, s.n));
+        long long upto = sum;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const long long y = __shfl_up_sync(~0u, upto, o);
+          if (lane >= o) upto += y;
+        }
+        const int owner = __ffs(__ballot_sync(~0u, rest < upto)) - 1;
+        rest -= __shfl_sync(~0u, upto - sum, owner);
+        for (g = owner * share;; ++g) {
+          const int n = kGroupCost + key_tiles(p.mask, s, min((g + 1) * step, s.n));
+          if (rest < n) break;
+          rest -= n;
+        }
       }
     } else {
-      const int n = key_tiles(p.mask, s, s.n);
-      tok0 = static_cast<int>(rest / n) * step;
-      rest %= n;
+      const int n = kGroupCost + key_tiles(p.mask, s, s.n);
+      g = static_cast<int>(quotient(rest, n));
+      rest -= static_cast<long long>(g) * n;
     }
-    t = static_cast<int>(rest);
+    tok0 = g * step;
+    t = static_cast<int>(rest) - kGroupCost;
   }
 
   __device__ __forceinline__ bool next(const Shared* sh, const AttendParams& p, const AttendSplit& sp, Segment* g) {
-    if (at >= end) return false;
     const int step = 2 * sp.tile_tokens;
-    while (sh->seq[seq].n == 0) ++seq;
-    g->s = sh->seq[seq];
-    g->seq = seq;
-    g->head = head;
-    g->tok0 = tok0;
-    g->tokens = min(step, g->s.n - tok0);
-    g->tiles = key_tiles(p.mask, g->s, tok0 + g->tokens);
-    g->t0 = t;
-    g->t1 = static_cast<int>(min(static_cast<long long>(g->tiles), t + (end - at)));
-    at += g->t1 - g->t0;
-    t = g->t1;
-    if (t == g->tiles) {
-      t = 0;
-      tok0 += step;
-      if (tok0 >= g->s.n) {
-        tok0 = 0;
-        if (++head == p.cache.heads) {
-          head = 0;
-          ++seq;
+    while (at < end) {
+      while (sh->seq[seq].n == 0) ++seq;
+      g->s = sh->seq[seq];
+      g->seq = seq;
+      g->head = head;
+      g->tok0 = tok0;
+      g->tokens = min(step, g->s.n - tok0);
+      g->tiles = key_tiles(p.mask, g->s, tok0 + g->tokens);
+      const int n = static_cast<int>(min(static_cast<long long>(g->tiles) - t, end - at));
+      g->t0 = max(t, 0);
+      at += n;
+      t += n;
+      g->t1 = t;
+      if (t == g->tiles) {
+        t = -kGroupCost;
+        tok0 += step;
+        if (tok0 >= g->s.n) {
+          tok0 = 0;
+          if (++head == p.cache.heads) {
+            head = 0;
+            ++seq;
+          }
         }
       }
+      if (g->t1 > g->t0) return true;
     }
-    return true;
+    return false;
   }
 };
 
+// A sequence's units; -1 where a causal one has several groups, each of its own length.
 __device__ __forceinline__ long long sequence_units(const AttendParams& p, const AttendSplit& sp, const Sequence& s) {
-  const int step = 2 * sp.tile_tokens;
-  long long n = 0;
-  if (p.mask == kMaskCausal)
-    for (int t = 0; t < s.n; t += step) n += key_tiles(p.mask, s, min(t + step, s.n));
-  else
-    n = static_cast<long long>((s.n + step - 1) / step) * key_tiles(p.mask, s, s.n);
-  return n * p.cache.heads;
+  const int groups = (s.n + 2 * sp.tile_tokens - 1) / (2 * sp.tile_tokens);
+  if (p.mask == kMaskCausal && groups > 1) return -1;
+  return static_cast<long long>(groups) * (kGroupCost + key_tiles(p.mask, s, s.n)) * p.cache.heads;
 }
 
 // The first key that some token from tok0 on may not see.
@@ -313,10 +362,11 @@ __device__ void load_warp(Shared* sh, uint8_t* ring, const CUtensorMap* keys, co
     for (unsigned i = it < kStages ? 0 : it - kStages; i < it; ++i) drain_wait(&sh->full[i % kStages], (i / kStages) & 1);
 }
 
+// The whole warp walks the line, one thread issues: what steers the products stays in uniform registers.
 template <typename T>
-__device__ void multiply_thread(Shared* sh, uint32_t q_addr, uint32_t ring_addr, const AttendParams& p, const AttendSplit& sp,
-                                Line line) {
-  constexpr bool kBf = sizeof(T) == 2 && !std::is_same<T, __half>::value;
+__device__ void multiply_warp(Shared* sh, uint32_t q_addr, uint32_t ring_addr, const AttendParams& p, const AttendSplit& sp,
+                              Line line) {
+  constexpr bool kBf = !std::is_same<T, __half>::value;
   const int steps = (p.cache.D + 15) / 16;
   const uint32_t tmem = sh->tmem;
   const uint32_t qk = idesc_16_f32(kBf, kAttendRows, kAttendKeys, false), wv = idesc_16_f32(kBf, kAttendRows, 16 * steps, true);
@@ -326,77 +376,87 @@ __device__ void multiply_thread(Shared* sh, uint32_t q_addr, uint32_t ring_addr,
     const unsigned stage = it % kStages;
     const bool ok = mbar_wait(&sh->full[stage], (it / kStages) & 1, &sh->abort, &sh->code);
     ++it;
-    return ok ? static_cast<int>(stage) : -1;
+    return __all_sync(~0u, ok) ? static_cast<int>(stage) : -1;
   };
-  auto scores = [&](int w, int tile, int stage) {
+  // S of warpgroup w from query tile `tile` and the keys in `stage`; last: nobody else wants them
+  auto scores = [&](int w, int tile, int stage, bool last) {
     tc_fence_after();
-    const uint64_t a = smem_desc_sw128(q_addr + tile * kTileBytes), b = smem_desc_sw128(ring_addr + stage * kTileBytes);
-    for (int k = 0; k < steps; ++k) {
-      const uint64_t step = static_cast<uint64_t>((k >> 2) * (kHalfBytes >> 4) + (k & 3) * 2);
-      tc_mma_bf16(tmem + kS + 128 * w, a + step, b + step, qk, k > 0);
-    }
-    tc_commit(&sh->s_full[w]);
-  };
-  auto weigh = [&](int w, int stage, bool add) {
-    tc_fence_after();
-    const uint64_t b = smem_desc_sw128_mn(ring_addr + stage * kTileBytes, kHalfBytes);
+    const uint32_t a = desc_low(q_addr + tile * kTileBytes, 16), b = desc_low(ring_addr + stage * kTileBytes, 16);
+    if (elect_one()) {
 #pragma unroll
-    for (int k = 0; k < kAttendKeys / 16; ++k)
-      tc_mma_f16_ts(tmem + kO + 128 * w, tmem + kS + 128 * w + 8 * k, b + k * (2048 >> 4), wv, add || k > 0);
-    tc_commit(&sh->o_done[w]);
+      for (int k = 0; k < 8; ++k) {
+        const uint32_t step = (k >> 2) * (kHalfBytes >> 4) + (k & 3) * 2;
+        if (k < steps) mma_ss(tmem + kS + 128 * w, a + step, b + step, qk, k > 0);
+      }
+      tc_commit(&sh->s_full[w]);
+      if (last) tc_commit(&sh->empty[stage]);
+    }
+    __syncwarp();
   };
-  auto weights = [&](int w) { return mbar_wait(&sh->w_ready[w], turns[w]++ & 1, &sh->abort, &sh->code); };
+  // O of warpgroup w, from its weights and the values in `stage`
+  auto weigh = [&](int w, int stage, bool add, bool last) {
+    tc_fence_after();
+    const uint32_t b = desc_low(ring_addr + stage * kTileBytes, kHalfBytes);
+    if (elect_one()) {
+#pragma unroll
+      for (int k = 0; k < kAttendKeys / 16; ++k)
+        mma_ts(tmem + kO + 128 * w, tmem + kS + 128 * w + 8 * k, b + k * (2048 >> 4), wv, k > 0 ? 1 : add);
+      tc_commit(&sh->o_done[w]);
+      if (last) tc_commit(&sh->empty[stage]);
+    }
+    __syncwarp();
+  };
+  auto weights = [&](int w) {
+    return __all_sync(~0u, mbar_wait(&sh->w_ready[w], turns[w]++ & 1, &sh->abort, &sh->code));
+  };
   while (line.next(sh, p, sp, &g)) {
-    if (!mbar_wait(&sh->q_ready, segment++ & 1, &sh->abort, &sh->code)) return;
+    if (!__all_sync(~0u, mbar_wait(&sh->q_ready, segment++ & 1, &sh->abort, &sh->code))) return;
     const bool two = g.tokens > sp.tile_tokens;
     const int n = g.t1 - g.t0;
     if (two) {
       int k = take();
       if (k < 0) return;
-      scores(0, 0, k);
-      scores(1, 1, k);
-      tc_commit(&sh->empty[k]);
+      scores(0, 0, k, false);
+      scores(1, 1, k, true);
       for (int j = 0; j < n; ++j) {
         if (!weights(0)) return;
         const int v = take();
         if (v < 0) return;
-        weigh(0, v, j > 0);
+        weigh(0, v, j > 0, false);
         if (j + 1 < n) {
           k = take();
           if (k < 0) return;
-          scores(0, 0, k);
+          scores(0, 0, k, false);
         }
         if (!weights(1)) return;
-        weigh(1, v, j > 0);
-        tc_commit(&sh->empty[v]);
-        if (j + 1 < n) {
-          scores(1, 1, k);
-          tc_commit(&sh->empty[k]);
-        }
+        weigh(1, v, j > 0, true);
+        if (j + 1 < n) scores(1, 1, k, true);
       }
     } else {
       for (int w = 0; w < 2 && w < n; ++w) {
         const int k = take();
         if (k < 0) return;
-        scores(w, 0, k);
-        tc_commit(&sh->empty[k]);
+        scores(w, 0, k, true);
       }
       for (int j = 0; j < n; ++j) {
         const int w = j & 1;
         if (!weights(w)) return;
         const int v = take();
         if (v < 0) return;
-        weigh(w, v, j >= 2);
-        tc_commit(&sh->empty[v]);
+        weigh(w, v, j >= 2, true);
         if (j + 2 < n) {
           const int k = take();
           if (k < 0) return;
-          scores(w, 0, k);
-          tc_commit(&sh->empty[k]);
+          scores(w, 0, k, true);
         }
       }
     }
   }
+}
+
+// Byte offset of a row's 16-byte unit in a 128-byte swizzled tile.
+__device__ __forceinline__ uint32_t unit_offset(int row, int unit) {
+  return (unit >> 3) * kHalfBytes + row * 128 + (((unit & 7) ^ (row & 7)) << 4);
 }
 
 // One warpgroup: queries into shared memory, a row's softmax, the end of a segment.
@@ -409,6 +469,8 @@ __device__ void soft_group(Shared* sh, uint8_t* q_smem, uint8_t* ring, const Att
   const float c = p.scale_log2;
   const int tile_rows = sp.tile_tokens * G;
   const int my_tok = r / G, my_head = r - my_tok * G;  // of a tile
+  const int inv_group = (65536 + G - 1) / G;             // row / G for rows below 128
+  const int units = 2 * steps, row_step = 128 / units, unit_row = r / units, unit = r - unit_row * units;
   unsigned segment = 0, turn = 0, base = 0;
   Segment g;
   for (; line.next(sh, p, sp, &g); ++segment, base += 2 * (g.t1 - g.t0)) {
@@ -418,23 +480,34 @@ __device__ void soft_group(Shared* sh, uint8_t* q_smem, uint8_t* ring, const Att
     named_bar_sync(1, kSoftThreads);  // the last segment's rows and accumulators are no longer read
     if (threadIdx.x == 0) sh->odd[(segment + 1) & 1] = 0;
 
-    {  // queries: whole tiles of our own, or half of the one tile
-      const int rows = two ? kAttendRows : kAttendRows / 2, row0 = two ? 0 : w * rows;
-      const int units = 2 * steps;  // 16 bytes each, the last one zeros where D is not a multiple of 16
-      uint8_t* const dst = q_smem + tile * kTileBytes;
-#pragma unroll 4
-      for (int x = r; x < rows * units; x += 128) {
-        const int row = row0 + x / units, u = x % units;
-        const int tok = tile * sp.tile_tokens + row / G, h = row % G;
-        uint4 v = make_uint4(0, 0, 0, 0);
-        if (row < tile_rows && tok < g.tokens && 8 * u < D)
-          v = *reinterpret_cast<const uint4*>(static_cast<const T*>(p.q) + (g.s.row + g.tok0 + tok) * p.q_stride +
-                                              (g.head * G + h) * D + 8 * u);
-        *reinterpret_cast<uint4*>(dst + (u >> 3) * kHalfBytes + row * 128 + (((u & 7) ^ (row & 7)) << 4)) = v;
+    // a tile's 16-byte units, a thread one column of them: queries in, results out
+    const int rows = two ? kAttendRows : kAttendRows / 2, row0 = two ? 0 : w * rows;
+    uint8_t* const q_tile = q_smem + tile * kTileBytes;
+    auto element = [&](int row, int64_t stride) {  // of the row's first query in a [token][head][D] tensor, or -1
+      const int tk = row * inv_group >> 16, tok = tile * sp.tile_tokens + tk;
+      return row < tile_rows && tok < g.tokens
+                 ? (g.s.row + g.tok0 + tok) * stride + static_cast<int64_t>(g.head * G + row - tk * G) * D + 8 * unit
+                 : -1;
+    };
+    if (unit_row < row_step) {
+      uint4 v[16];
+#pragma unroll 1
+      for (int x0 = 0; x0 < rows; x0 += 16 * row_step) {
+#pragma unroll
+        for (int x = 0; x < 16; ++x) {
+          const int row = unit_row + x0 + x * row_step;
+          const int64_t e = row < rows ? element(row0 + row, p.q_stride) : -1;
+          v[x] = e >= 0 && 8 * unit < D ? *reinterpret_cast<const uint4*>(static_cast<const T*>(p.q) + e) : make_uint4(0, 0, 0, 0);
+        }
+#pragma unroll
+        for (int x = 0; x < 16; ++x) {
+          const int row = unit_row + x0 + x * row_step;
+          if (row < rows) *reinterpret_cast<uint4*>(q_tile + unit_offset(row0 + row, unit)) = v[x];
+        }
       }
-      fence_async_smem();
-      mbar_arrive(&sh->q_ready);
     }
+    fence_async_smem();
+    mbar_arrive(&sh->q_ready);
 
     const int tok = tile * sp.tile_tokens + my_tok;  // in the group
     const bool valid = r < tile_rows && tok < g.tokens;
@@ -560,58 +633,70 @@ __device__ void soft_group(Shared* sh, uint8_t* q_smem, uint8_t* ring, const Att
     }
     const bool odd = *reinterpret_cast<volatile int*>(&sh->odd[segment & 1]) != 0;
     const bool whole = g.t0 == 0 && g.t1 == g.tiles;
-    const long long row = g.s.row + i;
-    const int head = g.head * G + my_head;
     const float inv = l == 0.f ? 0.f : 1.f / l;
     const int slot = 2 * blockIdx.x + (g.t0 == 0 ? 1 : 0), slot_row = tile * kAttendRows + r;
-    for (int d = two ? 0 : w; d < steps; d += two ? 1 : 2) {
-      float o[16];
+#pragma unroll 1
+    for (int d = two ? 0 : 32 * w; d < D; d += two ? 32 : 64) {
+      float o[32];
       if (two) {
-        tc_ld_x16(o_col + 16 * d, o);
+        tc_ld_x32(o_col + d, o);
         tc_wait_ld();
       } else {
-        float o1[16];
-        tc_ld_x16(tmem + kO + 16 * d, o);
-        tc_ld_x16(tmem + kO + 128 + 16 * d, o1);
+        float o1[32];
+        tc_ld_x32(tmem + kO + d, o);
+        tc_ld_x32(tmem + kO + 128 + d, o1);
         tc_wait_ld();
 #pragma unroll
-        for (int x = 0; x < 16; ++x) o[x] = (f0 == 0.f ? 0.f : o[x] * f0) + (f1 == 0.f ? 0.f : o1[x] * f1);
+        for (int x = 0; x < 32; ++x) o[x] = (f0 == 0.f ? 0.f : o[x] * f0) + (f1 == 0.f ? 0.f : o1[x] * f1);
       }
-      if (!valid) continue;
-      if (odd) {  // what was left out of the products, where this row sees it
-        const int end = min(g.s.kv, g.t1 * kAttendKeys);
-        for (int key = max(masked_from(p, g.s, g.tok0), g.t0 * kAttendKeys); key < end; ++key) {
-          if (!sees(p.mask, parent, p.N, i, static_cast<long long>(g.s.kv) - g.s.n, key)) continue;
-          const long long off = place_offset(p.cache, p.batch, g.seq, key);
-          if (off < 0) continue;
-          const T* const v = static_cast<const T*>(p.cache.v) + off + g.head * p.cache.head_stride;
+      if (valid) {
+        if (odd) {  // what was left out of the products, where this row sees it
+          const int end = min(g.s.kv, g.t1 * kAttendKeys);
+          for (int key = max(masked_from(p, g.s, g.tok0), g.t0 * kAttendKeys); key < end; ++key) {
+            if (!sees(p.mask, parent, p.N, i, static_cast<long long>(g.s.kv) - g.s.n, key)) continue;
+            const long long off = place_offset(p.cache, p.batch, g.seq, key);
+            if (off < 0) continue;
+            const T* const v = static_cast<const T*>(p.cache.v) + off + g.head * p.cache.head_stride;
 #pragma unroll
-          for (int x = 0; x < 16; ++x) {
-            if (16 * d + x >= D) break;
-            const float f = to_f32(v[16 * d + x]);
-            if (!isfinite(f)) o[x] += f;
+            for (int x = 0; x < 32; ++x) {
+              if (d + x >= D) break;
+              const float f = to_f32(v[d + x]);
+              if (!isfinite(f)) o[x] += f;
+            }
           }
         }
-      }
-      if (whole) {
-        T* const out = static_cast<T*>(p.out) + row * p.out_stride + static_cast<long long>(head) * D + 16 * d;
+        if (whole) {
 #pragma unroll
-        for (int x = 0; x < 16; x += 8) {
-          if (16 * d + x >= D) break;
-          float y[8];
+          for (int x = 0; x < 32; x += 8) {
+            float y[8];
 #pragma unroll
-          for (int e = 0; e < 8; ++e) y[e] = l == 0.f ? 0.f : o[x + e] * inv;
-          Vec<T> v;
-          pack(y, &v);
-          *reinterpret_cast<uint4*>(out + x) = v.raw;
+            for (int e = 0; e < 8; ++e) y[e] = l == 0.f ? 0.f : o[x + e] * inv;
+            Vec<T> v;
+            pack(y, &v);
+            if (d + x < D) *reinterpret_cast<uint4*>(q_tile + unit_offset(r, (d + x) >> 3)) = v.raw;
+          }
+        } else {
+          float* const part = sp.parts + (static_cast<long long>(slot) * D + d) * sp.slot_rows + slot_row;
+#pragma unroll
+          for (int x = 0; x < 32; ++x)
+            if (d + x < D) part[x * sp.slot_rows] = o[x];
         }
-      } else {
-        float* const part = sp.parts + (static_cast<long long>(slot) * D + 16 * d) * sp.slot_rows + slot_row;
-#pragma unroll
-        for (int x = 0; x < 16; ++x)
-          if (16 * d + x < D) part[static_cast<long long>(x) * sp.slot_rows] = o[x];
       }
+      __syncwarp();  // the loads of tensor memory are the whole warp's
     }
+    if (whole) {  // the results lie where the queries were: rows out side by side
+      if (two) named_bar_sync(2 + w, 128); else named_bar_sync(1, kSoftThreads);
+      if (unit_row < row_step && 8 * unit < D)
+#pragma unroll 4
+        for (int x = unit_row; x < rows; x += row_step) {
+          const int64_t e = element(row0 + x, p.out_stride);
+          if (e >= 0)
+            *reinterpret_cast<uint4*>(static_cast<T*>(p.out) + e) =
+                *reinterpret_cast<const uint4*>(q_tile + unit_offset(row0 + x, unit));
+        }
+    }
+    const long long row = g.s.row + i;
+    const int head = g.head * G + my_head;
     if (valid && (two || w == 0)) {
       if (!whole) {
         float* const norm = sp.norms + static_cast<long long>(slot) * 2 * sp.slot_rows + slot_row;
@@ -625,7 +710,7 @@ __device__ void soft_group(Shared* sh, uint8_t* q_smem, uint8_t* ring, const Att
   }
 }
 
-__device__ __forceinline__ long long stretch(long long units, int ctas) { return (units + ctas - 1) / ctas; }
+__device__ __forceinline__ long long stretch(long long units, int ctas) { return quotient(units + ctas - 1, ctas); }
 
 template <typename T>
 __global__ void __launch_bounds__(kThreads, 1)
@@ -660,15 +745,33 @@ __global__ void __launch_bounds__(kThreads, 1)
   }
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  bool several = false;
   for (int b = tid; b < p.batch.B; b += kThreads) {
     const Sequence s = load_sequence(p.cache, p.batch, p.tokens, b);
+    const long long n = sequence_units(p, sp, s);
+    several = several || n < 0;
     sh->seq[b] = s;
-    sh->before[b + 1] = sequence_units(p, sp, s);
+    sh->before[b + 1] = n;
   }
   if (tid == 0) sh->before[0] = 0;
   tc_fence_before();
-  __syncthreads();
+  several = __syncthreads_or(several);
   tc_fence_after();
+  const int lane = tid & 31;
+  if (several) {  // a warp a sequence, a lane a group
+    const int step = 2 * sp.tile_tokens;
+    for (int b = warp; b < p.batch.B; b += kThreads / 32) {
+      if (sh->before[b + 1] >= 0) continue;
+      const Sequence s = sh->seq[b];
+      long long n = 0;
+      for (int t = lane * step; t < s.n; t += 32 * step) n += kGroupCost + key_tiles(p.mask, s, min(t + step, s.n));
+#pragma unroll
+      for (int o = 16; o; o >>= 1) n += __shfl_xor_sync(~0u, n, o);
+      __syncwarp();
+      if (lane == 0) sh->before[b + 1] = n * p.cache.heads;
+    }
+    __syncthreads();
+  }
   if (warp == 0) {
     long long carry = 0;
     for (int b = 0; b < p.batch.B; b += 32) {
@@ -693,20 +796,22 @@ __global__ void __launch_bounds__(kThreads, 1)
   } else {
     regs_down<kOtherRegs>();
     if (warp == kSoftThreads / 32) load_warp(sh, ring, &keys, &values, p, sp, line);
-    if (tid == kSoftThreads + 32) {
-      multiply_thread<T>(sh, smem_u32(tiles), smem_u32(ring), p, sp, line);
-      // the last group of this stretch that goes on: where, for the kernel that joins
-      AttendTail tail{-1, 0, 0, 0};
-      Segment g;
-      while (line.next(sh, p, sp, &g))
-        if (g.t0 == 0 && g.t1 < g.tiles)
-          tail = AttendTail{static_cast<int>((line.at + g.tiles - g.t1 - 1) / each), g.s.row + g.tok0, g.head, g.tokens};
-      sp.tails[blockIdx.x] = tail;
+    if (warp == kSoftThreads / 32 + 1) {
+      multiply_warp<T>(sh, smem_u32(tiles), smem_u32(ring), p, sp, line);
       if (sh->abort) {  // products in flight read the tiles and write the accumulators: they take microseconds
         const long long t0 = clock64();
         while (clock64() - t0 < kWaitCycles / 1024) {
         }
       }
+    }
+    if (tid == kSoftThreads + 64) {
+      // the last group of this stretch that goes on: where, for the kernel that joins
+      AttendTail tail{-1, 0, 0, 0};
+      Segment g;
+      while (line.next(sh, p, sp, &g))
+        if (g.t0 == 0 && g.t1 < g.tiles)
+          tail = AttendTail{static_cast<int>(quotient(line.at + g.tiles - g.t1 - 1, each)), g.s.row + g.tok0, g.head, g.tokens};
+      sp.tails[blockIdx.x] = tail;
     }
   }
   __syncwarp();
@@ -721,9 +826,10 @@ __global__ void __launch_bounds__(kThreads, 1)
 
 // ---------------------------------------------------------------- joining
 constexpr int kJoinThreads = 256;
+constexpr int kJoinAhead = 8;  // partial results in flight
 
 // The group that CTA blockIdx.x began and others went on with: its rows' sums over all of them, in their order.  A thread
-// takes eight elements of a row; rows lie side by side in the slots.
+// takes four elements of a row; rows lie side by side in the slots.
 template <typename T>
 __global__ void __launch_bounds__(kJoinThreads) join_kernel(const AttendParams p, const AttendSplit sp) {
   asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -739,37 +845,50 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const AttendParams p
   }
   const AttendTail tail = sp.tails[blockIdx.x];
   if (tail.last < 0) return;
-  const int D = p.cache.D, G = p.group, rows = tail.tokens * G, octets = D / 8, first = blockIdx.x;
-  const long long slot_rows = sp.slot_rows;
-  for (int x = blockIdx.y * kJoinThreads + threadIdx.x; x < rows * octets; x += gridDim.y * kJoinThreads) {
-    const int oct = x / rows, at = x - oct * rows, tok = at / G, h = at - tok * G;
+  const int D = p.cache.D, G = p.group, rows = tail.tokens * G, first = blockIdx.x, slot_rows = sp.slot_rows;
+  for (int x = blockIdx.y * kJoinThreads + threadIdx.x; x < rows * (D / 4); x += gridDim.y * kJoinThreads) {
+    const int d = x / rows * 4, at = x - x / rows * rows, tok = at / G, h = at - tok * G;
     const int slot_row = tok < sp.tile_tokens ? at : kAttendRows + at - sp.tile_tokens * G;
-    auto slot = [&](int i) { return static_cast<long long>(i == first ? 2 * i + 1 : 2 * i); };
-    float m = -INFINITY;
-#pragma unroll 4
-    for (int i = first; i <= tail.last; ++i) m = fmaxf(m, sp.norms[slot(i) * 2 * slot_rows + slot_row]);
-    float l = 0.f, o[8];
+    float m = -INFINITY, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int i0 = first; i0 <= tail.last; i0 += kJoinAhead) {
+      float mi[kJoinAhead], li[kJoinAhead], oi[kJoinAhead][4];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) o[e] = 0.f;
-#pragma unroll 4
-    for (int i = first; i <= tail.last; ++i) {
-      const float* const norm = sp.norms + slot(i) * 2 * slot_rows + slot_row;
-      const float* const part = sp.parts + (slot(i) * D + 8 * oct) * slot_rows + slot_row;
-      const float mi = norm[0];
-      const float f = mi == -INFINITY ? 0.f : mi == m ? 1.f : ex2((mi - m) * p.scale_log2);
-      l = fmaf(norm[slot_rows], f, l);
+      for (int i = 0; i < kJoinAhead; ++i) {
+        const bool is = i0 + i <= tail.last;
+        const long long slot = i0 + i == first ? 2 * first + 1 : 2 * (is ? i0 + i : first);
+        const float* const norm = sp.norms + slot * 2 * slot_rows + slot_row;
+        const float* const part = sp.parts + (slot * D + d) * slot_rows + slot_row;
+        mi[i] = is ? norm[0] : -INFINITY;
+        li[i] = is ? norm[slot_rows] : 0.f;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) o[e] = fmaf(part[e * slot_rows], f, o[e]);
+        for (int e = 0; e < 4; ++e) oi[i][e] = is ? part[e * slot_rows] : 0.f;
+      }
+      float up = m;
+#pragma unroll
+      for (int i = 0; i < kJoinAhead; ++i) up = fmaxf(up, mi[i]);
+      const float keep = m == up ? 1.f : ex2((m - up) * p.scale_log2);
+      m = up;
+      l *= keep;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] *= keep;
+#pragma unroll
+      for (int i = 0; i < kJoinAhead; ++i) {
+        const float f = mi[i] == m ? 1.f : ex2((mi[i] - m) * p.scale_log2);
+        if (mi[i] == -INFINITY) continue;  // a part that saw nothing: sums of 0
+        l = fmaf(li[i], f, l);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = fmaf(oi[i][e], f, o[e]);
+      }
     }
     const long long row = tail.row + tok;
     const int head = tail.head * G + h;
     const float inv = 1.f / l;
+    alignas(8) T y[4];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) o[e] = l == 0.f ? 0.f : o[e] * inv;
-    Vec<T> v;
-    pack(o, &v);
-    *reinterpret_cast<uint4*>(static_cast<T*>(p.out) + row * p.out_stride + static_cast<long long>(head) * D + 8 * oct) = v.raw;
-    if (p.lse && oct == 0) p.lse[row * p.hq + head] = l == 0.f ? -INFINITY : fmaf(m, p.scale, logf(l));
+    for (int e = 0; e < 4; ++e) from_f32(l == 0.f ? 0.f : o[e] * inv, y + e);
+    *reinterpret_cast<uint2*>(static_cast<T*>(p.out) + row * p.out_stride + static_cast<long long>(head) * D + d) =
+        *reinterpret_cast<const uint2*>(y);
+    if (p.lse && d == 0) p.lse[row * p.hq + head] = l == 0.f ? -INFINITY : fmaf(m, p.scale, logf(l));
   }
 }
 
@@ -790,7 +909,7 @@ cudaError_t launch_tc_type(const CUtensorMap& keys, const CUtensorMap& values, c
   cfg.numAttrs = 1;
   e = cudaLaunchKernelEx(&cfg, attend_kernel<T>, keys, values, p, s);
   if (e != cudaSuccess) return e;
-  cfg.gridDim = dim3(grid, s.slot_rows > kAttendRows ? 8 : 1);
+  cfg.gridDim = dim3(grid, std::min(8, (s.slot_rows * p.cache.D / 4 + kJoinThreads - 1) / kJoinThreads));
   cfg.blockDim = dim3(kJoinThreads);
   cfg.dynamicSmemBytes = 0;
   return cudaLaunchKernelEx(&cfg, join_kernel<T>, p, s);

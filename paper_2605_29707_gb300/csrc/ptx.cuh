@@ -246,13 +246,6 @@ __device__ __forceinline__ uint64_t smem_desc_sw128(uint32_t saddr) {
   return d;
 }
 
-// The same for an MN-major operand: rows along K, 64 elements of MN (128 B) each, 8-row atoms 1024 B apart
-// (stride byte offset); the next 64 elements of MN lie `block` bytes on (leading byte offset).  Stepping K by 16 rows
-// adds 2048 bytes to the address.
-__device__ __forceinline__ uint64_t smem_desc_sw128_mn(uint32_t saddr, uint32_t block) {
-  return (smem_desc_sw128(saddr) & ~(static_cast<uint64_t>(0x3FFF) << 16)) | (static_cast<uint64_t>(block >> 4) << 16);
-}
-
 // Instruction descriptor of kind::f16: D fp32 (bits 4-5 = 1), A and B bf16 (bits 7-9 and
 // 10-12 = 1), both K-major (bits 15, 16 = 0), N >> 3 in bits 17-22, M >> 4 in bits 24-28.
 __host__ __device__ constexpr uint32_t idesc_bf16_f32(int M, int N) {
