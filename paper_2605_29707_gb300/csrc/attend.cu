@@ -39,7 +39,7 @@ constexpr int kStages = 4;          // tiles of keys or values in flight
 constexpr int kHalfBytes = 16384;   // 128 rows of 64 elements
 constexpr int kTileBytes = 2 * kHalfBytes;
 constexpr int kSoftThreads = 256;
-constexpr int kThreads = kSoftThreads + 128;  // and a warp that loads, one that multiplies, two that make up a warpgroup
+constexpr int kThreads = kSoftThreads + 128;  // and two warps that load, one that multiplies, one for the tail
 // Registers a thread: 168 at launch (384 threads share 65536); rows of 128 scores take more, the other warps less:
 // 2 x 128 x 216 + 128 x 72 = 384 x 168.
 constexpr int kSoftRegs = 216, kOtherRegs = 72;
@@ -122,7 +122,20 @@ __device__ __forceinline__ void tc_wait_st() {
   asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
 }
 
+// 16 bytes from global to shared memory, or zeros; cp.async.wait_all waits for the thread's.
+__device__ __forceinline__ void copy_async(void* dst, const void* src, bool full) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(dst)), "l"(src), "r"(full ? 16 : 0) : "memory");
+}
 __device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+// mbar_wait with its loop out of line: the kernel waits in many places, and code that fits the instruction cache counts
+// (145 KB of it made the end of a segment take 6000 cycles).
+__device__ __noinline__ bool wait_long(uint64_t* bar, uint32_t parity, int* abort, int* code) {
+  return mbar_wait(bar, parity, abort, code);
+}
+__device__ __forceinline__ bool wait_for(Shared* sh, uint64_t* bar, uint32_t parity) {
+  return mbar_try_wait(bar, parity) || wait_long(bar, parity, &sh->abort, &sh->code);
+}
 
 template <int N>
 __device__ __forceinline__ void regs_up() {
@@ -173,7 +186,7 @@ struct Segment {
   int t0, t1, tiles;   // tiles of keys here, of all
 };
 
-__device__ __forceinline__ long long quotient(long long a, long long b) {
+__device__ __noinline__ long long quotient(long long a, long long b) {
   if (((a | b) >> 32) == 0) return static_cast<unsigned>(a) / static_cast<unsigned>(b);
   return a / b;
 }
@@ -206,6 +219,7 @@ struct Line {
         const int lane = threadIdx.x & 31, share = (groups + 31) / 32;
         const int mine = min(groups, lane * share), stop = min(groups, mine + share);
         long long sum = 0;
+#pragma unroll 1
         for (int i = mine; i < stop; ++i) sum += kGroupCost + key_tiles(p.mask, s, min((i + 1) * step, s.n));
         long long upto = sum;
 #pragma unroll
@@ -215,6 +229,7 @@ struct Line {
         }
         const int owner = __ffs(__ballot_sync(~0u, rest < upto)) - 1;
         rest -= __shfl_sync(~0u, upto - sum, owner);
+#pragma unroll 1
         for (g = owner * share;; ++g) {
           const int n = kGroupCost + key_tiles(p.mask, s, min((g + 1) * step, s.n));
           if (rest < n) break;
@@ -312,54 +327,69 @@ __device__ __forceinline__ void drain_wait(uint64_t* bar, uint32_t parity) {
 // Tiles of a segment with n of them pass the ring as K_0 .. K_(a-1), then V_j and K_(j+a) in turn: the order in which the
 // products want them, a = 1 where both warpgroups take every tile, 2 where they alternate.
 __device__ __forceinline__ int value_place(int j, int n, int ahead) { return min(ahead, n) + j + min(j, max(0, n - ahead)); }
+__device__ __forceinline__ int key_place(int j, int n, int ahead) { return j < ahead ? j : value_place(j - ahead, n, ahead) + 1; }
 
-__device__ void load_warp(Shared* sh, uint8_t* ring, const CUtensorMap* keys, const CUtensorMap* values,
-                          const AttendParams& p, const AttendSplit& sp, Line line) {
+// One warp brings the keys, one the values: a copy a piece (what a page has in common with a tile) and half of the
+// elements.  A lane a piece keeps the piece's place and looks its page up a tile ahead.
+__device__ void load_warp(Shared* sh, uint8_t* ring, const CUtensorMap* map, bool values, const AttendParams& p,
+                          const AttendSplit& sp, Line line) {
   const int lane = threadIdx.x & 31;
-  const int halves = p.cache.D > 64 ? 2 : 1, pieces = kAttendKeys / sp.piece;
-  const bool mine = lane < pieces * halves;
-  const int piece = lane % pieces, half = lane / pieces;
-  const uint32_t offset = half * kHalfBytes + piece * sp.piece * 128;
+  const int pieces = kAttendKeys / sp.piece, page_size = p.cache.page;
+  const bool two_halves = p.cache.D > 64;
+  const uint32_t bytes = two_halves ? kTileBytes : kHalfBytes;
+  const int pages_on = kAttendKeys / page_size, places_on = kAttendKeys % page_size;
   const uint64_t policy = l2_policy_evict_normal();
-  unsigned it = 0;
+  unsigned base = 0, used[kStages] = {};  // used: our last copy into a stage, plus 1
   Segment g;
   bool ok = true;
   while (ok && line.next(sh, p, sp, &g)) {
-    const bool two = g.tokens > sp.tile_tokens;
-    const int n = g.t1 - g.t0, ahead = two ? 1 : 2;
+    const int n = g.t1 - g.t0, ahead = g.tokens > sp.tile_tokens ? 1 : 2;
     const int32_t* const table = p.batch.table + g.seq * p.batch.table_stride;
-    auto find = [&](int j, int* token) {  // this lane's page of tile j, past the last one where there is nothing
-      const int place = (g.t0 + j) * kAttendKeys + piece * sp.piece;
-      if (!mine || static_cast<unsigned>(place) >= static_cast<unsigned>(g.s.kv)) return p.cache.pages;
-      const int i = place / p.cache.page;
-      *token = place - i * p.cache.page;
-      const int page = table[i];
-      if (page >= 0 && page < p.cache.pages) return page;
-      sh->code = kStatusBadPage;
-      return p.cache.pages;
+    int place = g.t0 * kAttendKeys + lane * sp.piece, entry = place / page_size, token = place - entry * page_size;
+    auto look = [&]() {  // past the last page where there is nothing: reads as zeros
+      return lane < pieces && static_cast<unsigned>(place) < static_cast<unsigned>(g.s.kv) ? table[entry] : p.cache.pages;
     };
-    int next_k = 0, next_v = 0, token = 0, page = find(0, &token);
-    for (int c = 0; c < 2 * n; ++c, ++it) {
-      const bool value = next_k >= min(n, next_v + ahead);
-      if (value) ++next_v; else ++next_k;
-      // the page of the copy after this one is on its way while this one waits for room
-      int token_after = 0, page_after = 0;
-      if (c + 1 < 2 * n) page_after = find(next_k >= min(n, next_v + ahead) ? next_v : next_k, &token_after);
-      const int stage = it % kStages;
-      ok = it < kStages || mbar_wait(&sh->empty[stage], (it / kStages - 1) & 1, &sh->abort, &sh->code);
+    int found = look();
+    for (int j = 0; j < n; ++j) {
+      int page = found;
+      const int here = token;
+      if (page < 0 || page > p.cache.pages || (page == p.cache.pages && lane < pieces && place < g.s.kv)) {
+        sh->code = kStatusBadPage;
+        page = p.cache.pages;
+      }
+      place += kAttendKeys;
+      entry += pages_on;
+      token += places_on;
+      if (token >= page_size) {
+        token -= page_size;
+        ++entry;
+      }
+      if (j + 1 < n) found = look();
+      const unsigned at = base + (values ? value_place(j, n, ahead) : key_place(j, n, ahead));
+      const int stage = at % kStages;
+      ok = at < kStages || wait_for(sh, &sh->empty[stage], (at / kStages - 1) & 1);
       ok = __all_sync(~0u, ok);
       if (!ok) break;
-      if (lane == 0) mbar_arrive_expect_tx(&sh->full[stage], halves * kHalfBytes);
+      uint8_t* dst = ring + stage * kTileBytes;
+      if (elect_one()) mbar_arrive_expect_tx(&sh->full[stage], bytes);
       __syncwarp();
-      if (mine)
-        tma_load_4d(ring + stage * kTileBytes + offset, value ? values : keys, &sh->full[stage], half * 64, token, g.head, page,
-                    policy);
-      token = token_after;
-      page = page_after;
+#pragma unroll 1
+      for (int q = 0; q < pieces; ++q, dst += sp.piece * 128) {
+        const int y = __shfl_sync(~0u, here, q), w = __shfl_sync(~0u, page, q);
+        if (elect_one()) {
+          tma_load_4d(dst, map, &sh->full[stage], 0, y, g.head, w, policy);
+          if (two_halves) tma_load_4d(dst + kHalfBytes, map, &sh->full[stage], 64, y, g.head, w, policy);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < kStages; ++i) used[i] = i == stage ? at + 1 : used[i];
     }
+    base += 2 * n;
   }
   if (!ok)  // nothing of ours stays in flight
-    for (unsigned i = it < kStages ? 0 : it - kStages; i < it; ++i) drain_wait(&sh->full[i % kStages], (i / kStages) & 1);
+#pragma unroll
+    for (int i = 0; i < kStages; ++i)
+      if (used[i]) drain_wait(&sh->full[i], ((used[i] - 1) / kStages) & 1);
 }
 
 // The whole warp walks the line, one thread issues: what steers the products stays in uniform registers.
@@ -374,7 +404,7 @@ __device__ void multiply_warp(Shared* sh, uint32_t q_addr, uint32_t ring_addr, c
   Segment g;
   auto take = [&]() {
     const unsigned stage = it % kStages;
-    const bool ok = mbar_wait(&sh->full[stage], (it / kStages) & 1, &sh->abort, &sh->code);
+    const bool ok = wait_for(sh, &sh->full[stage], (it / kStages) & 1);
     ++it;
     return __all_sync(~0u, ok) ? static_cast<int>(stage) : -1;
   };
@@ -407,51 +437,38 @@ __device__ void multiply_warp(Shared* sh, uint32_t q_addr, uint32_t ring_addr, c
     __syncwarp();
   };
   auto weights = [&](int w) {
-    return __all_sync(~0u, mbar_wait(&sh->w_ready[w], turns[w]++ & 1, &sh->abort, &sh->code));
+    return __all_sync(~0u, wait_for(sh, &sh->w_ready[w], turns[w]++ & 1));
   };
   while (line.next(sh, p, sp, &g)) {
-    if (!__all_sync(~0u, mbar_wait(&sh->q_ready, segment++ & 1, &sh->abort, &sh->code))) return;
+    if (!__all_sync(~0u, wait_for(sh, &sh->q_ready, segment++ & 1))) return;
+    // step x: O of warpgroup x & 1 from its weights, then S of its next tile of keys; two steps of S alone go before
     const bool two = g.tokens > sp.tile_tokens;
-    const int n = g.t1 - g.t0;
-    if (two) {
-      int k = take();
-      if (k < 0) return;
-      scores(0, 0, k, false);
-      scores(1, 1, k, true);
-      for (int j = 0; j < n; ++j) {
-        if (!weights(0)) return;
-        const int v = take();
-        if (v < 0) return;
-        weigh(0, v, j > 0, false);
-        if (j + 1 < n) {
-          k = take();
-          if (k < 0) return;
-          scores(0, 0, k, false);
-        }
-        if (!weights(1)) return;
-        weigh(1, v, j > 0, true);
-        if (j + 1 < n) scores(1, 1, k, true);
-      }
-    } else {
-      for (int w = 0; w < 2 && w < n; ++w) {
-        const int k = take();
-        if (k < 0) return;
-        scores(w, 0, k, true);
-      }
-      for (int j = 0; j < n; ++j) {
-        const int w = j & 1;
+    const int n = g.t1 - g.t0, stop = two ? 2 * n : n;
+    int k = 0, v = 0;
+#pragma unroll 1
+    for (int x = -2; x < stop; ++x) {
+      const int w = x & 1;
+      const bool first = !two || w == 0, last = !two || w == 1;  // to want the tile
+      if (x >= 0) {
         if (!weights(w)) return;
-        const int v = take();
-        if (v < 0) return;
-        weigh(w, v, j >= 2, true);
-        if (j + 2 < n) {
-          const int k = take();
-          if (k < 0) return;
-          scores(w, 0, k, true);
-        }
+        if (first && (v = take()) < 0) return;
+        weigh(w, v, x >= 2, last);
+      }
+      if ((two ? x >> 1 : x + 1) + 1 < n) {
+        if (first && (k = take()) < 0) return;
+        scores(w, two ? w : 0, k, last);
       }
     }
   }
+}
+
+// Sets what is not finite among two elements to 0; true if something was.
+template <typename T>
+__device__ __forceinline__ bool drop_odd(uint32_t* w) {
+  constexpr uint32_t kExp = std::is_same<T, __half>::value ? 0x7C00u : 0x7F80u;  // all ones: infinity or NaN
+  const uint32_t keep = ((*w & kExp) == kExp ? 0 : 0xFFFFu) | ((*w & kExp << 16) == kExp << 16 ? 0 : 0xFFFF0000u);
+  *w &= keep;
+  return keep != ~0u;
 }
 
 // Byte offset of a row's 16-byte unit in a 128-byte swizzled tile.
@@ -489,23 +506,14 @@ __device__ void soft_group(Shared* sh, uint8_t* q_smem, uint8_t* ring, const Att
                  ? (g.s.row + g.tok0 + tok) * stride + static_cast<int64_t>(g.head * G + row - tk * G) * D + 8 * unit
                  : -1;
     };
-    if (unit_row < row_step) {
-      uint4 v[16];
-#pragma unroll 1
-      for (int x0 = 0; x0 < rows; x0 += 16 * row_step) {
-#pragma unroll
-        for (int x = 0; x < 16; ++x) {
-          const int row = unit_row + x0 + x * row_step;
-          const int64_t e = row < rows ? element(row0 + row, p.q_stride) : -1;
-          v[x] = e >= 0 && 8 * unit < D ? *reinterpret_cast<const uint4*>(static_cast<const T*>(p.q) + e) : make_uint4(0, 0, 0, 0);
-        }
-#pragma unroll
-        for (int x = 0; x < 16; ++x) {
-          const int row = unit_row + x0 + x * row_step;
-          if (row < rows) *reinterpret_cast<uint4*>(q_tile + unit_offset(row0 + row, unit)) = v[x];
-        }
+    if (unit_row < row_step)
+#pragma unroll 2
+      for (int x = unit_row; x < rows; x += row_step) {
+        const int64_t e = element(row0 + x, p.q_stride);
+        copy_async(q_tile + unit_offset(row0 + x, unit), static_cast<const T*>(p.q) + max(e, static_cast<int64_t>(0)),
+                   e >= 0 && 8 * unit < D);
       }
-    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
     fence_async_smem();
     mbar_arrive(&sh->q_ready);
 
@@ -549,6 +557,7 @@ __device__ void soft_group(Shared* sh, uint8_t* q_smem, uint8_t* ring, const Att
           const float keep = m == up ? 1.f : ex2((m - up) * c);
           mbar_wait(&sh->o_done[w], (turn - 1) & 1, &sh->abort, &sh->code);
           tc_fence_after();
+#pragma unroll 1
           for (int d = 0; d < steps; ++d) {
             float o[16];
             tc_ld_x16(o_col + 16 * d, o);
@@ -584,25 +593,17 @@ __device__ void soft_group(Shared* sh, uint8_t* q_smem, uint8_t* ring, const Att
         mbar_wait(&sh->full[stage], (place / kStages) & 1, &sh->abort, &sh->code);
         if (key >= from) {
           uint8_t* const row = ring + stage * kTileBytes + r * 128;
+#pragma unroll 1
           for (int u = 0; u < 2 * steps; ++u) {
             uint4* const at = reinterpret_cast<uint4*>(row + (u >> 3) * kHalfBytes + (((u & 7) ^ (r & 7)) << 4));
             if (key >= g.s.kv) {
               *at = make_uint4(0, 0, 0, 0);
             } else {
-              Vec<T> v;
-              v.raw = *at;
-              float f[8];
-              unpack(v, f);
-              bool odd = false;
-#pragma unroll
-              for (int x = 0; x < 8; ++x) odd = odd || !isfinite(f[x]);
-              if (odd) {
+              uint4 v = *at;
+              if (drop_odd<T>(&v.x) | drop_odd<T>(&v.y) | drop_odd<T>(&v.z) | drop_odd<T>(&v.w)) {
                 *reinterpret_cast<volatile int*>(&sh->odd[segment & 1]) = 1;
                 __threadfence_block();
-#pragma unroll
-                for (int x = 0; x < 8; ++x) f[x] = isfinite(f[x]) ? f[x] : 0.f;
-                pack(f, &v);
-                *at = v.raw;
+                *at = v;
               }
             }
           }
@@ -636,58 +637,68 @@ __device__ void soft_group(Shared* sh, uint8_t* q_smem, uint8_t* ring, const Att
     const float inv = l == 0.f ? 0.f : 1.f / l;
     const int slot = 2 * blockIdx.x + (g.t0 == 0 ? 1 : 0), slot_row = tile * kAttendRows + r;
 #pragma unroll 1
-    for (int d = two ? 0 : 32 * w; d < D; d += two ? 32 : 64) {
-      float o[32];
+    for (int d = two ? 0 : 16 * w; d < D; d += two ? 16 : 32) {
+      float o[16];
+      tc_ld_x16((two ? o_col : tmem + kO) + d, o);
       if (two) {
-        tc_ld_x32(o_col + d, o);
         tc_wait_ld();
       } else {
-        float o1[32];
-        tc_ld_x32(tmem + kO + d, o);
-        tc_ld_x32(tmem + kO + 128 + d, o1);
+        float o1[16];
+        tc_ld_x16(tmem + kO + 128 + d, o1);
         tc_wait_ld();
 #pragma unroll
-        for (int x = 0; x < 32; ++x) o[x] = (f0 == 0.f ? 0.f : o[x] * f0) + (f1 == 0.f ? 0.f : o1[x] * f1);
+        for (int x = 0; x < 16; ++x) {
+          if (f0 == 0.f) o[x] = 0.f;
+          if (f1 == 0.f) o1[x] = 0.f;
+          o[x] = fmaf(o[x], f0, o1[x] * f1);
+        }
       }
       if (valid) {
-        if (odd) {  // what was left out of the products, where this row sees it
-          const int end = min(g.s.kv, g.t1 * kAttendKeys);
-          for (int key = max(masked_from(p, g.s, g.tok0), g.t0 * kAttendKeys); key < end; ++key) {
-            if (!sees(p.mask, parent, p.N, i, static_cast<long long>(g.s.kv) - g.s.n, key)) continue;
-            const long long off = place_offset(p.cache, p.batch, g.seq, key);
-            if (off < 0) continue;
-            const T* const v = static_cast<const T*>(p.cache.v) + off + g.head * p.cache.head_stride;
 #pragma unroll
-            for (int x = 0; x < 32; ++x) {
-              if (d + x >= D) break;
-              const float f = to_f32(v[d + x]);
-              if (!isfinite(f)) o[x] += f;
-            }
-          }
-        }
-        if (whole) {
-#pragma unroll
-          for (int x = 0; x < 32; x += 8) {
+        for (int x = 0; x < 16; x += 8) {
+          if (d + x >= D) break;
+          if (whole) {
             float y[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) y[e] = l == 0.f ? 0.f : o[x + e] * inv;
+            for (int e = 0; e < 8; ++e) y[e] = o[x + e] * inv;
             Vec<T> v;
             pack(y, &v);
-            if (d + x < D) *reinterpret_cast<uint4*>(q_tile + unit_offset(r, (d + x) >> 3)) = v.raw;
-          }
-        } else {
-          float* const part = sp.parts + (static_cast<long long>(slot) * D + d) * sp.slot_rows + slot_row;
+            if (l == 0.f) v.raw = make_uint4(0, 0, 0, 0);
+            *reinterpret_cast<uint4*>(q_tile + unit_offset(r, (d + x) >> 3)) = v.raw;
+          } else {
+            float* const part = sp.parts + (static_cast<long long>(slot) * D + d + x) * sp.slot_rows + slot_row;
 #pragma unroll
-          for (int x = 0; x < 32; ++x)
-            if (d + x < D) part[x * sp.slot_rows] = o[x];
+            for (int e = 0; e < 8; ++e) part[e * sp.slot_rows] = o[x + e];
+          }
         }
       }
       __syncwarp();  // the loads of tensor memory are the whole warp's
     }
+    if (odd && valid) {  // what was left out of the products, where this row sees it
+      const int end = min(g.s.kv, g.t1 * kAttendKeys);
+#pragma unroll 1
+      for (int key = max(masked_from(p, g.s, g.tok0), g.t0 * kAttendKeys); key < end; ++key) {
+        if (!sees(p.mask, parent, p.N, i, static_cast<long long>(g.s.kv) - g.s.n, key)) continue;
+        const long long off = place_offset(p.cache, p.batch, g.seq, key);
+        if (off < 0) continue;
+        const T* const v = static_cast<const T*>(p.cache.v) + off + g.head * p.cache.head_stride;
+#pragma unroll 1
+        for (int d = 0; d < D; ++d) {
+          const float f = to_f32(v[d]);
+          if (isfinite(f) || (!two && (d >> 4 & 1) != w)) continue;
+          if (whole) {
+            T* const at = reinterpret_cast<T*>(q_tile + unit_offset(r, d >> 3)) + (d & 7);
+            from_f32(to_f32(*at) + f, at);
+          } else {
+            sp.parts[(static_cast<long long>(slot) * D + d) * sp.slot_rows + slot_row] += f;
+          }
+        }
+      }
+    }
     if (whole) {  // the results lie where the queries were: rows out side by side
       if (two) named_bar_sync(2 + w, 128); else named_bar_sync(1, kSoftThreads);
       if (unit_row < row_step && 8 * unit < D)
-#pragma unroll 4
+#pragma unroll 2
         for (int x = unit_row; x < rows; x += row_step) {
           const int64_t e = element(row0 + x, p.out_stride);
           if (e >= 0)
@@ -746,6 +757,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   bool several = false;
+#pragma unroll 1
   for (int b = tid; b < p.batch.B; b += kThreads) {
     const Sequence s = load_sequence(p.cache, p.batch, p.tokens, b);
     const long long n = sequence_units(p, sp, s);
@@ -764,6 +776,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (sh->before[b + 1] >= 0) continue;
       const Sequence s = sh->seq[b];
       long long n = 0;
+#pragma unroll 1
       for (int t = lane * step; t < s.n; t += 32 * step) n += kGroupCost + key_tiles(p.mask, s, min(t + step, s.n));
 #pragma unroll
       for (int o = 16; o; o >>= 1) n += __shfl_xor_sync(~0u, n, o);
@@ -774,6 +787,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   }
   if (warp == 0) {
     long long carry = 0;
+#pragma unroll 1
     for (int b = 0; b < p.batch.B; b += 32) {
       long long x = b + tid < p.batch.B ? sh->before[b + tid + 1] : 0;
 #pragma unroll
@@ -795,7 +809,10 @@ __global__ void __launch_bounds__(kThreads, 1)
     soft_group<T>(sh, tiles, ring, p, sp, line);
   } else {
     regs_down<kOtherRegs>();
-    if (warp == kSoftThreads / 32) load_warp(sh, ring, &keys, &values, p, sp, line);
+    if (warp == kSoftThreads / 32 || warp == kSoftThreads / 32 + 2) {
+      const bool v = warp == kSoftThreads / 32 + 2;
+      load_warp(sh, ring, v ? &values : &keys, v, p, sp, line);
+    }
     if (warp == kSoftThreads / 32 + 1) {
       multiply_warp<T>(sh, smem_u32(tiles), smem_u32(ring), p, sp, line);
       if (sh->abort) {  // products in flight read the tiles and write the accumulators: they take microseconds
@@ -804,7 +821,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
       }
     }
-    if (tid == kSoftThreads + 64) {
+    if (tid == kSoftThreads + 96) {
       // the last group of this stretch that goes on: where, for the kernel that joins
       AttendTail tail{-1, 0, 0, 0};
       Segment g;
