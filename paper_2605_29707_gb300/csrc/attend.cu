@@ -39,21 +39,20 @@ constexpr int kStages = 4;          // tiles of keys or values in flight
 constexpr int kHalfBytes = 16384;   // 128 rows of 64 elements
 constexpr int kTileBytes = 2 * kHalfBytes;
 constexpr int kSoftThreads = 256;
-constexpr int kThreads = kSoftThreads + 128;  // and two warps that load, one that multiplies, one for the tail
+constexpr int kThreads = kSoftThreads + 128;  // and two warps for keys and values, one for queries, one that multiplies
 // Registers a thread: 168 at launch (384 threads share 65536); rows of 128 scores take more, the other warps less:
 // 2 x 128 x 216 + 128 x 72 = 384 x 168.
-constexpr int kSoftRegs = 216, kOtherRegs = 72;
+constexpr int kSoftRegs = 200, kOtherRegs = 104;
 constexpr int kS = 0, kO = 256;     // tensor memory columns: S of warpgroup w at 128 w, O at 256 + 128 w
-constexpr int kGroupCost = 3;       // what a group's queries and its end cost, in tiles of keys
 constexpr float kGrowth = 8.f;      // log2 of what a maximum may grow before O is scaled
 
 struct Shared {
-  uint64_t full[kStages], empty[kStages], s_full[2], w_ready[2], o_done[2], q_ready;
+  uint64_t full[kStages], empty[kStages], s_full[2], w_ready[2], o_done[2], q_ready[2], q_free[2];
   uint32_t tmem;
   int abort, code;
-  int odd[2];  // by the segment's parity: a value that is not finite in a masked tile
+  unsigned odd[2];  // by the segment's parity: the segment, from 1 on, that met a value that is not finite in a masked tile
   float norm[2][2][kAttendRows];  // warpgroup: maximum, sum
-  long long before[kAttendSeqs + 1];  // units of work before a sequence
+  int before[kAttendSeqs + 1];  // units of work before a sequence
   Sequence seq[kAttendSeqs];
 };
 constexpr size_t kSharedBytes = 1024 + static_cast<size_t>(2 + kStages) * kTileBytes + sizeof(Shared);
@@ -126,6 +125,11 @@ __device__ __forceinline__ void tc_wait_st() {
 __device__ __forceinline__ void copy_async(void* dst, const void* src, bool full) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(dst)), "l"(src), "r"(full ? 16 : 0) : "memory");
 }
+// One arrival for a warp, after what its threads did before.
+__device__ __forceinline__ void warp_arrive(uint64_t* bar) {
+  __syncwarp();
+  if ((threadIdx.x & 31) == 0) mbar_arrive(bar);
+}
 __device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
 // mbar_wait with its loop out of line: the kernel waits in many places, and code that fits the instruction cache counts
@@ -174,9 +178,8 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi, __half) {
 // Keys that some token below `last` of a sequence sees, in tiles; a group that sees none still has one, for its rows'
 // zeros.
 __device__ __forceinline__ int key_tiles(int mask, const Sequence& s, int last) {
-  const long long seen = mask == kMaskCausal ? static_cast<long long>(s.kv) - s.n + last : s.kv;
-  const int k = static_cast<int>(min(max(seen, 0LL), static_cast<long long>(s.kv)));
-  return max(1, k / kAttendKeys + (k % kAttendKeys != 0));
+  const int seen = mask == kMaskCausal ? min(max(s.kv - s.n + last, 0), s.kv) : s.kv;
+  return max(1, seen / kAttendKeys + (seen % kAttendKeys != 0));
 }
 
 struct Segment {
@@ -186,67 +189,61 @@ struct Segment {
   int t0, t1, tiles;   // tiles of keys here, of all
 };
 
-__device__ __noinline__ long long quotient(long long a, long long b) {
-  if (((a | b) >> 32) == 0) return static_cast<unsigned>(a) / static_cast<unsigned>(b);
-  return a / b;
-}
-
-// A CTA's stretch of the line.  A group of queries counts kGroupCost units and one a tile of keys.
+// A CTA's stretch of the line.  A group of queries counts kAttendGroupCost units and one a tile of keys.
 struct Line {
-  long long at, end;
+  int at, end;
   int seq, head, tok0, t;  // t: the tile at `at`, negative in the units before the first
 
-  __device__ __forceinline__ void begin(const Shared* sh, const AttendParams& p, const AttendSplit& sp, long long from,
-                                        long long to) {
+  __device__ __forceinline__ void begin(const Shared* sh, const AttendParams& p, const AttendSplit& sp, int from, int to) {
     at = from;
     end = to;
     if (at >= end) return;
     int lo = 0, hi = p.batch.B;
+#pragma unroll 1
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
       if (sh->before[mid] <= at) lo = mid; else hi = mid;
     }
     seq = lo;
-    const long long each = quotient(sh->before[lo + 1] - sh->before[lo], p.cache.heads);
-    long long rest = at - sh->before[lo];
-    head = static_cast<int>(quotient(rest, each));
+    const int each = (sh->before[lo + 1] - sh->before[lo]) / p.cache.heads;
+    int rest = at - sh->before[lo];
+    head = rest / each;
     rest -= head * each;
     const Sequence s = sh->seq[seq];
     const int step = 2 * sp.tile_tokens, groups = (s.n + step - 1) / step;
     int g = 0;
-    if (p.mask == kMaskCausal) {
-      if (groups > 1) {  // every lane of the warp adds up a part of them; the one where `rest` lies goes through its own
-        const int lane = threadIdx.x & 31, share = (groups + 31) / 32;
-        const int mine = min(groups, lane * share), stop = min(groups, mine + share);
-        long long sum = 0;
+    if (p.mask != kMaskCausal) {
+      const int n = kAttendGroupCost + key_tiles(p.mask, s, s.n);
+      g = rest / n;
+      rest -= g * n;
+    } else if (groups > 1) {  // every lane of the warp adds up a part of them; the one where `rest` lies goes through its own
+      const int lane = threadIdx.x & 31, share = (groups + 31) / 32;
+      const int mine = min(groups, lane * share), stop = min(groups, mine + share);
+      int sum = 0;
 #pragma unroll 1
-        for (int i = mine; i < stop; ++i) sum += kGroupCost + key_tiles(p.mask, s, min((i + 1) * step, s.n));
-        long long upto = sum;
+      for (int i = mine; i < stop; ++i) sum += kAttendGroupCost + key_tiles(p.mask, s, min((i + 1) * step, s.n));
+      int upto = sum;
 #pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-          const long long y = __shfl_up_sync(~0u, upto, o);
-          if (lane >= o) upto += y;
-        }
-        const int owner = __ffs(__ballot_sync(~0u, rest < upto)) - 1;
-        rest -= __shfl_sync(~0u, upto - sum, owner);
-#pragma unroll 1
-        for (g = owner * share;; ++g) {
-          const int n = kGroupCost + key_tiles(p.mask, s, min((g + 1) * step, s.n));
-          if (rest < n) break;
-          rest -= n;
-        }
+      for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(~0u, upto, o);
+        if (lane >= o) upto += y;
       }
-    } else {
-      const int n = kGroupCost + key_tiles(p.mask, s, s.n);
-      g = static_cast<int>(quotient(rest, n));
-      rest -= static_cast<long long>(g) * n;
+      const int owner = __ffs(__ballot_sync(~0u, rest < upto)) - 1;
+      rest -= __shfl_sync(~0u, upto - sum, owner);
+#pragma unroll 1
+      for (g = owner * share;; ++g) {
+        const int n = kAttendGroupCost + key_tiles(p.mask, s, min((g + 1) * step, s.n));
+        if (rest < n) break;
+        rest -= n;
+      }
     }
     tok0 = g * step;
-    t = static_cast<int>(rest) - kGroupCost;
+    t = rest - kAttendGroupCost;
   }
 
   __device__ __forceinline__ bool next(const Shared* sh, const AttendParams& p, const AttendSplit& sp, Segment* g) {
     const int step = 2 * sp.tile_tokens;
+#pragma unroll 1
     while (at < end) {
       while (sh->seq[seq].n == 0) ++seq;
       g->s = sh->seq[seq];
@@ -255,13 +252,13 @@ struct Line {
       g->tok0 = tok0;
       g->tokens = min(step, g->s.n - tok0);
       g->tiles = key_tiles(p.mask, g->s, tok0 + g->tokens);
-      const int n = static_cast<int>(min(static_cast<long long>(g->tiles) - t, end - at));
+      const int n = min(g->tiles - t, end - at);
       g->t0 = max(t, 0);
       at += n;
       t += n;
       g->t1 = t;
       if (t == g->tiles) {
-        t = -kGroupCost;
+        t = -kAttendGroupCost;
         tok0 += step;
         if (tok0 >= g->s.n) {
           tok0 = 0;
@@ -278,17 +275,16 @@ struct Line {
 };
 
 // A sequence's units; -1 where a causal one has several groups, each of its own length.
-__device__ __forceinline__ long long sequence_units(const AttendParams& p, const AttendSplit& sp, const Sequence& s) {
+__device__ __forceinline__ int sequence_units(const AttendParams& p, const AttendSplit& sp, const Sequence& s) {
   const int groups = (s.n + 2 * sp.tile_tokens - 1) / (2 * sp.tile_tokens);
   if (p.mask == kMaskCausal && groups > 1) return -1;
-  return static_cast<long long>(groups) * (kGroupCost + key_tiles(p.mask, s, s.n)) * p.cache.heads;
+  return groups * (kAttendGroupCost + key_tiles(p.mask, s, s.n)) * p.cache.heads;
 }
 
 // The first key that some token from tok0 on may not see.
 __device__ __forceinline__ int masked_from(const AttendParams& p, const Sequence& s, int tok0) {
   if (p.mask == kMaskFull) return s.kv;
-  const long long k = static_cast<long long>(s.kv) - s.n + (p.mask == kMaskCausal ? tok0 + 1 : 0);
-  return static_cast<int>(min(max(k, 0LL), static_cast<long long>(s.kv)));
+  return min(max(s.kv - s.n + (p.mask == kMaskCausal ? tok0 + 1 : 0), 0), s.kv);
 }
 
 // Which of 128 keys from key0 on token i sees, a bit each.
@@ -392,7 +388,8 @@ __device__ void load_warp(Shared* sh, uint8_t* ring, const CUtensorMap* map, boo
       if (used[i]) drain_wait(&sh->full[i], ((used[i] - 1) / kStages) & 1);
 }
 
-// The whole warp walks the line, one thread issues: what steers the products stays in uniform registers.
+// The whole warp walks the line, one thread issues: what steers the products stays in uniform registers.  The tensor core
+// waits for little else than this warp, so the loops are written out for either kind of group.
 template <typename T>
 __device__ void multiply_warp(Shared* sh, uint32_t q_addr, uint32_t ring_addr, const AttendParams& p, const AttendSplit& sp,
                               Line line) {
@@ -400,16 +397,16 @@ __device__ void multiply_warp(Shared* sh, uint32_t q_addr, uint32_t ring_addr, c
   const int steps = (p.cache.D + 15) / 16;
   const uint32_t tmem = sh->tmem;
   const uint32_t qk = idesc_16_f32(kBf, kAttendRows, kAttendKeys, false), wv = idesc_16_f32(kBf, kAttendRows, 16 * steps, true);
-  unsigned it = 0, segment = 0, turns[2] = {0, 0};
+  unsigned it = 0, turns[2] = {0, 0}, queries[2] = {0, 0};  // tiles, weights of an accumulator, tiles of queries
   Segment g;
   auto take = [&]() {
     const unsigned stage = it % kStages;
-    const bool ok = wait_for(sh, &sh->full[stage], (it / kStages) & 1);
+    const bool ok = mbar_wait(&sh->full[stage], (it / kStages) & 1, &sh->abort, &sh->code);
     ++it;
     return __all_sync(~0u, ok) ? static_cast<int>(stage) : -1;
   };
-  // S of warpgroup w from query tile `tile` and the keys in `stage`; last: nobody else wants them
-  auto scores = [&](int w, int tile, int stage, bool last) {
+  // S of accumulator w from query tile `tile` and the keys in `stage`; last: nobody else wants them; free: nor the queries
+  auto scores = [&](int w, int tile, int stage, bool last, bool free) {
     tc_fence_after();
     const uint32_t a = desc_low(q_addr + tile * kTileBytes, 16), b = desc_low(ring_addr + stage * kTileBytes, 16);
     if (elect_one()) {
@@ -420,10 +417,11 @@ __device__ void multiply_warp(Shared* sh, uint32_t q_addr, uint32_t ring_addr, c
       }
       tc_commit(&sh->s_full[w]);
       if (last) tc_commit(&sh->empty[stage]);
+      if (free) tc_commit(&sh->q_free[tile]);
     }
     __syncwarp();
   };
-  // O of warpgroup w, from its weights and the values in `stage`
+  // O of accumulator w, from its weights and the values in `stage`
   auto weigh = [&](int w, int stage, bool add, bool last) {
     tc_fence_after();
     const uint32_t b = desc_low(ring_addr + stage * kTileBytes, kHalfBytes);
@@ -437,26 +435,52 @@ __device__ void multiply_warp(Shared* sh, uint32_t q_addr, uint32_t ring_addr, c
     __syncwarp();
   };
   auto weights = [&](int w) {
-    return __all_sync(~0u, wait_for(sh, &sh->w_ready[w], turns[w]++ & 1));
+    return __all_sync(~0u, mbar_wait(&sh->w_ready[w], turns[w]++ & 1, &sh->abort, &sh->code));
+  };
+  auto queried = [&](int tile) {
+    return __all_sync(~0u, mbar_wait(&sh->q_ready[tile], queries[tile]++ & 1, &sh->abort, &sh->code));
   };
   while (line.next(sh, p, sp, &g)) {
-    if (!__all_sync(~0u, wait_for(sh, &sh->q_ready, segment++ & 1))) return;
-    // step x: O of warpgroup x & 1 from its weights, then S of its next tile of keys; two steps of S alone go before
     const bool two = g.tokens > sp.tile_tokens;
-    const int n = g.t1 - g.t0, stop = two ? 2 * n : n;
-    int k = 0, v = 0;
-#pragma unroll 1
-    for (int x = -2; x < stop; ++x) {
-      const int w = x & 1;
-      const bool first = !two || w == 0, last = !two || w == 1;  // to want the tile
-      if (x >= 0) {
-        if (!weights(w)) return;
-        if (first && (v = take()) < 0) return;
-        weigh(w, v, x >= 2, last);
+    const int n = g.t1 - g.t0;
+    if (!queried(0)) return;
+    if (two) {
+      int k = take();
+      if (k < 0) return;
+      scores(0, 0, k, false, n == 1);
+      if (!queried(1)) return;
+      scores(1, 1, k, true, n == 1);
+      for (int j = 0; j < n; ++j) {
+        if (!weights(0)) return;
+        const int v = take();
+        if (v < 0) return;
+        weigh(0, v, j > 0, false);
+        if (j + 1 < n) {
+          k = take();
+          if (k < 0) return;
+          scores(0, 0, k, false, j + 2 == n);
+        }
+        if (!weights(1)) return;
+        weigh(1, v, j > 0, true);
+        if (j + 1 < n) scores(1, 1, k, true, j + 2 == n);
       }
-      if ((two ? x >> 1 : x + 1) + 1 < n) {
-        if (first && (k = take()) < 0) return;
-        scores(w, two ? w : 0, k, last);
+    } else {
+      for (int w = 0; w < 2 && w < n; ++w) {
+        const int k = take();
+        if (k < 0) return;
+        scores(w, 0, k, true, n <= 2 && w + 1 == n);
+      }
+      for (int j = 0; j < n; ++j) {
+        const int w = j & 1;
+        if (!weights(w)) return;
+        const int v = take();
+        if (v < 0) return;
+        weigh(w, v, j >= 2, true);
+        if (j + 2 < n) {
+          const int k = take();
+          if (k < 0) return;
+          scores(w, 0, k, true, j + 3 == n);
+        }
       }
     }
   }
@@ -476,49 +500,81 @@ __device__ __forceinline__ uint32_t unit_offset(int row, int unit) {
   return (unit >> 3) * kHalfBytes + row * 128 + (((unit & 7) ^ (row & 7)) << 4);
 }
 
-// One warpgroup: queries into shared memory, a row's softmax, the end of a segment.
+// Rows row0 .. row0 + rows - 1 of a tile of queries into shared memory, by `threads` threads of which this is number `tid`:
+// 16 bytes each, zeros where there is no query and behind the last element.
+template <typename T>
+__device__ __forceinline__ void bring_queries(uint8_t* dst, int tile, int row0, int rows, const AttendParams& p,
+                                              const AttendSplit& sp, const Segment& g, int tid, int threads) {
+  const int G = p.group, units = (p.cache.D + 15) / 16 * 2, step = threads / units;
+  const int unit = tid % units, tile_rows = sp.tile_tokens * G, inv_group = (65536 + G - 1) / G;  // row / G, rows below 128
+  if (tid / units < step)
+#pragma unroll 2
+    for (int row = row0 + tid / units; row < row0 + rows; row += step) {
+      const int tk = row * inv_group >> 16, tok = tile * sp.tile_tokens + tk;
+      const bool is = row < tile_rows && tok < g.tokens && 8 * unit < p.cache.D;
+      const T* const src = static_cast<const T*>(p.q) + (g.s.row + g.tok0 + tok) * p.q_stride +
+                           static_cast<int64_t>(g.head * G + row - tk * G) * p.cache.D + 8 * unit;
+      copy_async(dst + unit_offset(row, unit), is ? src : static_cast<const T*>(p.q), is);
+    }
+  asm volatile("cp.async.wait_all;" ::: "memory");
+  fence_async_smem();
+}
+
+// A warp that brings every segment's queries but the first's, as soon as the products are done with the last ones, and
+// notes the group that goes on behind this stretch for the kernel that joins.
+template <typename T>
+__device__ void query_warp(Shared* sh, uint8_t* q_smem, const AttendParams& p, const AttendSplit& sp, Line line, int each) {
+  const int lane = threadIdx.x & 31;
+  unsigned queries[2] = {0, 0};
+  AttendTail tail{-1, 0, 0, 0};
+  Segment g;
+  bool ok = true;
+  for (bool start = true; line.next(sh, p, sp, &g); start = false) {
+    const bool two = g.tokens > sp.tile_tokens;
+    if (g.t0 == 0 && g.t1 < g.tiles) tail = AttendTail{(line.at + g.tiles - g.t1 - 1) / each, g.s.row + g.tok0, g.head, g.tokens};
+#pragma unroll 1
+    for (int tile = 0; tile < (two ? 2 : 1); ++tile) {
+      const unsigned use = queries[tile]++;
+      if (start || !ok) continue;
+      ok = use == 0 || wait_for(sh, &sh->q_free[tile], (use - 1) & 1);
+      ok = __all_sync(~0u, ok);
+      if (!ok) continue;
+      bring_queries<T>(q_smem + tile * kTileBytes, tile, 0, kAttendRows, p, sp, g, lane, 32);
+      warp_arrive(&sh->q_ready[tile]);
+    }
+  }
+  if (lane == 0) sp.tails[blockIdx.x] = tail;
+}
+
+// One warpgroup: a row's softmax, the end of a segment.
 template <typename T>
 __device__ void soft_group(Shared* sh, uint8_t* q_smem, uint8_t* ring, const AttendParams& p, const AttendSplit& sp, Line line) {
   const int w = threadIdx.x >> 7, r = threadIdx.x & 127, lane_base = (threadIdx.x >> 5 & 3) * 32;
-  const int D = p.cache.D, G = p.group, steps = (D + 15) / 16;
+  const int D = p.cache.D, G = p.group, steps = (D + 15) / 16, units = 2 * steps;
   const uint32_t tmem = sh->tmem + (static_cast<uint32_t>(lane_base) << 16);
   const uint32_t s_col = tmem + kS + 128 * w, o_col = tmem + kO + 128 * w;
   const float c = p.scale_log2;
   const int tile_rows = sp.tile_tokens * G;
   const int my_tok = r / G, my_head = r - my_tok * G;  // of a tile
-  const int inv_group = (65536 + G - 1) / G;             // row / G for rows below 128
-  const int units = 2 * steps, row_step = 128 / units, unit_row = r / units, unit = r - unit_row * units;
   unsigned segment = 0, turn = 0, base = 0;
+  bool crossed = false;
   Segment g;
   for (; line.next(sh, p, sp, &g); ++segment, base += 2 * (g.t1 - g.t0)) {
     const bool two = g.tokens > sp.tile_tokens;
     const int n = g.t1 - g.t0, ahead = two ? 1 : 2;
     const int tile = two ? w : 0;
-    named_bar_sync(1, kSoftThreads);  // the last segment's rows and accumulators are no longer read
-    if (threadIdx.x == 0) sh->odd[(segment + 1) & 1] = 0;
-
-    // a tile's 16-byte units, a thread one column of them: queries in, results out
-    const int rows = two ? kAttendRows : kAttendRows / 2, row0 = two ? 0 : w * rows;
-    uint8_t* const q_tile = q_smem + tile * kTileBytes;
-    auto element = [&](int row, int64_t stride) {  // of the row's first query in a [token][head][D] tensor, or -1
-      const int tk = row * inv_group >> 16, tok = tile * sp.tile_tokens + tk;
-      return row < tile_rows && tok < g.tokens
-                 ? (g.s.row + g.tok0 + tok) * stride + static_cast<int64_t>(g.head * G + row - tk * G) * D + 8 * unit
-                 : -1;
-    };
-    if (unit_row < row_step)
-#pragma unroll 2
-      for (int x = unit_row; x < rows; x += row_step) {
-        const int64_t e = element(row0 + x, p.q_stride);
-        copy_async(q_tile + unit_offset(row0 + x, unit), static_cast<const T*>(p.q) + max(e, static_cast<int64_t>(0)),
-                   e >= 0 && 8 * unit < D);
-      }
-    asm volatile("cp.async.wait_all;" ::: "memory");
-    fence_async_smem();
-    mbar_arrive(&sh->q_ready);
-
+    if (segment == 0) {  // everybody brings the first queries
+      bring_queries<T>(q_smem + tile * kTileBytes, tile, two ? 0 : 64 * w, two ? kAttendRows : 64, p, sp, g, r, 128);
+      named_bar_sync(1, kSoftThreads);
+      if (threadIdx.x == 0) mbar_arrive(&sh->q_ready[0]);
+      if (threadIdx.x == 128 && two) mbar_arrive(&sh->q_ready[1]);
+    } else if (crossed) {  // the other warpgroup has read our accumulator
+      named_bar_sync(1, kSoftThreads);
+    }
+    crossed = !two;
     const int tok = tile * sp.tile_tokens + my_tok;  // in the group
     const bool valid = r < tile_rows && tok < g.tokens;
+    const bool busy = __any_sync(~0u, valid);  // a warp without rows only keeps time: what its lanes hold reaches nobody
     const int i = g.tok0 + tok;
     const int32_t* const parent = p.mask == kMaskTree ? p.parent + static_cast<long long>(g.seq) * p.N : nullptr;
     const int from = masked_from(p, g.s, g.tok0 + tile * sp.tile_tokens);
@@ -529,79 +585,21 @@ __device__ void soft_group(Shared* sh, uint8_t* q_smem, uint8_t* ring, const Att
       const bool masked = key0 + kAttendKeys > from;
       mbar_wait(&sh->s_full[w], turn & 1, &sh->abort, &sh->code);
       tc_fence_after();
-      float s[4][32];
-#pragma unroll
-      for (int x = 0; x < 4; ++x) tc_ld_x32(s_col + 32 * x, s[x]);
-      tc_wait_ld();
-      if (masked) {
-        uint32_t bits[4] = {0, 0, 0, 0};
-        if (valid) seen_bits(p, g.s, parent, i, key0, bits);
-#pragma unroll
-        for (int x = 0; x < 4; ++x)
-#pragma unroll
-          for (int y = 0; y < 32; ++y) s[x][y] = bits[x] >> y & 1 ? s[x][y] : -INFINITY;
-      }
-      float top[4];
-#pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        top[x] = fmaxf(s[x][0], s[x][1]);
-#pragma unroll
-        for (int y = 2; y < 32; y += 2) top[x] = fmaxf(fmaxf(top[x], s[x][y]), s[x][y + 1]);
-      }
-      const float seen = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
-      if (!started) {
-        m = seen;
-      } else {
-        const float up = fmaxf(m, seen);
-        if (__any_sync(~0u, (up - m) * c > kGrowth)) {
-          const float keep = m == up ? 1.f : ex2((m - up) * c);
-          mbar_wait(&sh->o_done[w], (turn - 1) & 1, &sh->abort, &sh->code);
-          tc_fence_after();
-#pragma unroll 1
-          for (int d = 0; d < steps; ++d) {
-            float o[16];
-            tc_ld_x16(o_col + 16 * d, o);
-            tc_wait_ld();
-#pragma unroll
-            for (int x = 0; x < 16; ++x) o[x] *= keep;
-            tc_st_x16(o_col + 16 * d, o);
-          }
-          l *= keep;
-          m = up;
-        }
-      }
-      const float mc = m == -INFINITY ? 0.f : -m * c;
-      float sum[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int x = 0; x < 4; x += 2) {
-        uint32_t pk[32];
-#pragma unroll
-        for (int y = 0; y < 64; y += 2) {
-          float a = s[x + y / 32][y % 32], b = s[x + y / 32][y % 32 + 1];
-          fma2(a, b, c, mc);
-          a = ex2(a);
-          b = ex2(b);
-          add2(sum[y & 2], sum[(y & 2) + 1], a, b);
-          pk[y / 2] = pack2(a, b, T());
-        }
-        tc_st_x32(s_col + 16 * x, pk);
-      }
-      l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
       if (masked) {  // values that weights of 0 must not meet
         const unsigned place = base + value_place(j, n, ahead);
         const int stage = place % kStages, key = key0 + r;
         mbar_wait(&sh->full[stage], (place / kStages) & 1, &sh->abort, &sh->code);
         if (key >= from) {
           uint8_t* const row = ring + stage * kTileBytes + r * 128;
-#pragma unroll 1
-          for (int u = 0; u < 2 * steps; ++u) {
+#pragma unroll 2
+          for (int u = 0; u < units; ++u) {
             uint4* const at = reinterpret_cast<uint4*>(row + (u >> 3) * kHalfBytes + (((u & 7) ^ (r & 7)) << 4));
             if (key >= g.s.kv) {
               *at = make_uint4(0, 0, 0, 0);
             } else {
               uint4 v = *at;
               if (drop_odd<T>(&v.x) | drop_odd<T>(&v.y) | drop_odd<T>(&v.z) | drop_odd<T>(&v.w)) {
-                *reinterpret_cast<volatile int*>(&sh->odd[segment & 1]) = 1;
+                *reinterpret_cast<volatile unsigned*>(&sh->odd[segment & 1]) = segment + 1;
                 __threadfence_block();
                 *at = v;
               }
@@ -610,9 +608,76 @@ __device__ void soft_group(Shared* sh, uint8_t* q_smem, uint8_t* ring, const Att
         }
         fence_async_smem();
       }
-      tc_wait_st();
+      auto softmax = [&](auto Masked) {
+        constexpr bool kMasked = decltype(Masked)::value;
+        float s[4][32], top[4];
+        uint32_t bits[4] = {0, 0, 0, 0};
+#pragma unroll
+        for (int x = 0; x < 4; ++x) tc_ld_x32(s_col + 32 * x, s[x]);
+        if constexpr (kMasked) {
+          if (valid) seen_bits(p, g.s, parent, i, key0, bits);
+          __syncwarp();
+        }
+        tc_wait_ld();
+        if constexpr (kMasked) {
+#pragma unroll
+          for (int x = 0; x < 4; ++x)
+#pragma unroll
+            for (int y = 0; y < 32; ++y) s[x][y] = bits[x] >> y & 1 ? s[x][y] : -INFINITY;
+        }
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          top[x] = fmaxf(s[x][0], s[x][1]);
+#pragma unroll
+          for (int y = 2; y < 32; y += 2) top[x] = fmaxf(fmaxf(top[x], s[x][y]), s[x][y + 1]);
+        }
+        const float seen = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+        if (!started) {
+          m = seen;
+        } else {
+          const float up = fmaxf(m, seen);
+          if (__any_sync(~0u, (up - m) * c > kGrowth)) {
+            const float keep = m == up ? 1.f : ex2((m - up) * c);
+            mbar_wait(&sh->o_done[w], (turn - 1) & 1, &sh->abort, &sh->code);
+            tc_fence_after();
+#pragma unroll 1
+            for (int d = 0; d < steps; ++d) {
+              float o[16];
+              tc_ld_x16(o_col + 16 * d, o);
+              tc_wait_ld();
+#pragma unroll
+              for (int x = 0; x < 16; ++x) o[x] *= keep;
+              tc_st_x16(o_col + 16 * d, o);
+            }
+            l *= keep;
+            m = up;
+          }
+        }
+        const float mc = m == -INFINITY ? 0.f : -m * c;
+        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int x = 0; x < 4; x += 2) {
+          uint32_t pk[32];
+#pragma unroll
+          for (int y = 0; y < 64; y += 2) {
+            float a = s[x + y / 32][y % 32], b = s[x + y / 32][y % 32 + 1];
+            fma2(a, b, c, mc);
+            a = ex2(a);
+            b = ex2(b);
+            add2(sum[y & 2], sum[(y & 2) + 1], a, b);
+            pk[y / 2] = pack2(a, b, T());
+          }
+          tc_st_x32(s_col + 16 * x, pk);
+        }
+        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        tc_wait_st();
+      };
+      if (busy) {
+        if (masked) softmax(std::true_type());
+        else softmax(std::false_type());
+      }
       tc_fence_before();
-      mbar_arrive(&sh->w_ready[w]);
+      warp_arrive(&sh->w_ready[w]);
     }
 
     // the segment's end: sums into the output, or into the workspace where the group's keys go on elsewhere
@@ -632,48 +697,52 @@ __device__ void soft_group(Shared* sh, uint8_t* q_smem, uint8_t* ring, const Att
       f1 = m1 == -INFINITY ? 0.f : m1 == m ? 1.f : ex2((m1 - m) * c);
       l = sh->norm[0][1][r] * f0 + sh->norm[1][1][r] * f1;
     }
-    const bool odd = *reinterpret_cast<volatile int*>(&sh->odd[segment & 1]) != 0;
+    const bool odd = *reinterpret_cast<volatile unsigned*>(&sh->odd[segment & 1]) == segment + 1;
     const bool whole = g.t0 == 0 && g.t1 == g.tiles;
     const float inv = l == 0.f ? 0.f : 1.f / l;
     const int slot = 2 * blockIdx.x + (g.t0 == 0 ? 1 : 0), slot_row = tile * kAttendRows + r;
+    const long long row = g.s.row + i;
+    const int head = g.head * G + my_head;
+    T* const out = static_cast<T*>(p.out) + row * p.out_stride + static_cast<long long>(head) * D;
+    float* const part = sp.parts + static_cast<long long>(slot) * D * sp.slot_rows + slot_row;
+    if (busy)
 #pragma unroll 1
-    for (int d = two ? 0 : 16 * w; d < D; d += two ? 16 : 32) {
-      float o[16];
-      tc_ld_x16((two ? o_col : tmem + kO) + d, o);
-      if (two) {
-        tc_wait_ld();
-      } else {
-        float o1[16];
-        tc_ld_x16(tmem + kO + 128 + d, o1);
-        tc_wait_ld();
+      for (int d = two ? 0 : 16 * w; d < D; d += 32) {
+        float o[32];  // 32 elements, or 16 that two accumulators share
+        if (two) {
+          tc_ld_x32(o_col + d, o);
+          tc_wait_ld();
+        } else {
+          tc_ld_x16(tmem + kO + d, reinterpret_cast<float(&)[16]>(o[0]));
+          tc_ld_x16(tmem + kO + 128 + d, reinterpret_cast<float(&)[16]>(o[16]));
+          tc_wait_ld();
 #pragma unroll
-        for (int x = 0; x < 16; ++x) {
-          if (f0 == 0.f) o[x] = 0.f;
-          if (f1 == 0.f) o1[x] = 0.f;
-          o[x] = fmaf(o[x], f0, o1[x] * f1);
-        }
-      }
-      if (valid) {
-#pragma unroll
-        for (int x = 0; x < 16; x += 8) {
-          if (d + x >= D) break;
-          if (whole) {
-            float y[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) y[e] = o[x + e] * inv;
-            Vec<T> v;
-            pack(y, &v);
-            if (l == 0.f) v.raw = make_uint4(0, 0, 0, 0);
-            *reinterpret_cast<uint4*>(q_tile + unit_offset(r, (d + x) >> 3)) = v.raw;
-          } else {
-            float* const part = sp.parts + (static_cast<long long>(slot) * D + d + x) * sp.slot_rows + slot_row;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) part[e * sp.slot_rows] = o[x + e];
+          for (int x = 0; x < 16; ++x) {
+            if (f0 == 0.f) o[x] = 0.f;
+            if (f1 == 0.f) o[16 + x] = 0.f;
+            o[x] = fmaf(o[x], f0, o[16 + x] * f1);
           }
         }
+        if (valid) {
+#pragma unroll
+          for (int x = 0; x < 32; x += 8) {
+            if (d + x >= D || (x == 16 && !two)) break;
+            if (whole) {
+              float y[8];
+#pragma unroll
+              for (int e = 0; e < 8; ++e) y[e] = o[x + e] * inv;
+              Vec<T> v;
+              pack(y, &v);
+              if (l == 0.f) v.raw = make_uint4(0, 0, 0, 0);
+              *reinterpret_cast<uint4*>(out + d + x) = v.raw;
+            } else {
+#pragma unroll
+              for (int e = 0; e < 8; ++e) part[static_cast<long long>(d + x + e) * sp.slot_rows] = o[x + e];
+            }
+          }
+        }
+        __syncwarp();  // the loads of tensor memory are the whole warp's
       }
-      __syncwarp();  // the loads of tensor memory are the whole warp's
-    }
     if (odd && valid) {  // what was left out of the products, where this row sees it
       const int end = min(g.s.kv, g.t1 * kAttendKeys);
 #pragma unroll 1
@@ -686,28 +755,13 @@ __device__ void soft_group(Shared* sh, uint8_t* q_smem, uint8_t* ring, const Att
         for (int d = 0; d < D; ++d) {
           const float f = to_f32(v[d]);
           if (isfinite(f) || (!two && (d >> 4 & 1) != w)) continue;
-          if (whole) {
-            T* const at = reinterpret_cast<T*>(q_tile + unit_offset(r, d >> 3)) + (d & 7);
-            from_f32(to_f32(*at) + f, at);
-          } else {
-            sp.parts[(static_cast<long long>(slot) * D + d) * sp.slot_rows + slot_row] += f;
-          }
+          if (whole)
+            from_f32(to_f32(out[d]) + f, out + d);
+          else
+            part[static_cast<long long>(d) * sp.slot_rows] += f;
         }
       }
     }
-    if (whole) {  // the results lie where the queries were: rows out side by side
-      if (two) named_bar_sync(2 + w, 128); else named_bar_sync(1, kSoftThreads);
-      if (unit_row < row_step && 8 * unit < D)
-#pragma unroll 2
-        for (int x = unit_row; x < rows; x += row_step) {
-          const int64_t e = element(row0 + x, p.out_stride);
-          if (e >= 0)
-            *reinterpret_cast<uint4*>(static_cast<T*>(p.out) + e) =
-                *reinterpret_cast<const uint4*>(q_tile + unit_offset(row0 + x, unit));
-        }
-    }
-    const long long row = g.s.row + i;
-    const int head = g.head * G + my_head;
     if (valid && (two || w == 0)) {
       if (!whole) {
         float* const norm = sp.norms + static_cast<long long>(slot) * 2 * sp.slot_rows + slot_row;
@@ -720,8 +774,6 @@ __device__ void soft_group(Shared* sh, uint8_t* q_smem, uint8_t* ring, const Att
     tc_fence_before();
   }
 }
-
-__device__ __forceinline__ long long stretch(long long units, int ctas) { return quotient(units + ctas - 1, ctas); }
 
 template <typename T>
 __global__ void __launch_bounds__(kThreads, 1)
@@ -739,11 +791,12 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&sh->s_full[i], 1);
-      mbar_init(&sh->w_ready[i], 128);
+      mbar_init(&sh->w_ready[i], 4);  // a warp each
       mbar_init(&sh->o_done[i], 1);
+      mbar_init(&sh->q_ready[i], 1);
+      mbar_init(&sh->q_free[i], 1);
       sh->odd[i] = 0;
     }
-    mbar_init(&sh->q_ready, kSoftThreads);
     fence_mbar_init();
     sh->abort = 0;
     sh->code = 0;
@@ -760,7 +813,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll 1
   for (int b = tid; b < p.batch.B; b += kThreads) {
     const Sequence s = load_sequence(p.cache, p.batch, p.tokens, b);
-    const long long n = sequence_units(p, sp, s);
+    const int n = sequence_units(p, sp, s);
     several = several || n < 0;
     sh->seq[b] = s;
     sh->before[b + 1] = n;
@@ -775,9 +828,9 @@ __global__ void __launch_bounds__(kThreads, 1)
     for (int b = warp; b < p.batch.B; b += kThreads / 32) {
       if (sh->before[b + 1] >= 0) continue;
       const Sequence s = sh->seq[b];
-      long long n = 0;
+      int n = 0;
 #pragma unroll 1
-      for (int t = lane * step; t < s.n; t += 32 * step) n += kGroupCost + key_tiles(p.mask, s, min(t + step, s.n));
+      for (int t = lane * step; t < s.n; t += 32 * step) n += kAttendGroupCost + key_tiles(p.mask, s, min(t + step, s.n));
 #pragma unroll
       for (int o = 16; o; o >>= 1) n += __shfl_xor_sync(~0u, n, o);
       __syncwarp();
@@ -786,13 +839,13 @@ __global__ void __launch_bounds__(kThreads, 1)
     __syncthreads();
   }
   if (warp == 0) {
-    long long carry = 0;
+    int carry = 0;
 #pragma unroll 1
     for (int b = 0; b < p.batch.B; b += 32) {
-      long long x = b + tid < p.batch.B ? sh->before[b + tid + 1] : 0;
+      int x = b + tid < p.batch.B ? sh->before[b + tid + 1] : 0;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
-        const long long y = __shfl_up_sync(~0u, x, o);
+        const int y = __shfl_up_sync(~0u, x, o);
         if (tid >= o) x += y;
       }
       x += carry;
@@ -801,9 +854,10 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
   }
   __syncthreads();
-  const long long units = sh->before[p.batch.B], each = stretch(units, gridDim.x);
+  const int units = sh->before[p.batch.B], each = (units - 1) / gridDim.x + 1;
+  const int from = blockIdx.x < (units + each - 1) / each ? blockIdx.x * each : units;
   Line line;
-  line.begin(sh, p, sp, min(units, blockIdx.x * each), min(units, (blockIdx.x + 1) * each));
+  line.begin(sh, p, sp, from, from + min(each, units - from));
   if (tid < kSoftThreads) {
     regs_up<kSoftRegs>();
     soft_group<T>(sh, tiles, ring, p, sp, line);
@@ -821,15 +875,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
       }
     }
-    if (tid == kSoftThreads + 96) {
-      // the last group of this stretch that goes on: where, for the kernel that joins
-      AttendTail tail{-1, 0, 0, 0};
-      Segment g;
-      while (line.next(sh, p, sp, &g))
-        if (g.t0 == 0 && g.t1 < g.tiles)
-          tail = AttendTail{static_cast<int>(quotient(line.at + g.tiles - g.t1 - 1, each)), g.s.row + g.tok0, g.head, g.tokens};
-      sp.tails[blockIdx.x] = tail;
-    }
+    if (warp == kSoftThreads / 32 + 3) query_warp<T>(sh, tiles, p, sp, line, each);
   }
   __syncwarp();
   tc_fence_before();

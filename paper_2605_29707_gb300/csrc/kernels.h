@@ -373,6 +373,7 @@ struct AttendParams {
 constexpr int kAttendKeys = 128;   // keys a tile
 constexpr int kAttendRows = 128;   // queries a tile
 constexpr int kAttendSeqs = 1024;  // sequences a launch
+constexpr int kAttendGroupCost = 3;  // what a group of queries costs beside its tiles of keys, in such tiles
 struct AttendTail {  // a group of queries whose keys go on behind the CTA that began them
   int last;          // the CTA that ends them, -1: none
   int row, head, tokens;
