@@ -1362,7 +1362,7 @@ int enqueue_attend_tc(const dm::AttendParams& a, const domino_kv_cache& c, int s
     // at most this much work: fewer CTAs where there is less of it than SMs
     const long long groups = a.tokens / (2 * plan.tile_tokens) + part.batch.B;
     const long long tiles = static_cast<long long>(a.batch.table_width) * c.page / dm::kAttendKeys + 1;
-    const double units = static_cast<double>(groups) * (tiles + dm::kAttendGroupCost) * c.heads;
+    const double units = static_cast<double>(groups) * (tiles * dm::kAttendTwoCost + dm::kAttendGroupCost) * c.heads;
     if (units > 2e9) return DOMINO_ERR_UNSUPPORTED;  // counted in 32 bits
     const int rc = cuda_rc(dm::launch_attend_tc(keys, values, part, s, c.dtype, units < sms ? static_cast<int>(units) : sms, st));
     if (rc != DOMINO_OK) return rc;

@@ -187,12 +187,23 @@ struct Segment {
   int seq, head;
   int tok0, tokens;    // the group's, in the sequence
   int t0, t1, tiles;   // tiles of keys here, of all
+  int last;            // the unit at which the last tile begins
 };
 
-// A CTA's stretch of the line.  A group of queries counts kAttendGroupCost units and one a tile of keys.
+// What a group from token tok0 on counts: kAttendGroupCost for its queries and its end, and for every tile of keys what
+// two tiles of queries, or one, cost there.
+__device__ __forceinline__ int tile_cost(const AttendSplit& sp, int tokens) {
+  return tokens > sp.tile_tokens ? kAttendTwoCost : kAttendOneCost;
+}
+__device__ __forceinline__ int group_units(const AttendParams& p, const AttendSplit& sp, const Sequence& s, int tok0) {
+  const int tokens = min(2 * sp.tile_tokens, s.n - tok0);
+  return kAttendGroupCost + key_tiles(p.mask, s, tok0 + tokens) * tile_cost(sp, tokens);
+}
+
+// A CTA's stretch of the line.  A tile of keys belongs to the stretch in which it begins.
 struct Line {
   int at, end;
-  int seq, head, tok0, t;  // t: the tile at `at`, negative in the units before the first
+  int seq, head, tok0, u;  // u: units of the group before `at`
 
   __device__ __forceinline__ void begin(const Shared* sh, const AttendParams& p, const AttendSplit& sp, int from, int to) {
     at = from;
@@ -206,43 +217,41 @@ struct Line {
     }
     seq = lo;
     const int each = (sh->before[lo + 1] - sh->before[lo]) / p.cache.heads;
-    int rest = at - sh->before[lo];
-    head = rest / each;
-    rest -= head * each;
+    u = at - sh->before[lo];
+    head = u / each;
+    u -= head * each;
     const Sequence s = sh->seq[seq];
     const int step = 2 * sp.tile_tokens, groups = (s.n + step - 1) / step;
     int g = 0;
-    if (p.mask != kMaskCausal) {
-      const int n = kAttendGroupCost + key_tiles(p.mask, s, s.n);
-      g = rest / n;
-      rest -= g * n;
-    } else if (groups > 1) {  // every lane of the warp adds up a part of them; the one where `rest` lies goes through its own
+    if (groups > 1 && p.mask != kMaskCausal) {  // all but the last alike
+      const int n = group_units(p, sp, s, 0);
+      g = min(u / n, groups - 1);
+      u -= g * n;
+    } else if (groups > 1) {  // every lane of the warp adds up a part of them; the one where u lies goes through its own
       const int lane = threadIdx.x & 31, share = (groups + 31) / 32;
       const int mine = min(groups, lane * share), stop = min(groups, mine + share);
       int sum = 0;
 #pragma unroll 1
-      for (int i = mine; i < stop; ++i) sum += kAttendGroupCost + key_tiles(p.mask, s, min((i + 1) * step, s.n));
+      for (int i = mine; i < stop; ++i) sum += group_units(p, sp, s, i * step);
       int upto = sum;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
         const int y = __shfl_up_sync(~0u, upto, o);
         if (lane >= o) upto += y;
       }
-      const int owner = __ffs(__ballot_sync(~0u, rest < upto)) - 1;
-      rest -= __shfl_sync(~0u, upto - sum, owner);
+      const int owner = __ffs(__ballot_sync(~0u, u < upto)) - 1;
+      u -= __shfl_sync(~0u, upto - sum, owner);
 #pragma unroll 1
       for (g = owner * share;; ++g) {
-        const int n = kAttendGroupCost + key_tiles(p.mask, s, min((g + 1) * step, s.n));
-        if (rest < n) break;
-        rest -= n;
+        const int n = group_units(p, sp, s, g * step);
+        if (u < n) break;
+        u -= n;
       }
     }
     tok0 = g * step;
-    t = rest - kAttendGroupCost;
   }
 
   __device__ __forceinline__ bool next(const Shared* sh, const AttendParams& p, const AttendSplit& sp, Segment* g) {
-    const int step = 2 * sp.tile_tokens;
 #pragma unroll 1
     while (at < end) {
       while (sh->seq[seq].n == 0) ++seq;
@@ -250,16 +259,18 @@ struct Line {
       g->seq = seq;
       g->head = head;
       g->tok0 = tok0;
-      g->tokens = min(step, g->s.n - tok0);
+      g->tokens = min(2 * sp.tile_tokens, g->s.n - tok0);
       g->tiles = key_tiles(p.mask, g->s, tok0 + g->tokens);
-      const int n = min(g->tiles - t, end - at);
-      g->t0 = max(t, 0);
+      const int cost = tile_cost(sp, g->tokens), all = kAttendGroupCost + g->tiles * cost;
+      const int n = min(all - u, end - at);
+      g->t0 = (max(u - kAttendGroupCost, 0) + cost - 1) / cost;
+      u += n;
       at += n;
-      t += n;
-      g->t1 = t;
-      if (t == g->tiles) {
-        t = -kAttendGroupCost;
-        tok0 += step;
+      g->t1 = (max(u - kAttendGroupCost, 0) + cost - 1) / cost;
+      g->last = at - u + all - cost;
+      if (u == all) {
+        u = 0;
+        tok0 += 2 * sp.tile_tokens;
         if (tok0 >= g->s.n) {
           tok0 = 0;
           if (++head == p.cache.heads) {
@@ -276,9 +287,10 @@ struct Line {
 
 // A sequence's units; -1 where a causal one has several groups, each of its own length.
 __device__ __forceinline__ int sequence_units(const AttendParams& p, const AttendSplit& sp, const Sequence& s) {
-  const int groups = (s.n + 2 * sp.tile_tokens - 1) / (2 * sp.tile_tokens);
+  const int step = 2 * sp.tile_tokens, groups = (s.n + step - 1) / step;
   if (p.mask == kMaskCausal && groups > 1) return -1;
-  return groups * (kAttendGroupCost + key_tiles(p.mask, s, s.n)) * p.cache.heads;
+  if (groups == 0) return 0;
+  return ((groups - 1) * group_units(p, sp, s, 0) + group_units(p, sp, s, (groups - 1) * step)) * p.cache.heads;
 }
 
 // The first key that some token from tok0 on may not see.
@@ -531,7 +543,7 @@ __device__ void query_warp(Shared* sh, uint8_t* q_smem, const AttendParams& p, c
   bool ok = true;
   for (bool start = true; line.next(sh, p, sp, &g); start = false) {
     const bool two = g.tokens > sp.tile_tokens;
-    if (g.t0 == 0 && g.t1 < g.tiles) tail = AttendTail{(line.at + g.tiles - g.t1 - 1) / each, g.s.row + g.tok0, g.head, g.tokens};
+    if (g.t0 == 0 && g.t1 < g.tiles) tail = AttendTail{g.last / each, g.s.row + g.tok0, g.head, g.tokens};
 #pragma unroll 1
     for (int tile = 0; tile < (two ? 2 : 1); ++tile) {
       const unsigned use = queries[tile]++;
@@ -587,22 +599,20 @@ __device__ void soft_group(Shared* sh, uint8_t* q_smem, uint8_t* ring, const Att
       tc_fence_after();
       if (masked) {  // values that weights of 0 must not meet
         const unsigned place = base + value_place(j, n, ahead);
-        const int stage = place % kStages, key = key0 + r;
+        const int stage = place % kStages, row0 = max(from - key0, 0);
         mbar_wait(&sh->full[stage], (place / kStages) & 1, &sh->abort, &sh->code);
-        if (key >= from) {
-          uint8_t* const row = ring + stage * kTileBytes + r * 128;
-#pragma unroll 2
-          for (int u = 0; u < units; ++u) {
-            uint4* const at = reinterpret_cast<uint4*>(row + (u >> 3) * kHalfBytes + (((u & 7) ^ (r & 7)) << 4));
-            if (key >= g.s.kv) {
-              *at = make_uint4(0, 0, 0, 0);
-            } else {
-              uint4 v = *at;
-              if (drop_odd<T>(&v.x) | drop_odd<T>(&v.y) | drop_odd<T>(&v.z) | drop_odd<T>(&v.w)) {
-                *reinterpret_cast<volatile unsigned*>(&sh->odd[segment & 1]) = segment + 1;
-                __threadfence_block();
-                *at = v;
-              }
+#pragma unroll 1
+        for (int x = r; x < (kAttendKeys - row0) * units; x += 128) {
+          const int row = row0 + x / units, unit = x % units;
+          uint4* const at = reinterpret_cast<uint4*>(ring + stage * kTileBytes + unit_offset(row, unit));
+          if (key0 + row >= g.s.kv) {
+            *at = make_uint4(0, 0, 0, 0);
+          } else {
+            uint4 v = *at;
+            if (drop_odd<T>(&v.x) | drop_odd<T>(&v.y) | drop_odd<T>(&v.z) | drop_odd<T>(&v.w)) {
+              *reinterpret_cast<volatile unsigned*>(&sh->odd[segment & 1]) = segment + 1;
+              __threadfence_block();
+              *at = v;
             }
           }
         }
@@ -705,28 +715,30 @@ __device__ void soft_group(Shared* sh, uint8_t* q_smem, uint8_t* ring, const Att
     const int head = g.head * G + my_head;
     T* const out = static_cast<T*>(p.out) + row * p.out_stride + static_cast<long long>(head) * D;
     float* const part = sp.parts + static_cast<long long>(slot) * D * sp.slot_rows + slot_row;
+    const int share = two ? 0 : w, shares = two ? 1 : 2;  // of the blocks of 16 elements
     if (busy)
 #pragma unroll 1
-      for (int d = two ? 0 : 16 * w; d < D; d += 32) {
-        float o[32];  // 32 elements, or 16 that two accumulators share
+      for (int d = 16 * share; d < D; d += 16 * shares) {
+        float o[16];
         if (two) {
-          tc_ld_x32(o_col + d, o);
+          tc_ld_x16(o_col + d, o);
           tc_wait_ld();
         } else {
-          tc_ld_x16(tmem + kO + d, reinterpret_cast<float(&)[16]>(o[0]));
-          tc_ld_x16(tmem + kO + 128 + d, reinterpret_cast<float(&)[16]>(o[16]));
+          float o1[16];
+          tc_ld_x16(tmem + kO + d, o);
+          tc_ld_x16(tmem + kO + 128 + d, o1);
           tc_wait_ld();
 #pragma unroll
           for (int x = 0; x < 16; ++x) {
             if (f0 == 0.f) o[x] = 0.f;
-            if (f1 == 0.f) o[16 + x] = 0.f;
-            o[x] = fmaf(o[x], f0, o[16 + x] * f1);
+            if (f1 == 0.f) o1[x] = 0.f;
+            o[x] = fmaf(o[x], f0, o1[x] * f1);
           }
         }
         if (valid) {
 #pragma unroll
-          for (int x = 0; x < 32; x += 8) {
-            if (d + x >= D || (x == 16 && !two)) break;
+          for (int x = 0; x < 16; x += 8) {
+            if (d + x >= D) break;
             if (whole) {
               float y[8];
 #pragma unroll
@@ -754,7 +766,7 @@ __device__ void soft_group(Shared* sh, uint8_t* q_smem, uint8_t* ring, const Att
 #pragma unroll 1
         for (int d = 0; d < D; ++d) {
           const float f = to_f32(v[d]);
-          if (isfinite(f) || (!two && (d >> 4 & 1) != w)) continue;
+          if (isfinite(f) || (d >> 4) % shares != share) continue;
           if (whole)
             from_f32(to_f32(out[d]) + f, out + d);
           else
@@ -830,7 +842,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       const Sequence s = sh->seq[b];
       int n = 0;
 #pragma unroll 1
-      for (int t = lane * step; t < s.n; t += 32 * step) n += kAttendGroupCost + key_tiles(p.mask, s, min(t + step, s.n));
+      for (int t = lane * step; t < s.n; t += 32 * step) n += group_units(p, sp, s, t);
 #pragma unroll
       for (int o = 16; o; o >>= 1) n += __shfl_xor_sync(~0u, n, o);
       __syncwarp();
@@ -854,8 +866,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
   }
   __syncthreads();
-  const int units = sh->before[p.batch.B], each = (units - 1) / gridDim.x + 1;
-  const int from = blockIdx.x < (units + each - 1) / each ? blockIdx.x * each : units;
+  const int units = sh->before[p.batch.B], each = max(kAttendLeast, (units + static_cast<int>(gridDim.x) - 1) / static_cast<int>(gridDim.x));
+  const int from = static_cast<int>(blockIdx.x) < (units + each - 1) / each ? static_cast<int>(blockIdx.x) * each : units;
   Line line;
   line.begin(sh, p, sp, from, from + min(each, units - from));
   if (tid < kSoftThreads) {
