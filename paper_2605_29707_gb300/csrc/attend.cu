@@ -346,7 +346,7 @@ __device__ void load_warp(Shared* sh, uint8_t* ring, const CUtensorMap* map, boo
   const bool two_halves = p.cache.D > 64;
   const uint32_t bytes = two_halves ? kTileBytes : kHalfBytes;
   const int pages_on = kAttendKeys / page_size, places_on = kAttendKeys % page_size;
-  const uint64_t policy = l2_policy_evict_normal();
+  const uint64_t keep = l2_policy_evict_last(), drop = l2_policy_evict_first();
   unsigned base = 0, used[kStages] = {};  // used: our last copy into a stage, plus 1
   Segment g;
   bool ok = true;
@@ -357,6 +357,8 @@ __device__ void load_warp(Shared* sh, uint8_t* ring, const CUtensorMap* map, boo
     auto look = [&]() {  // past the last page where there is nothing: reads as zeros
       return lane < pieces && static_cast<unsigned>(place) < static_cast<unsigned>(g.s.kv) ? table[entry] : p.cache.pages;
     };
+    // the next group of queries reads the same tiles
+    const uint64_t policy = g.tok0 + g.tokens < g.s.n ? keep : drop;
     int found = look();
     for (int j = 0; j < n; ++j) {
       int page = found;
@@ -568,6 +570,7 @@ __device__ void soft_group(Shared* sh, uint8_t* q_smem, uint8_t* ring, const Att
   const float c = p.scale_log2;
   const int tile_rows = sp.tile_tokens * G;
   const int my_tok = r / G, my_head = r - my_tok * G;  // of a tile
+  const int row_step = 128 / units, unit_row = r / units, unit = r - unit_row * units;  // 16 bytes a thread
   unsigned segment = 0, turn = 0, base = 0;
   bool crossed = false;
   Segment g;
@@ -597,27 +600,6 @@ __device__ void soft_group(Shared* sh, uint8_t* q_smem, uint8_t* ring, const Att
       const bool masked = key0 + kAttendKeys > from;
       mbar_wait(&sh->s_full[w], turn & 1, &sh->abort, &sh->code);
       tc_fence_after();
-      if (masked) {  // values that weights of 0 must not meet
-        const unsigned place = base + value_place(j, n, ahead);
-        const int stage = place % kStages, row0 = max(from - key0, 0);
-        mbar_wait(&sh->full[stage], (place / kStages) & 1, &sh->abort, &sh->code);
-#pragma unroll 1
-        for (int x = r; x < (kAttendKeys - row0) * units; x += 128) {
-          const int row = row0 + x / units, unit = x % units;
-          uint4* const at = reinterpret_cast<uint4*>(ring + stage * kTileBytes + unit_offset(row, unit));
-          if (key0 + row >= g.s.kv) {
-            *at = make_uint4(0, 0, 0, 0);
-          } else {
-            uint4 v = *at;
-            if (drop_odd<T>(&v.x) | drop_odd<T>(&v.y) | drop_odd<T>(&v.z) | drop_odd<T>(&v.w)) {
-              *reinterpret_cast<volatile unsigned*>(&sh->odd[segment & 1]) = segment + 1;
-              __threadfence_block();
-              *at = v;
-            }
-          }
-        }
-        fence_async_smem();
-      }
       auto softmax = [&](auto Masked) {
         constexpr bool kMasked = decltype(Masked)::value;
         float s[4][32], top[4];
@@ -685,6 +667,28 @@ __device__ void soft_group(Shared* sh, uint8_t* q_smem, uint8_t* ring, const Att
       if (busy) {
         if (masked) softmax(std::true_type());
         else softmax(std::false_type());
+      }
+      if (masked) {  // values that weights of 0 must not meet
+        const unsigned place = base + value_place(j, n, ahead);
+        const int stage = place % kStages, row0 = max(from - key0, 0);
+        mbar_wait(&sh->full[stage], (place / kStages) & 1, &sh->abort, &sh->code);
+        if (unit_row < row_step)
+#pragma unroll 2
+          for (int row = row0 + unit_row; row < kAttendKeys; row += row_step) {
+            uint4* const at = reinterpret_cast<uint4*>(ring + stage * kTileBytes + unit_offset(row, unit));
+            if (key0 + row >= g.s.kv) {
+              *at = make_uint4(0, 0, 0, 0);
+            } else {
+              uint4 v = *at;
+              if (drop_odd<T>(&v.x) | drop_odd<T>(&v.y) | drop_odd<T>(&v.z) | drop_odd<T>(&v.w)) {
+                *reinterpret_cast<volatile unsigned*>(&sh->odd[segment & 1]) = segment + 1;
+                __threadfence_block();
+                *at = v;
+              }
+            }
+          }
+        fence_async_smem();
+        __syncwarp();
       }
       tc_fence_before();
       warp_arrive(&sh->w_ready[w]);
