@@ -41,17 +41,32 @@ constexpr int kTileBytes = 2 * kHalfBytes;
 constexpr int kSoftThreads = 256;
 constexpr int kThreads = kSoftThreads + 128;  // and two warps for keys and values, one for queries, one that multiplies
 // Registers a thread: 168 at launch (384 threads share 65536); rows of 128 scores take more, the other warps less:
-// 2 x 128 x 216 + 128 x 72 = 384 x 168.
-constexpr int kSoftRegs = 200, kOtherRegs = 104;
+// 2 x 128 x 192 + 128 x 120 = 384 x 168.
+constexpr int kSoftRegs = 192, kOtherRegs = 120;
 constexpr int kS = 0, kO = 256;     // tensor memory columns: S of warpgroup w at 128 w, O at 256 + 128 w
 constexpr float kGrowth = 8.f;      // log2 of what a maximum may grow before O is scaled
 
+constexpr int kSegments = 2;        // segments described ahead
+constexpr int kTreeWords = 3;       // a token's ancestors among the first 96 new tokens, a bit each
+constexpr int kConsumers = kSoftThreads / 32 + 3;  // warps that follow the segments: the softmax's, two loads, the products
+
+struct Segment {
+  Sequence s;
+  int seq, head;
+  int tok0, tokens;    // the group's, in the sequence
+  int t0, t1, tiles;   // tiles of keys here, of all; none: the end of the line
+  int last;            // the unit at which the last tile begins
+};
+
 struct Shared {
-  uint64_t full[kStages], empty[kStages], s_full[2], w_ready[2], o_done[2], q_ready[2], q_free[2];
+  uint64_t full[kStages], empty[kStages], s_full[2], w_ready[2], o_done[2], q_ready[2], q_free[2], seg_ready[kSegments],
+      seg_done[kSegments], met;
   uint32_t tmem;
   int abort, code;
   unsigned odd[2];  // by the segment's parity: the segment, from 1 on, that met a value that is not finite in a masked tile
-  float norm[2][2][kAttendRows];  // warpgroup: maximum, sum
+  float norm[2][2][kAttendRows];  // accumulator: maximum, sum
+  Segment seg[kSegments];
+  uint32_t above[kSegments][2 * kAttendRows][kTreeWords];  // a tree's tokens: themselves and their ancestors
   int before[kAttendSeqs + 1];  // units of work before a sequence
   Sequence seq[kAttendSeqs];
 };
@@ -132,15 +147,6 @@ __device__ __forceinline__ void warp_arrive(uint64_t* bar) {
 }
 __device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
-// mbar_wait with its loop out of line: the kernel waits in many places, and code that fits the instruction cache counts
-// (145 KB of it made the end of a segment take 6000 cycles).
-__device__ __noinline__ bool wait_long(uint64_t* bar, uint32_t parity, int* abort, int* code) {
-  return mbar_wait(bar, parity, abort, code);
-}
-__device__ __forceinline__ bool wait_for(Shared* sh, uint64_t* bar, uint32_t parity) {
-  return mbar_try_wait(bar, parity) || wait_long(bar, parity, &sh->abort, &sh->code);
-}
-
 template <int N>
 __device__ __forceinline__ void regs_up() {
   asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N));
@@ -181,14 +187,6 @@ __device__ __forceinline__ int key_tiles(int mask, const Sequence& s, int last) 
   const int seen = mask == kMaskCausal ? min(max(s.kv - s.n + last, 0), s.kv) : s.kv;
   return max(1, seen / kAttendKeys + (seen % kAttendKeys != 0));
 }
-
-struct Segment {
-  Sequence s;
-  int seq, head;
-  int tok0, tokens;    // the group's, in the sequence
-  int t0, t1, tiles;   // tiles of keys here, of all
-  int last;            // the unit at which the last tile begins
-};
 
 // What a group from token tok0 on counts: kAttendGroupCost for its queries and its end, and for every tile of keys what
 // two tiles of queries, or one, cost there.
@@ -299,12 +297,17 @@ __device__ __forceinline__ int masked_from(const AttendParams& p, const Sequence
   return min(max(s.kv - s.n + (p.mask == kMaskCausal ? tok0 + 1 : 0), 0), s.kv);
 }
 
+// Whether a tree's tokens have their ancestors in `above`.
+__device__ __forceinline__ bool tree_in_words(const AttendParams& p, const Segment& g) {
+  return p.mask == kMaskTree && g.s.n <= 32 * kTreeWords;
+}
+
 // Which of 128 keys from key0 on token i sees, a bit each.
-__device__ __forceinline__ void seen_bits(const AttendParams& p, const Sequence& s, const int32_t* parent, int i, int key0,
+__device__ __forceinline__ void seen_bits(const AttendParams& p, const Segment& g, const uint32_t* above, int i, int key0,
                                           uint32_t (&bits)[4]) {
-  const int first = s.kv - s.n;
-  int limit = s.kv;  // every key below it is seen
-  if (p.mask == kMaskCausal) limit = min(max(first + i + 1, 0), s.kv);
+  const int first = g.s.kv - g.s.n;
+  int limit = g.s.kv;  // every key below it is seen
+  if (p.mask == kMaskCausal) limit = min(max(first + i + 1, 0), g.s.kv);
   if (p.mask == kMaskTree) limit = i > p.N ? 0 : max(first, 0);
 #pragma unroll
   for (int w = 0; w < 4; ++w) {
@@ -312,7 +315,18 @@ __device__ __forceinline__ void seen_bits(const AttendParams& p, const Sequence&
     bits[w] = n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1;
   }
   if (p.mask != kMaskTree || i > p.N) return;
-  for (int a = i;;) {
+  if (tree_in_words(p, g)) {  // (places before 0 are nobody's)
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const int t = key0 + 32 * w - first, word = t >> 5;  // the word of keys begins at new token t
+      const uint32_t lo = word >= 0 && word < kTreeWords ? above[word] : 0;
+      const uint32_t hi = word >= -1 && word < kTreeWords - 1 ? above[word + 1] : 0;
+      bits[w] |= __funnelshift_r(lo, hi, t & 31);
+    }
+    return;
+  }
+  const int32_t* const parent = p.parent + static_cast<long long>(g.seq) * p.N;
+  for (int a = i;; a = tree_up(parent, a)) {
     const int at = first + a - key0;
     if (at < 0) break;
     const uint32_t bit = 1u << (at & 31);
@@ -320,7 +334,6 @@ __device__ __forceinline__ void seen_bits(const AttendParams& p, const Sequence&
     for (int w = 0; w < 4; ++w)
       if (at >> 5 == w) bits[w] |= bit;
     if (a == 0) break;
-    a = tree_up(parent, a);
   }
 }
 
@@ -332,6 +345,18 @@ __device__ __forceinline__ void drain_wait(uint64_t* bar, uint32_t parity) {
 }
 
 // ---------------------------------------------------------------- warps
+// The whole warp waits; false: somebody has given up.
+__device__ __forceinline__ bool warp_wait(Shared* sh, uint64_t* bar, uint32_t parity) {
+  return __all_sync(~0u, mbar_wait(bar, parity, &sh->abort, &sh->code));
+}
+// The warp's segment number `index`, or nullptr at the end of the line.
+__device__ __forceinline__ const Segment* next_segment(Shared* sh, unsigned index) {
+  if (!warp_wait(sh, &sh->seg_ready[index % kSegments], index / kSegments & 1)) return nullptr;
+  const Segment* const g = &sh->seg[index % kSegments];
+  return g->t1 > g->t0 ? g : nullptr;
+}
+__device__ __forceinline__ void segment_done(Shared* sh, unsigned index) { warp_arrive(&sh->seg_done[index % kSegments]); }
+
 // Tiles of a segment with n of them pass the ring as K_0 .. K_(a-1), then V_j and K_(j+a) in turn: the order in which the
 // products want them, a = 1 where both warpgroups take every tile, 2 where they alternate.
 __device__ __forceinline__ int value_place(int j, int n, int ahead) { return min(ahead, n) + j + min(j, max(0, n - ahead)); }
@@ -340,7 +365,7 @@ __device__ __forceinline__ int key_place(int j, int n, int ahead) { return j < a
 // One warp brings the keys, one the values: a copy a piece (what a page has in common with a tile) and half of the
 // elements.  A lane a piece keeps the piece's place and looks its page up a tile ahead.
 __device__ void load_warp(Shared* sh, uint8_t* ring, const CUtensorMap* map, bool values, const AttendParams& p,
-                          const AttendSplit& sp, Line line) {
+                          const AttendSplit& sp) {
   const int lane = threadIdx.x & 31;
   const int pieces = kAttendKeys / sp.piece, page_size = p.cache.page;
   const bool two_halves = p.cache.D > 64;
@@ -348,22 +373,21 @@ __device__ void load_warp(Shared* sh, uint8_t* ring, const CUtensorMap* map, boo
   const int pages_on = kAttendKeys / page_size, places_on = kAttendKeys % page_size;
   const uint64_t keep = l2_policy_evict_last(), drop = l2_policy_evict_first();
   unsigned base = 0, used[kStages] = {};  // used: our last copy into a stage, plus 1
-  Segment g;
   bool ok = true;
-  while (ok && line.next(sh, p, sp, &g)) {
-    const int n = g.t1 - g.t0, ahead = g.tokens > sp.tile_tokens ? 1 : 2;
-    const int32_t* const table = p.batch.table + g.seq * p.batch.table_stride;
-    int place = g.t0 * kAttendKeys + lane * sp.piece, entry = place / page_size, token = place - entry * page_size;
-    auto look = [&]() {  // past the last page where there is nothing: reads as zeros
-      return lane < pieces && static_cast<unsigned>(place) < static_cast<unsigned>(g.s.kv) ? table[entry] : p.cache.pages;
-    };
-    // the next group of queries reads the same tiles
-    const uint64_t policy = g.tok0 + g.tokens < g.s.n ? keep : drop;
-    int found = look();
+  const Segment* g;
+  for (unsigned index = 0; ok && (g = next_segment(sh, index)) != nullptr; ++index) {
+    const int n = g->t1 - g->t0, ahead = g->tokens > sp.tile_tokens ? 1 : 2, kv = g->s.kv, head = g->head;
+    const int32_t* const table = p.batch.table + g->seq * p.batch.table_stride;
+    const uint64_t policy = g->tok0 + g->tokens < g->s.n ? keep : drop;  // the next group of queries reads the same tiles
+    int place = g->t0 * kAttendKeys + lane * sp.piece, entry = place / page_size, token = place - entry * page_size;
+    auto inside = [&]() { return lane < pieces && static_cast<unsigned>(place) < static_cast<unsigned>(kv); };
+    int found = inside() ? table[entry] : 0;
     for (int j = 0; j < n; ++j) {
       int page = found;
       const int here = token;
-      if (page < 0 || page > p.cache.pages || (page == p.cache.pages && lane < pieces && place < g.s.kv)) {
+      if (!inside()) {
+        page = p.cache.pages;  // past the last page: reads as zeros
+      } else if (page < 0 || page >= p.cache.pages) {
         sh->code = kStatusBadPage;
         page = p.cache.pages;
       }
@@ -374,11 +398,10 @@ __device__ void load_warp(Shared* sh, uint8_t* ring, const CUtensorMap* map, boo
         token -= page_size;
         ++entry;
       }
-      if (j + 1 < n) found = look();
+      if (j + 1 < n && inside()) found = table[entry];
       const unsigned at = base + (values ? value_place(j, n, ahead) : key_place(j, n, ahead));
       const int stage = at % kStages;
-      ok = at < kStages || wait_for(sh, &sh->empty[stage], (at / kStages - 1) & 1);
-      ok = __all_sync(~0u, ok);
+      ok = at < kStages || warp_wait(sh, &sh->empty[stage], (at / kStages - 1) & 1);
       if (!ok) break;
       uint8_t* dst = ring + stage * kTileBytes;
       if (elect_one()) mbar_arrive_expect_tx(&sh->full[stage], bytes);
@@ -387,37 +410,36 @@ __device__ void load_warp(Shared* sh, uint8_t* ring, const CUtensorMap* map, boo
       for (int q = 0; q < pieces; ++q, dst += sp.piece * 128) {
         const int y = __shfl_sync(~0u, here, q), w = __shfl_sync(~0u, page, q);
         if (elect_one()) {
-          tma_load_4d(dst, map, &sh->full[stage], 0, y, g.head, w, policy);
-          if (two_halves) tma_load_4d(dst + kHalfBytes, map, &sh->full[stage], 64, y, g.head, w, policy);
+          tma_load_4d(dst, map, &sh->full[stage], 0, y, head, w, policy);
+          if (two_halves) tma_load_4d(dst + kHalfBytes, map, &sh->full[stage], 64, y, head, w, policy);
         }
       }
 #pragma unroll
       for (int i = 0; i < kStages; ++i) used[i] = i == stage ? at + 1 : used[i];
     }
     base += 2 * n;
+    segment_done(sh, index);
   }
-  if (!ok)  // nothing of ours stays in flight
+  if (sh->abort)  // nothing of ours stays in flight
 #pragma unroll
     for (int i = 0; i < kStages; ++i)
       if (used[i]) drain_wait(&sh->full[i], ((used[i] - 1) / kStages) & 1);
 }
 
-// The whole warp walks the line, one thread issues: what steers the products stays in uniform registers.  The tensor core
+// The whole warp follows the segments, one thread issues: what steers the products stays in uniform registers.  The tensor core
 // waits for little else than this warp, so the loops are written out for either kind of group.
 template <typename T>
-__device__ void multiply_warp(Shared* sh, uint32_t q_addr, uint32_t ring_addr, const AttendParams& p, const AttendSplit& sp,
-                              Line line) {
+__device__ void multiply_warp(Shared* sh, uint32_t q_addr, uint32_t ring_addr, const AttendParams& p, const AttendSplit& sp) {
   constexpr bool kBf = !std::is_same<T, __half>::value;
   const int steps = (p.cache.D + 15) / 16;
   const uint32_t tmem = sh->tmem;
   const uint32_t qk = idesc_16_f32(kBf, kAttendRows, kAttendKeys, false), wv = idesc_16_f32(kBf, kAttendRows, 16 * steps, true);
   unsigned it = 0, turns[2] = {0, 0}, queries[2] = {0, 0};  // tiles, weights of an accumulator, tiles of queries
-  Segment g;
   auto take = [&]() {
     const unsigned stage = it % kStages;
-    const bool ok = mbar_wait(&sh->full[stage], (it / kStages) & 1, &sh->abort, &sh->code);
+    const bool ok = warp_wait(sh, &sh->full[stage], (it / kStages) & 1);
     ++it;
-    return __all_sync(~0u, ok) ? static_cast<int>(stage) : -1;
+    return ok ? static_cast<int>(stage) : -1;
   };
   // S of accumulator w from query tile `tile` and the keys in `stage`; last: nobody else wants them; free: nor the queries
   auto scores = [&](int w, int tile, int stage, bool last, bool free) {
@@ -448,15 +470,13 @@ __device__ void multiply_warp(Shared* sh, uint32_t q_addr, uint32_t ring_addr, c
     }
     __syncwarp();
   };
-  auto weights = [&](int w) {
-    return __all_sync(~0u, mbar_wait(&sh->w_ready[w], turns[w]++ & 1, &sh->abort, &sh->code));
-  };
-  auto queried = [&](int tile) {
-    return __all_sync(~0u, mbar_wait(&sh->q_ready[tile], queries[tile]++ & 1, &sh->abort, &sh->code));
-  };
-  while (line.next(sh, p, sp, &g)) {
-    const bool two = g.tokens > sp.tile_tokens;
-    const int n = g.t1 - g.t0;
+  auto weights = [&](int w) { return warp_wait(sh, &sh->w_ready[w], turns[w]++ & 1); };
+  auto queried = [&](int tile) { return warp_wait(sh, &sh->q_ready[tile], queries[tile]++ & 1); };
+  const Segment* g;
+  for (unsigned index = 0; (g = next_segment(sh, index)) != nullptr; ++index) {
+    const bool two = g->tokens > sp.tile_tokens;
+    const int n = g->t1 - g->t0;
+    segment_done(sh, index);
     if (!queried(0)) return;
     if (two) {
       int k = take();
@@ -534,25 +554,42 @@ __device__ __forceinline__ void bring_queries(uint8_t* dst, int tile, int row0, 
   fence_async_smem();
 }
 
-// A warp that brings every segment's queries but the first's, as soon as the products are done with the last ones, and
-// notes the group that goes on behind this stretch for the kernel that joins.
+// A warp that walks the line: describes the segments, brings their queries (but the first's) as soon as the products are
+// done with the ones before, and notes the group that goes on behind this stretch for the kernel that joins.
 template <typename T>
-__device__ void query_warp(Shared* sh, uint8_t* q_smem, const AttendParams& p, const AttendSplit& sp, Line line, int each) {
+__device__ void line_warp(Shared* sh, uint8_t* q_smem, const AttendParams& p, const AttendSplit& sp, Line line, int each) {
   const int lane = threadIdx.x & 31;
   unsigned queries[2] = {0, 0};
   AttendTail tail{-1, 0, 0, 0};
   Segment g;
-  bool ok = true;
-  for (bool start = true; line.next(sh, p, sp, &g); start = false) {
+  for (unsigned index = 0;; ++index) {
+    const bool more = line.next(sh, p, sp, &g);
+    const unsigned slot = index % kSegments;
+    if (index >= kSegments && !warp_wait(sh, &sh->seg_done[slot], (index / kSegments - 1) & 1)) break;
+    if (!more) g.t0 = g.t1 = 0;
+    if (more && tree_in_words(p, g)) {
+      const int32_t* const parent = p.parent + static_cast<long long>(g.seq) * p.N;
+      for (int t = lane; t < g.tokens; t += 32) {
+        uint32_t words[kTreeWords] = {};
+        for (int a = min(g.tok0 + t, p.N);; a = tree_up(parent, a)) {  // (tokens past the tree see nothing anyway)
+#pragma unroll
+          for (int w = 0; w < kTreeWords; ++w) words[w] |= a >> 5 == w ? 1u << (a & 31) : 0u;
+          if (a == 0) break;
+        }
+#pragma unroll
+        for (int w = 0; w < kTreeWords; ++w) sh->above[slot][t][w] = words[w];
+      }
+    }
+    if (lane == 0) sh->seg[slot] = g;
+    warp_arrive(&sh->seg_ready[slot]);
+    if (!more) break;
     const bool two = g.tokens > sp.tile_tokens;
     if (g.t0 == 0 && g.t1 < g.tiles) tail = AttendTail{g.last / each, g.s.row + g.tok0, g.head, g.tokens};
 #pragma unroll 1
     for (int tile = 0; tile < (two ? 2 : 1); ++tile) {
       const unsigned use = queries[tile]++;
-      if (start || !ok) continue;
-      ok = use == 0 || wait_for(sh, &sh->q_free[tile], (use - 1) & 1);
-      ok = __all_sync(~0u, ok);
-      if (!ok) continue;
+      if (index == 0 || sh->abort) continue;
+      if (use > 0 && !warp_wait(sh, &sh->q_free[tile], (use - 1) & 1)) continue;
       bring_queries<T>(q_smem + tile * kTileBytes, tile, 0, kAttendRows, p, sp, g, lane, 32);
       warp_arrive(&sh->q_ready[tile]);
     }
@@ -562,7 +599,7 @@ __device__ void query_warp(Shared* sh, uint8_t* q_smem, const AttendParams& p, c
 
 // One warpgroup: a row's softmax, the end of a segment.
 template <typename T>
-__device__ void soft_group(Shared* sh, uint8_t* q_smem, uint8_t* ring, const AttendParams& p, const AttendSplit& sp, Line line) {
+__device__ void soft_group(Shared* sh, uint8_t* q_smem, uint8_t* ring, const AttendParams& p, const AttendSplit& sp) {
   const int w = threadIdx.x >> 7, r = threadIdx.x & 127, lane_base = (threadIdx.x >> 5 & 3) * 32;
   const int D = p.cache.D, G = p.group, steps = (D + 15) / 16, units = 2 * steps;
   const uint32_t tmem = sh->tmem + (static_cast<uint32_t>(lane_base) << 16);
@@ -571,34 +608,39 @@ __device__ void soft_group(Shared* sh, uint8_t* q_smem, uint8_t* ring, const Att
   const int tile_rows = sp.tile_tokens * G;
   const int my_tok = r / G, my_head = r - my_tok * G;  // of a tile
   const int row_step = 128 / units, unit_row = r / units, unit = r - unit_row * units;  // 16 bytes a thread
-  unsigned segment = 0, turn = 0, base = 0;
+  unsigned segment = 0, turn = 0, base = 0, meetings = 0;
+  auto meet = [&]() {  // all warps of both accumulators
+    warp_arrive(&sh->met);
+    return warp_wait(sh, &sh->met, meetings++ & 1);
+  };
   bool crossed = false;
-  Segment g;
-  for (; line.next(sh, p, sp, &g); ++segment, base += 2 * (g.t1 - g.t0)) {
+  const Segment* seg;
+  for (; (seg = next_segment(sh, segment)) != nullptr; ++segment) {
+    const Segment& g = *seg;
     const bool two = g.tokens > sp.tile_tokens;
     const int n = g.t1 - g.t0, ahead = two ? 1 : 2;
     const int tile = two ? w : 0;
     if (segment == 0) {  // everybody brings the first queries
       bring_queries<T>(q_smem + tile * kTileBytes, tile, two ? 0 : 64 * w, two ? kAttendRows : 64, p, sp, g, r, 128);
-      named_bar_sync(1, kSoftThreads);
+      if (!meet()) return;
       if (threadIdx.x == 0) mbar_arrive(&sh->q_ready[0]);
       if (threadIdx.x == 128 && two) mbar_arrive(&sh->q_ready[1]);
-    } else if (crossed) {  // the other warpgroup has read our accumulator
-      named_bar_sync(1, kSoftThreads);
+      __syncwarp();
+    } else if (crossed) {  // the other accumulator's warps have read ours
+      if (!meet()) return;
     }
     crossed = !two;
     const int tok = tile * sp.tile_tokens + my_tok;  // in the group
     const bool valid = r < tile_rows && tok < g.tokens;
     const bool busy = __any_sync(~0u, valid);  // a warp without rows only keeps time: what its lanes hold reaches nobody
     const int i = g.tok0 + tok;
-    const int32_t* const parent = p.mask == kMaskTree ? p.parent + static_cast<long long>(g.seq) * p.N : nullptr;
     const int from = masked_from(p, g.s, g.tok0 + tile * sp.tile_tokens);
     float m = -INFINITY, l = 0.f;
     for (int j = two ? 0 : w; j < n; j += two ? 1 : 2, ++turn) {
       const bool started = j >= (two ? 1 : 2);
       const int key0 = (g.t0 + j) * kAttendKeys;
       const bool masked = key0 + kAttendKeys > from;
-      mbar_wait(&sh->s_full[w], turn & 1, &sh->abort, &sh->code);
+      if (!warp_wait(sh, &sh->s_full[w], turn & 1)) return;
       tc_fence_after();
       auto softmax = [&](auto Masked) {
         constexpr bool kMasked = decltype(Masked)::value;
@@ -607,7 +649,7 @@ __device__ void soft_group(Shared* sh, uint8_t* q_smem, uint8_t* ring, const Att
 #pragma unroll
         for (int x = 0; x < 4; ++x) tc_ld_x32(s_col + 32 * x, s[x]);
         if constexpr (kMasked) {
-          if (valid) seen_bits(p, g.s, parent, i, key0, bits);
+          if (valid) seen_bits(p, g, sh->above[segment % kSegments][tok], i, key0, bits);
           __syncwarp();
         }
         tc_wait_ld();
@@ -671,7 +713,7 @@ __device__ void soft_group(Shared* sh, uint8_t* q_smem, uint8_t* ring, const Att
       if (masked) {  // values that weights of 0 must not meet
         const unsigned place = base + value_place(j, n, ahead);
         const int stage = place % kStages, row0 = max(from - key0, 0);
-        mbar_wait(&sh->full[stage], (place / kStages) & 1, &sh->abort, &sh->code);
+        if (!warp_wait(sh, &sh->full[stage], (place / kStages) & 1)) return;
         if (unit_row < row_step)
 #pragma unroll 2
           for (int row = row0 + unit_row; row < kAttendKeys; row += row_step) {
@@ -696,14 +738,14 @@ __device__ void soft_group(Shared* sh, uint8_t* q_smem, uint8_t* ring, const Att
 
     // the segment's end: sums into the output, or into the workspace where the group's keys go on elsewhere
     const bool any = n > (two ? 0 : w);
-    if (any) mbar_wait(&sh->o_done[w], (turn - 1) & 1, &sh->abort, &sh->code);
+    if (any && !warp_wait(sh, &sh->o_done[w], (turn - 1) & 1)) return;
     tc_fence_after();
     float f0 = 1.f, f1 = 0.f;  // one tile of queries: the warpgroups' weights
     if (!two) {
       sh->norm[w][0][r] = m;
       sh->norm[w][1][r] = l;
       tc_fence_before();
-      named_bar_sync(1, kSoftThreads);
+      if (!meet()) return;
       tc_fence_after();
       const float m0 = sh->norm[0][0][r], m1 = sh->norm[1][0][r];
       m = fmaxf(m0, m1);
@@ -763,7 +805,7 @@ __device__ void soft_group(Shared* sh, uint8_t* q_smem, uint8_t* ring, const Att
       const int end = min(g.s.kv, g.t1 * kAttendKeys);
 #pragma unroll 1
       for (int key = max(masked_from(p, g.s, g.tok0), g.t0 * kAttendKeys); key < end; ++key) {
-        if (!sees(p.mask, parent, p.N, i, static_cast<long long>(g.s.kv) - g.s.n, key)) continue;
+        if (!sees(p.mask, p.parent ? p.parent + static_cast<long long>(g.seq) * p.N : nullptr, p.N, i, static_cast<long long>(g.s.kv) - g.s.n, key)) continue;
         const long long off = place_offset(p.cache, p.batch, g.seq, key);
         if (off < 0) continue;
         const T* const v = static_cast<const T*>(p.cache.v) + off + g.head * p.cache.head_stride;
@@ -788,6 +830,8 @@ __device__ void soft_group(Shared* sh, uint8_t* q_smem, uint8_t* ring, const Att
       }
     }
     tc_fence_before();
+    base += 2 * n;
+    segment_done(sh, segment);
   }
 }
 
@@ -813,6 +857,11 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_init(&sh->q_free[i], 1);
       sh->odd[i] = 0;
     }
+    for (int i = 0; i < kSegments; ++i) {
+      mbar_init(&sh->seg_ready[i], 1);
+      mbar_init(&sh->seg_done[i], kConsumers);
+    }
+    mbar_init(&sh->met, kSoftThreads / 32);
     fence_mbar_init();
     sh->abort = 0;
     sh->code = 0;
@@ -876,22 +925,22 @@ __global__ void __launch_bounds__(kThreads, 1)
   line.begin(sh, p, sp, from, from + min(each, units - from));
   if (tid < kSoftThreads) {
     regs_up<kSoftRegs>();
-    soft_group<T>(sh, tiles, ring, p, sp, line);
+    soft_group<T>(sh, tiles, ring, p, sp);
   } else {
     regs_down<kOtherRegs>();
     if (warp == kSoftThreads / 32 || warp == kSoftThreads / 32 + 2) {
       const bool v = warp == kSoftThreads / 32 + 2;
-      load_warp(sh, ring, v ? &values : &keys, v, p, sp, line);
+      load_warp(sh, ring, v ? &values : &keys, v, p, sp);
     }
     if (warp == kSoftThreads / 32 + 1) {
-      multiply_warp<T>(sh, smem_u32(tiles), smem_u32(ring), p, sp, line);
+      multiply_warp<T>(sh, smem_u32(tiles), smem_u32(ring), p, sp);
       if (sh->abort) {  // products in flight read the tiles and write the accumulators: they take microseconds
         const long long t0 = clock64();
         while (clock64() - t0 < kWaitCycles / 1024) {
         }
       }
     }
-    if (warp == kSoftThreads / 32 + 3) query_warp<T>(sh, tiles, p, sp, line, each);
+    if (warp == kSoftThreads / 32 + 3) line_warp<T>(sh, tiles, p, sp, line, each);
   }
   __syncwarp();
   tc_fence_before();
