@@ -1180,7 +1180,8 @@ int enqueue_rope(dm::RopeParams& r, int dtype, int layout, bool by16, bool by8, 
   if (rc != DOMINO_OK) return rc;
   r.pairs = layout == DOMINO_ROPE_PAIRS;
   const int n16 = static_cast<int>(16 / elem_bytes(dtype)), n8 = n16 / 2;
-  const int unit = by16 && r.rot / 2 % n16 == 0 && r.D % n16 == 0 ? 16 : by8 && r.rot / 2 % n8 == 0 && r.D % n8 == 0 ? 8 : 0;
+  const int span = r.pairs ? r.rot : r.rot / 2;  // that has to be whole units
+  const int unit = by16 && span % n16 == 0 && r.D % n16 == 0 ? 16 : by8 && span % n8 == 0 && r.D % n8 == 0 ? 8 : 0;
   const long long blocks = (static_cast<long long>(r.tokens) * r.D + 255) / 256;  // the most that any unit takes
   if (blocks > 0x7fffffffLL) return DOMINO_ERR_UNSUPPORTED;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
@@ -1451,9 +1452,12 @@ int domino_cache_commit(const domino_kv_cache* cache, const domino_kv_batch* bat
   const size_t e = elem_bytes(cache->dtype);
   const bool vector = cache_aligned(*cache, 16) && stride_aligned(layer_stride, layers, cache->dtype, 16) &&
                       cache->head_dim % static_cast<int>(16 / e) == 0;
+  int sms = 0, major = 0, minor = 0;
+  rc = device_sms(&sms, &major, &minor);
+  if (rc != DOMINO_OK) return rc;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const int ts = timing_open(DOMINO_KERNEL_COMMIT, st);
-  rc = cuda_rc(dm::launch_commit(c, static_cast<int>(e), vector, st));
+  rc = cuda_rc(dm::launch_commit(c, static_cast<int>(e), vector, sms, st));
   timing_close(ts, st);
   return rc;
 } catch (...) {

@@ -9,6 +9,8 @@
 // integers too, and cos and sin of the rest, at most an eighth of a turn, are taken in fp32.
 #include <math.h>
 
+#include <type_traits>
+
 #include "kernels.h"
 #include "paged.cuh"
 #include "rows.cuh"
@@ -17,6 +19,7 @@ namespace dm {
 namespace {
 
 constexpr int kRopeThreads = 256;
+constexpr int kRopeBlocks = 8;
 
 // f / (2 pi) in units of 2^-64 of a turn, modulo a turn: f = m 2^e with m below 2^24, |f| <= 1024.
 __device__ __forceinline__ uint64_t turn_speed(float f) {
@@ -48,176 +51,189 @@ __device__ __forceinline__ void turn(int p, uint64_t F, float amplitude, float* 
 // N elements in one access of 16 or 8 bytes, or one element.
 template <typename T, int N>
 struct Unit {
-  float v[N];
   static constexpr int kBytes = N * static_cast<int>(sizeof(T));
-  __device__ __forceinline__ void load(const T* p) {
-    if constexpr (kBytes == 16) {
-      Vec<T> r;
-      r.raw = *reinterpret_cast<const uint4*>(p);
-      unpack(r, v);
-    } else if constexpr (kBytes == 8 && N > 1) {
-      alignas(8) T e[N];
-      *reinterpret_cast<uint2*>(e) = *reinterpret_cast<const uint2*>(p);
+  using Raw = typename std::conditional<kBytes == 16, uint4, typename std::conditional<kBytes == 8, uint2, T>::type>::type;
+  Raw raw;
+  __device__ __forceinline__ void load(const T* p) { raw = *reinterpret_cast<const Raw*>(p); }
+  __device__ __forceinline__ void store(T* p) const { *reinterpret_cast<Raw*>(p) = raw; }
+  __device__ __forceinline__ void get(float (&v)[N]) const {
+    const T* const e = reinterpret_cast<const T*>(&raw);
 #pragma unroll
-      for (int i = 0; i < N; ++i) v[i] = to_f32(e[i]);
-    } else {
-      v[0] = to_f32(*p);
-    }
+    for (int i = 0; i < N; ++i) v[i] = to_f32(e[i]);
   }
-  __device__ __forceinline__ void store(T* p) const {
-    if constexpr (kBytes == 16) {
-      Vec<T> r;
-      pack(v, &r);
-      *reinterpret_cast<uint4*>(p) = r.raw;
-    } else if constexpr (kBytes == 8 && N > 1) {
-      alignas(8) T e[N];
+  __device__ __forceinline__ void put(const float (&v)[N]) {
+    T* const e = reinterpret_cast<T*>(&raw);
 #pragma unroll
-      for (int i = 0; i < N; ++i) from_f32(v[i], e + i);
-      *reinterpret_cast<uint2*>(p) = *reinterpret_cast<const uint2*>(e);
-    } else {
-      from_f32(v[0], p);
-    }
+    for (int i = 0; i < N; ++i) from_f32(v[i], e + i);
   }
 };
 
-// A thread keeps one share of a token's head, its angles in registers, and takes it through the heads h0 .. h1 - 1:
-// the heads of x, then those of k.  Values have no angles; their units go round the token's threads.
-//   shares: rot / 2 / N of N pairs each (halves: a unit of each half; neighbours: two units), then (D - rot) / N units
-//   that are copied.
-template <typename T, int N>
+constexpr int kUnitsAhead = 8;  // a thread's loads in flight
+
+// A thread keeps one share of a token's head, its angles in registers, and takes it through the heads h0 .. h1 - 1: those
+// of x, then those of k, then those of v.  A share is a unit of N elements that holds pairs of neighbours (INSIDE), or
+// two units whose elements pair up; the units behind the turned ones, and all of v's, are copied.  The first heads are on
+// their way while the angles are computed.
+// Bound by DRAM where there are many tokens, by one thread's chain of latencies where there are few: XXX
+template <typename T, int N, bool INSIDE>
 __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const RopeParams p, int shares, int heads_a_block) {
-  using U = Unit<T, N>;
+  constexpr int kUnits = INSIDE ? 1 : 2, kHeads = kUnitsAhead / kUnits, kAngles = INSIDE ? N / 2 : N;
   const long long at = static_cast<long long>(blockIdx.x) * kRopeThreads + threadIdx.x;
   const int token = static_cast<int>(at / shares), share = static_cast<int>(at - static_cast<long long>(token) * shares);
   if (token >= p.tokens) return;
-  const int turned = p.rot / 2 / N;
   const bool append = p.k != nullptr;
 
-  int place = -1, pos = 0, seq = -1;
+  int pos = 0;
   long long dst = -1;
   if (append) {
-    seq = find_sequence(p.batch, token);
+    const int seq = find_sequence(p.batch, token);
     if (seq < 0) return;  // a row behind the last sequence
     const Sequence s = load_sequence(p.cache, p.batch, p.tokens, seq);
     const int i = token - s.row, first = s.kv - s.n;
-    place = first + i;
-    dst = place_offset(p.cache, p.batch, seq, place);
-    pos = place;
+    pos = first + i;
+    dst = place_offset(p.cache, p.batch, seq, pos);
     if (p.depth && i >= 1 && i <= p.N) pos = first + p.depth[static_cast<long long>(seq) * p.N + i - 1];
   }
   if (p.positions) pos = p.positions[token];
 
-  const int h0 = blockIdx.y * heads_a_block, all = p.heads + (append ? 2 * p.cache.heads : 0);
-  const int h1 = min(h0 + heads_a_block, all), spun = p.heads + (append ? p.cache.heads : 0);
-  T* const ck = static_cast<T*>(p.cache.k);
-  T* const cv = static_cast<T*>(p.cache.v);
+  // the share's elements: o0, and o1 where there is a second unit
+  const int turned = INSIDE ? p.rot / N : p.rot / 2 / N, behind = share - turned;
+  int o0 = share * N, o1 = p.D;
+  if (!INSIDE) {
+    if (behind >= 0) {
+      o0 = p.rot + 2 * N * behind;
+      o1 = o0 + N;
+    } else if (p.pairs) {  // N is 1
+      o0 = 2 * share;
+      o1 = o0 + 1;
+    } else {
+      o1 = o0 + p.rot / 2;
+    }
+  }
+  const bool second = !INSIDE && o1 < p.D;
+  const int spun = p.heads + (append ? p.cache.heads : 0), all = spun + (append ? p.cache.heads : 0);
+  const int h0 = blockIdx.y * heads_a_block, h1 = min(h0 + heads_a_block, all);
   auto source = [&](int h) {
-    return h < p.heads ? static_cast<const T*>(p.x) + token * p.x_token + h * p.x_head
-                       : static_cast<const T*>(p.k) + token * p.k_token + static_cast<long long>(h - p.heads) * p.D;
+    if (h < p.heads) return static_cast<const T*>(p.x) + token * p.x_token + h * p.x_head;
+    if (h < spun) return static_cast<const T*>(p.k) + token * p.k_token + static_cast<long long>(h - p.heads) * p.D;
+    return static_cast<const T*>(p.v) + token * p.v_token + static_cast<long long>(h - spun) * p.D;
   };
   auto target = [&](int h) -> T* {
     if (h < p.heads) return static_cast<T*>(p.y) + token * p.y_token + h * p.y_head;
-    return dst < 0 ? nullptr : ck + dst + (h - p.heads) * p.cache.head_stride;
+    if (dst < 0) return nullptr;  // no place in the cache
+    if (h < spun) return static_cast<T*>(p.cache.k) + dst + (h - p.heads) * p.cache.head_stride;
+    return static_cast<T*>(p.cache.v) + dst + (h - spun) * p.cache.head_stride;
   };
-
-  if (share < turned) {
-    if (h0 < spun) {
-      float co[N], si[N];
+  Unit<T, N> u[kHeads][kUnits];
+  auto load = [&](int h) {
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
-        turn(pos, turn_speed(p.freq[share * N + i]), p.amplitude, &co[i], &si[i]);
-        if (p.back) si[i] = -si[i];
-      }
-      const int o0 = p.pairs ? 2 * share * N : share * N;
-      const int o1 = p.pairs ? o0 + N : o0 + p.rot / 2;
-#pragma unroll 4
-      for (int h = h0; h < min(h1, spun); ++h) {
-        const T* const x = source(h);
-        T* const y = target(h);
-        U a, b;
-        a.load(x + o0);
-        b.load(x + o1);
-        if (p.pairs) {
-#pragma unroll
-          for (int i = 0; i < N; ++i) {  // pair i of the share: elements 2 i and 2 i + 1 of the two units in a row
-            float& x0 = 2 * i < N ? a.v[2 * i < N ? 2 * i : 0] : b.v[2 * i < N ? 0 : 2 * i - N];
-            float& x1 = 2 * i + 1 < N ? a.v[2 * i + 1 < N ? 2 * i + 1 : 0] : b.v[2 * i + 1 < N ? 0 : 2 * i + 1 - N];
-            const float y0 = fmaf(x0, co[i], -(x1 * si[i])), y1 = fmaf(x1, co[i], x0 * si[i]);
-            x0 = y0;
-            x1 = y1;
-          }
-        } else {
-#pragma unroll
-          for (int i = 0; i < N; ++i) {
-            const float y0 = fmaf(a.v[i], co[i], -(b.v[i] * si[i])), y1 = fmaf(b.v[i], co[i], a.v[i] * si[i]);
-            a.v[i] = y0;
-            b.v[i] = y1;
-          }
-        }
-        if (y) {
-          a.store(y + o0);
-          b.store(y + o1);
-        }
-      }
+    for (int i = 0; i < kHeads; ++i) {
+      if (h + i >= h1) break;
+      const T* const x = source(h + i);
+      u[i][0].load(x + o0);
+      if (second) u[i][kUnits - 1].load(x + o1);
     }
-  } else {
-    const int o = p.rot + (share - turned) * N;
-#pragma unroll 4
-    for (int h = h0; h < min(h1, spun); ++h) {
-      T* const y = target(h);
-      U a;
-      a.load(source(h) + o);
-      if (y) a.store(y + o);
+  };
+  load(h0);
+
+  float co[kAngles], si[kAngles];
+  if (behind < 0) {
+#pragma unroll
+    for (int i = 0; i < kAngles; ++i) {
+      turn(pos, turn_speed(p.freq[share * kAngles + i]), p.amplitude, &co[i], &si[i]);
+      if (p.back) si[i] = -si[i];
     }
   }
-  if (!append || dst < 0) return;
-  const int units = p.D / N;
-#pragma unroll 2
-  for (int h = max(h0, spun) - spun; h < h1 - spun; ++h) {
-    const T* const x = static_cast<const T*>(p.v) + token * p.v_token + static_cast<long long>(h) * p.D;
-    T* const y = cv + dst + h * p.cache.head_stride;
-    for (int u = share; u < units; u += shares) {
-      U a;
-      a.load(x + u * N);
-      a.store(y + u * N);
+  for (int h = h0;;) {
+#pragma unroll
+    for (int i = 0; i < kHeads; ++i) {
+      if (h + i >= h1) break;
+      if (behind < 0 && h + i < spun) {
+        float a[N];
+        u[i][0].get(a);
+        if constexpr (INSIDE) {
+#pragma unroll
+          for (int e = 0; e < kAngles; ++e) {
+            const float x0 = a[2 * e], x1 = a[2 * e + 1];
+            a[2 * e] = fmaf(x0, co[e], -(x1 * si[e]));
+            a[2 * e + 1] = fmaf(x1, co[e], x0 * si[e]);
+          }
+        } else {
+          float b[N];
+          u[i][kUnits - 1].get(b);
+#pragma unroll
+          for (int e = 0; e < N; ++e) {
+            const float x0 = a[e], x1 = b[e];
+            a[e] = fmaf(x0, co[e], -(x1 * si[e]));
+            b[e] = fmaf(x1, co[e], x0 * si[e]);
+          }
+          u[i][kUnits - 1].put(b);
+        }
+        u[i][0].put(a);
+      }
+      T* const y = target(h + i);
+      if (y) {
+        u[i][0].store(y + o0);
+        if (second) u[i][kUnits - 1].store(y + o1);
+      }
     }
+    h += kHeads;
+    if (h >= h1) break;
+    load(h);
   }
 }
 
-template <typename T, int N>
+template <typename T, int N, bool INSIDE>
 cudaError_t launch_rope_units(const RopeParams& p, int sms, cudaStream_t stream) {
-  const int shares = p.rot / 2 / N + (p.D - p.rot) / N;
+  const int rest = (p.D - p.rot) / N;
+  const int shares = INSIDE ? p.D / N : p.rot / 2 / N + (rest + 1) / 2;
   const int heads = p.heads + (p.k ? 2 * p.cache.heads : 0);
   const long long blocks = (static_cast<long long>(p.tokens) * shares + kRopeThreads - 1) / kRopeThreads;
-  // Angles cost as much as several heads, so a thread takes all of them where the tokens fill the chip four blocks an SM
-  // deep; fewer tokens spread their heads over the blocks.
-  long long split = (4LL * sms + blocks - 1) / blocks;
+  // Angles cost as much as several heads, so a thread takes all of them where the tokens fill the chip kRopeBlocks blocks an
+  // SM; fewer tokens spread their heads over the blocks.
+  long long split = (static_cast<long long>(kRopeBlocks) * sms + blocks - 1) / blocks;
   split = split < 1 ? 1 : split > heads ? heads : split;
   const int each = static_cast<int>((heads + split - 1) / split);
   const dim3 grid(static_cast<unsigned>(blocks), static_cast<unsigned>((heads + each - 1) / each));
-  rope_kernel<T, N><<<grid, kRopeThreads, 0, stream>>>(p, shares, each);
+  rope_kernel<T, N, INSIDE><<<grid, kRopeThreads, 0, stream>>>(p, shares, each);
   return cudaGetLastError();
 }
 
 template <typename T>
 cudaError_t launch_rope_type(const RopeParams& p, int unit_bytes, int sms, cudaStream_t stream) {
   constexpr int kElem = static_cast<int>(sizeof(T));
-  if (unit_bytes == 16) return launch_rope_units<T, 16 / kElem>(p, sms, stream);
-  if (unit_bytes == 8) return launch_rope_units<T, 8 / kElem>(p, sms, stream);
-  return launch_rope_units<T, 1>(p, sms, stream);
+  if (unit_bytes == 16 && p.pairs) return launch_rope_units<T, 16 / kElem, true>(p, sms, stream);
+  if (unit_bytes == 8 && p.pairs) return launch_rope_units<T, 8 / kElem, true>(p, sms, stream);
+  if (unit_bytes == 16) return launch_rope_units<T, 16 / kElem, false>(p, sms, stream);
+  if (unit_bytes == 8) return launch_rope_units<T, 8 / kElem, false>(p, sms, stream);
+  return launch_rope_units<T, 1, false>(p, sms, stream);
 }
 
 // ---------------------------------------------------------------- accepted nodes
 constexpr int kCommitThreads = 256;
+constexpr int kCommitBlocks = 8;  // blocks an SM that share the layers out
+constexpr int kMoves = 256;       // moves looked up at a time
 constexpr int kMovesAhead = 8;
 
-// A block takes a sequence's keys, or values, of one layer; a thread one unit of every node.  The list rises, so node
-// j's source lies behind the targets of all moves before it: moves may read ahead of the earlier ones' writes, and a
-// thread that reads eight before it writes them leaves every unit what one move after the other would.
+template <typename E, typename V, int N>
+struct MoveUnit {
+  using elem = E;
+  using type = V;
+  static constexpr int kN = N;
+};
+
+// A block takes some layers of a sequence, keys and values.  It looks the whole list through, then the moves' places, once
+// for all layers; a thread takes one unit of a place through all moves.  The list rises, so node j's source lies behind
+// the targets of all moves before it: moves may read ahead of the earlier ones' writes, and a thread that reads eight
+// before it writes them leaves every unit what one move after the other would.
+// Bound by the chain of look-ups (sequence, list, table, keys) where little moves, by DRAM's rate on short rows where much
+// does: XXX
 template <typename U>
-__global__ void __launch_bounds__(kCommitThreads) commit_kernel(const CommitParams p, int units) {
-  const int b = blockIdx.x, layer = blockIdx.y >> 1, tid = threadIdx.x;
-  const bool values = blockIdx.y & 1;
+__global__ void __launch_bounds__(kCommitThreads) commit_kernel(const CommitParams p, int units, int layers_a_block) {
+  using E = typename U::elem;
+  using V = typename U::type;
+  __shared__ long long s_from[kMoves], s_to[kMoves];
+  const int b = blockIdx.x, tid = threadIdx.x;
   const PagedCache& c = p.cache;
   const int s0 = p.batch.start[b], s1 = p.batch.start[b + 1], kv = p.batch.kv_len[b], count = p.count[b];
   const int tree = min(p.N, s1 - s0 - 1);  // nodes
@@ -226,51 +242,63 @@ __global__ void __launch_bounds__(kCommitThreads) commit_kernel(const CommitPara
   bool good = s0 >= 0 && s1 >= s0 && kv >= 0 && kv <= table_places(c, p.batch);
   if (s1 == s0) good = good && count == 0;
   else good = good && first >= 1 && count >= 0 && count <= tree;
+  const int f = static_cast<int>(first);
+  // move j's element offsets, -1 where nothing moves; false where it cannot be made
+  auto look = [&](int j, long long* from, long long* to) {
+    const int node = nodes[j];
+    if (node < 0 || node >= tree || (j > 0 && node <= nodes[j - 1])) return false;
+    *from = place_offset(c, p.batch, b, f + node);
+    *to = place_offset(c, p.batch, b, f + j);
+    const bool is = *from >= 0 && *to >= 0;
+    if (node == j) *from = -1;
+    return is;
+  };
   if (good)
     for (int j = tid; j < count; j += kCommitThreads) {
-      const int node = nodes[j];
-      good = good && node >= 0 && node < tree && (j == 0 || node > nodes[j - 1]);
-      if (good) {
-        good = place_offset(c, p.batch, b, static_cast<int>(first) + node) >= 0 &&
-               place_offset(c, p.batch, b, static_cast<int>(first) + j) >= 0;
+      long long from, to;
+      good = look(j, &from, &to) && good;
+      if (j < kMoves) {
+        s_from[j] = from;
+        s_to[j] = to;
       }
     }
   good = __syncthreads_and(good);
-  if (blockIdx.y == 0 && tid == 0)
-    p.new_len[b] = !good ? -1 : s1 == s0 ? kv : static_cast<int>(first) + count;
+  if (blockIdx.y == 0 && tid == 0) p.new_len[b] = !good ? -1 : s1 == s0 ? kv : f + count;
   if (!good) return;
-  const int f = static_cast<int>(first);
-  using E = typename U::elem;
-  E* const e = static_cast<E*>(values ? c.v : c.k) + layer * p.layer_stride;
-  const int per_head = c.D / U::kN;
-  for (int u = tid; u < units; u += kCommitThreads) {
-    const int head = u / per_head;
-    const long long o = head * c.head_stride + static_cast<long long>(u - head * per_head) * U::kN;
-    for (int j0 = 0; j0 < count; j0 += kMovesAhead) {
-      typename U::type r[kMovesAhead];
-      long long to[kMovesAhead];
+  const int l0 = blockIdx.y * layers_a_block, layers = min(layers_a_block, p.layers - l0), per_head = c.D / U::kN;
+  for (int m0 = 0; m0 < count; m0 += kMoves) {
+    const int moves = min(kMoves, count - m0);
+    if (m0 > 0) {
+      __syncthreads();
+      if (tid < moves) look(m0 + tid, &s_from[tid], &s_to[tid]);
+      __syncthreads();
+    }
+    for (int x = tid; x < 2 * units * layers; x += kCommitThreads) {
+      const int slice = x / units, u = x - slice * units, head = u / per_head;  // slice: layer, keys or values
+      E* const e = static_cast<E*>(slice & 1 ? c.v : c.k) + (l0 + (slice >> 1)) * p.layer_stride + head * c.head_stride +
+                   static_cast<long long>(u - head * per_head) * U::kN;
+      for (int j0 = 0; j0 < moves; j0 += kMovesAhead) {
+        V r[kMovesAhead];
 #pragma unroll
-      for (int i = 0; i < kMovesAhead; ++i) {
-        const int j = j0 + i;
-        to[i] = -1;
-        if (j < count && nodes[j] != j) {
-          to[i] = place_offset(c, p.batch, b, f + j) + o;
-          r[i] = *reinterpret_cast<const typename U::type*>(e + place_offset(c, p.batch, b, f + nodes[j]) + o);
-        }
+        for (int i = 0; i < kMovesAhead; ++i)
+          if (j0 + i < moves && s_from[j0 + i] >= 0) r[i] = *reinterpret_cast<const V*>(e + s_from[j0 + i]);
+#pragma unroll
+        for (int i = 0; i < kMovesAhead; ++i)
+          if (j0 + i < moves && s_from[j0 + i] >= 0) *reinterpret_cast<V*>(e + s_to[j0 + i]) = r[i];
       }
-#pragma unroll
-      for (int i = 0; i < kMovesAhead; ++i)
-        if (to[i] >= 0) *reinterpret_cast<typename U::type*>(e + to[i]) = r[i];
     }
   }
 }
 
-template <typename E, typename V, int N>
-struct MoveUnit {
-  using elem = E;
-  using type = V;
-  static constexpr int kN = N;
-};
+template <typename U>
+cudaError_t launch_commit_units(const CommitParams& p, int sms, cudaStream_t stream) {
+  const long long slots = static_cast<long long>(kCommitBlocks) * sms;
+  const long long each = (static_cast<long long>(p.layers) * p.batch.B + slots - 1) / slots;
+  const int layers = static_cast<int>(each > p.layers ? p.layers : each);
+  const dim3 grid(static_cast<unsigned>(p.batch.B), static_cast<unsigned>((p.layers + layers - 1) / layers));
+  commit_kernel<U><<<grid, kCommitThreads, 0, stream>>>(p, p.cache.heads * p.cache.D / U::kN, layers);
+  return cudaGetLastError();
+}
 
 }  // namespace
 
@@ -280,18 +308,11 @@ cudaError_t launch_rope(const RopeParams& p, int dtype, int unit_bytes, int sms,
   return launch_rope_type<__half>(p, unit_bytes, sms, stream);
 }
 
-cudaError_t launch_commit(const CommitParams& p, int elem_bytes, bool vector, cudaStream_t stream) {
-  const dim3 grid(static_cast<unsigned>(p.batch.B), static_cast<unsigned>(2 * p.layers));
-  const int elems = p.cache.heads * p.cache.D;
-  if (vector && elem_bytes == 2)
-    commit_kernel<MoveUnit<uint16_t, uint4, 8>><<<grid, kCommitThreads, 0, stream>>>(p, elems / 8);
-  else if (vector)
-    commit_kernel<MoveUnit<uint32_t, uint4, 4>><<<grid, kCommitThreads, 0, stream>>>(p, elems / 4);
-  else if (elem_bytes == 2)
-    commit_kernel<MoveUnit<uint16_t, uint16_t, 1>><<<grid, kCommitThreads, 0, stream>>>(p, elems);
-  else
-    commit_kernel<MoveUnit<uint32_t, uint32_t, 1>><<<grid, kCommitThreads, 0, stream>>>(p, elems);
-  return cudaGetLastError();
+cudaError_t launch_commit(const CommitParams& p, int elem_bytes, bool vector, int sms, cudaStream_t stream) {
+  if (vector && elem_bytes == 2) return launch_commit_units<MoveUnit<uint16_t, uint4, 8>>(p, sms, stream);
+  if (vector) return launch_commit_units<MoveUnit<uint32_t, uint4, 4>>(p, sms, stream);
+  if (elem_bytes == 2) return launch_commit_units<MoveUnit<uint16_t, uint16_t, 1>>(p, sms, stream);
+  return launch_commit_units<MoveUnit<uint32_t, uint32_t, 1>>(p, sms, stream);
 }
 
 }  // namespace dm

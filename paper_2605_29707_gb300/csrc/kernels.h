@@ -336,7 +336,7 @@ struct RopeParams {
   PagedCache cache;
   PagedBatch batch;
 };
-// unit_bytes: 16 or 8 where every pointer and stride, rot / 2 and D are whole units; otherwise anything else
+// unit_bytes: 16 or 8 where every pointer and stride, D and rot (pairs) or rot / 2 are whole units; otherwise anything else
 cudaError_t launch_rope(const RopeParams& p, int dtype, int unit_bytes, int sms, cudaStream_t stream);
 
 struct CommitParams {
@@ -349,7 +349,7 @@ struct CommitParams {
   int N;
   int32_t* new_len;
 };
-cudaError_t launch_commit(const CommitParams& p, int elem_bytes, bool vector, cudaStream_t stream);
+cudaError_t launch_commit(const CommitParams& p, int elem_bytes, bool vector, int sms, cudaStream_t stream);
 
 // Masks; numerically equal to enum domino_mask.
 constexpr int kMaskCausal = 0, kMaskFull = 1, kMaskTree = 2;
