@@ -24,7 +24,6 @@
 #include <cuda_fp16.h>
 #include <math.h>
 
-#include <algorithm>
 #include <type_traits>
 
 #include "kernels.h"
@@ -954,70 +953,89 @@ __global__ void __launch_bounds__(kThreads, 1)
 
 // ---------------------------------------------------------------- joining
 constexpr int kJoinThreads = 256;
-constexpr int kJoinAhead = 8;  // partial results in flight
+constexpr int kJoinRows = 32;  // rows a block: a lane a row
+constexpr int kJoinAhead = 4;  // partial results in flight
+constexpr int kJoinWarps = kJoinThreads / 32, kJoinElems = 4;  // elements a thread
+constexpr int kJoinCols = kJoinWarps * kJoinElems;             // and a block
 
-// The group that CTA blockIdx.x began and others went on with: its rows' sums over all of them, in their order.  A thread
-// takes four elements of a row; rows lie side by side in the slots.
+// The group that CTA blockIdx.x began and others went on with: 32 of its rows' sums over all of them, in their order.  Rows
+// lie side by side in the slots: a lane takes a row, a warp four elements of a block's 32; the results turn round in shared
+// memory.
 template <typename T>
 __global__ void __launch_bounds__(kJoinThreads) join_kernel(const AttendParams p, const AttendSplit sp) {
+  __shared__ float s_out[kJoinRows][kJoinCols + 1];
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x < 32) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (blockIdx.x == 0 && blockIdx.y == 0 && blockIdx.z == 0 && warp == 0) {
     int code = 0;
-    for (unsigned i = threadIdx.x; i < gridDim.x; i += 32) {
+    for (unsigned i = lane; i < gridDim.x; i += 32) {
       const int x = sp.codes[i];
       code = x != 0 ? x : code;
     }
     const unsigned bad = __ballot_sync(~0u, code != 0);
     if (bad) code = __shfl_sync(~0u, code, __ffs(bad) - 1);
-    if (threadIdx.x == 0 && (sp.first || code != 0)) *p.status = code;
+    if (lane == 0 && (sp.first || code != 0)) *p.status = code;
   }
   const AttendTail tail = sp.tails[blockIdx.x];
-  if (tail.last < 0) return;
-  const int D = p.cache.D, G = p.group, rows = tail.tokens * G, first = blockIdx.x, slot_rows = sp.slot_rows;
-  for (int x = blockIdx.y * kJoinThreads + threadIdx.x; x < rows * (D / 4); x += gridDim.y * kJoinThreads) {
-    const int d = x / rows * 4, at = x - x / rows * rows, tok = at / G, h = at - tok * G;
-    const int slot_row = tok < sp.tile_tokens ? at : kAttendRows + at - sp.tile_tokens * G;
-    float m = -INFINITY, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int i0 = first; i0 <= tail.last; i0 += kJoinAhead) {
-      float mi[kJoinAhead], li[kJoinAhead], oi[kJoinAhead][4];
+  const int D = p.cache.D, G = p.group, rows = tail.tokens * G, first = blockIdx.x, row0 = blockIdx.y * kJoinRows;
+  const int col0 = blockIdx.z * kJoinCols, d = col0 + warp * kJoinElems;  // D is a multiple of 8: four elements, or none
+  if (tail.last < 0 || row0 >= rows) return;
+  const long long slot_rows = sp.slot_rows;
+  const int at = min(row0 + lane, rows - 1), tok = at / G, h = at - tok * G;
+  const int slot_row = tok < sp.tile_tokens ? at : kAttendRows + at - sp.tile_tokens * G;
+  float m = -INFINITY, l = 0.f, o[kJoinElems];
 #pragma unroll
-      for (int i = 0; i < kJoinAhead; ++i) {
-        const bool is = i0 + i <= tail.last;
-        const long long slot = i0 + i == first ? 2 * first + 1 : 2 * (is ? i0 + i : first);
-        const float* const norm = sp.norms + slot * 2 * slot_rows + slot_row;
-        const float* const part = sp.parts + (slot * D + d) * slot_rows + slot_row;
-        mi[i] = is ? norm[0] : -INFINITY;
-        li[i] = is ? norm[slot_rows] : 0.f;
+  for (int e = 0; e < kJoinElems; ++e) o[e] = 0.f;
+  for (int i0 = first; i0 <= tail.last; i0 += kJoinAhead) {
+    float mi[kJoinAhead], li[kJoinAhead], v[kJoinAhead][kJoinElems];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) oi[i][e] = is ? part[e * slot_rows] : 0.f;
+    for (int i = 0; i < kJoinAhead; ++i) {
+      if (i0 + i > tail.last) {
+        mi[i] = -INFINITY;
+        continue;
       }
-      float up = m;
+      const long long slot = i0 + i == first ? 2 * first + 1 : 2 * (i0 + i);
+      const float* const norm = sp.norms + slot * 2 * slot_rows + slot_row;
+      const float* const part = sp.parts + (slot * D + d) * slot_rows + slot_row;
+      mi[i] = norm[0];
+      li[i] = norm[slot_rows];
 #pragma unroll
-      for (int i = 0; i < kJoinAhead; ++i) up = fmaxf(up, mi[i]);
-      const float keep = m == up ? 1.f : ex2((m - up) * p.scale_log2);
-      m = up;
-      l *= keep;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) o[e] *= keep;
-#pragma unroll
-      for (int i = 0; i < kJoinAhead; ++i) {
-        const float f = mi[i] == m ? 1.f : ex2((mi[i] - m) * p.scale_log2);
-        if (mi[i] == -INFINITY) continue;  // a part that saw nothing: sums of 0
-        l = fmaf(li[i], f, l);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] = fmaf(oi[i][e], f, o[e]);
-      }
+      for (int e = 0; e < kJoinElems; ++e) v[i][e] = d < D ? part[e * slot_rows] : 0.f;
     }
-    const long long row = tail.row + tok;
-    const int head = tail.head * G + h;
-    const float inv = 1.f / l;
-    alignas(8) T y[4];
+    float up = m;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) from_f32(l == 0.f ? 0.f : o[e] * inv, y + e);
-    *reinterpret_cast<uint2*>(static_cast<T*>(p.out) + row * p.out_stride + static_cast<long long>(head) * D + d) =
-        *reinterpret_cast<const uint2*>(y);
-    if (p.lse && d == 0) p.lse[row * p.hq + head] = l == 0.f ? -INFINITY : fmaf(m, p.scale, logf(l));
+    for (int i = 0; i < kJoinAhead; ++i) up = fmaxf(up, mi[i]);
+    const float keep = m == up ? 1.f : ex2((m - up) * p.scale_log2);
+    m = up;
+    l *= keep;
+#pragma unroll
+    for (int e = 0; e < kJoinElems; ++e) o[e] *= keep;
+#pragma unroll
+    for (int i = 0; i < kJoinAhead; ++i) {
+      if (mi[i] == -INFINITY) continue;  // no part, or one that saw nothing: sums of 0
+      const float f = mi[i] == m ? 1.f : ex2((mi[i] - m) * p.scale_log2);
+      l = fmaf(li[i], f, l);
+#pragma unroll
+      for (int e = 0; e < kJoinElems; ++e) o[e] = fmaf(v[i][e], f, o[e]);
+    }
   }
+  const float inv = 1.f / l;
+#pragma unroll
+  for (int e = 0; e < kJoinElems; ++e)
+    s_out[lane][warp * kJoinElems + e] = l == 0.f ? 0.f : o[e] * inv;
+  if (p.lse && blockIdx.z == 0 && warp == 0 && row0 + lane < rows)
+    p.lse[(tail.row + tok) * static_cast<long long>(p.hq) + tail.head * G + h] = l == 0.f ? -INFINITY : fmaf(m, p.scale, logf(l));
+  __syncthreads();
+  const int r = threadIdx.x / (kJoinCols / 8), x = threadIdx.x % (kJoinCols / 8) * 8;
+  if (r >= kJoinRows || row0 + r >= rows || col0 + x >= D) return;
+  const int tk = (row0 + r) / G, head = tail.head * G + row0 + r - tk * G;
+  float y[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) y[e] = s_out[r][x + e];
+  Vec<T> v;
+  pack(y, &v);
+  *reinterpret_cast<uint4*>(static_cast<T*>(p.out) + static_cast<long long>(tail.row + tk) * p.out_stride +
+                            static_cast<long long>(head) * D + col0 + x) = v.raw;
 }
 
 template <typename T>
@@ -1037,7 +1055,7 @@ cudaError_t launch_tc_type(const CUtensorMap& keys, const CUtensorMap& values, c
   cfg.numAttrs = 1;
   e = cudaLaunchKernelEx(&cfg, attend_kernel<T>, keys, values, p, s);
   if (e != cudaSuccess) return e;
-  cfg.gridDim = dim3(grid, std::min(8, (s.slot_rows * p.cache.D / 4 + kJoinThreads - 1) / kJoinThreads));
+  cfg.gridDim = dim3(grid, (s.slot_rows + kJoinRows - 1) / kJoinRows, (p.cache.D + kJoinCols - 1) / kJoinCols);
   cfg.blockDim = dim3(kJoinThreads);
   cfg.dynamicSmemBytes = 0;
   return cudaLaunchKernelEx(&cfg, join_kernel<T>, p, s);

@@ -19,7 +19,6 @@ namespace dm {
 namespace {
 
 constexpr int kRopeThreads = 256;
-constexpr int kRopeBlocks = 8;
 
 // f / (2 pi) in units of 2^-64 of a turn, modulo a turn: f = m 2^e with m below 2^24, |f| <= 1024.
 __device__ __forceinline__ uint64_t turn_speed(float f) {
@@ -68,7 +67,11 @@ struct Unit {
   }
 };
 
-constexpr int kUnitsAhead = 8;  // a thread's loads in flight
+// Loads of a thread in flight, and blocks an SM that share the heads out: neighbours in one unit, or two units that pair up.
+// us at 4 / 8 / 16 loads (8 blocks) and 4 / 8 / 16 blocks (the loads as chosen): 12003 tokens x 48 fp16 heads in a cache, pairs
+// of neighbours, 50.5 / 49.6 / 56.8 and 52.8 / 49.6 / 50.3; 16384 x 32 bf16 heads, halves, 47.4 / 53.5 / 73.3 and 45.9 / 47.4 / 48.6.
+__host__ __device__ constexpr int units_ahead(bool inside) { return inside ? 8 : 4; }
+__host__ __device__ constexpr int rope_blocks(bool inside) { return inside ? 6 : 4; }
 
 // A thread keeps one share of a token's head, its angles in registers, and takes it through the heads h0 .. h1 - 1: those
 // of x, then those of k, then those of v.  A share is a unit of N elements that holds pairs of neighbours (INSIDE), or
@@ -77,7 +80,7 @@ constexpr int kUnitsAhead = 8;  // a thread's loads in flight
 // Bound by DRAM where there are many tokens, by one thread's chain of latencies where there are few: XXX
 template <typename T, int N, bool INSIDE>
 __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const RopeParams p, int shares, int heads_a_block) {
-  constexpr int kUnits = INSIDE ? 1 : 2, kHeads = kUnitsAhead / kUnits, kAngles = INSIDE ? N / 2 : N;
+  constexpr int kUnits = INSIDE ? 1 : 2, kHeads = units_ahead(INSIDE) / kUnits, kAngles = INSIDE ? N / 2 : N;
   const long long at = static_cast<long long>(blockIdx.x) * kRopeThreads + threadIdx.x;
   const int token = static_cast<int>(at / shares), share = static_cast<int>(at - static_cast<long long>(token) * shares);
   if (token >= p.tokens) return;
@@ -189,9 +192,9 @@ cudaError_t launch_rope_units(const RopeParams& p, int sms, cudaStream_t stream)
   const int shares = INSIDE ? p.D / N : p.rot / 2 / N + (rest + 1) / 2;
   const int heads = p.heads + (p.k ? 2 * p.cache.heads : 0);
   const long long blocks = (static_cast<long long>(p.tokens) * shares + kRopeThreads - 1) / kRopeThreads;
-  // Angles cost as much as several heads, so a thread takes all of them where the tokens fill the chip kRopeBlocks blocks an
+  // Angles cost as much as several heads, so a thread takes all of them where the tokens fill the chip that many blocks an
   // SM; fewer tokens spread their heads over the blocks.
-  long long split = (static_cast<long long>(kRopeBlocks) * sms + blocks - 1) / blocks;
+  long long split = (static_cast<long long>(rope_blocks(INSIDE)) * sms + blocks - 1) / blocks;
   split = split < 1 ? 1 : split > heads ? heads : split;
   const int each = static_cast<int>((heads + split - 1) / split);
   const dim3 grid(static_cast<unsigned>(blocks), static_cast<unsigned>((heads + each - 1) / each));
