@@ -533,20 +533,21 @@ __device__ __forceinline__ uint32_t unit_offset(int row, int unit) {
   return (unit >> 3) * kHalfBytes + row * 128 + (((unit & 7) ^ (row & 7)) << 4);
 }
 
-// Rows row0 .. row0 + rows - 1 of a tile of queries into shared memory, by `threads` threads of which this is number `tid`:
-// 16 bytes each, zeros where there is no query and behind the last element.
+// A tile's queries into shared memory, by `threads` threads of which this is number `tid`: 16 bytes each, zeros behind the
+// last element.  Rows without a query keep what they hold: it reaches nobody.
 template <typename T>
-__device__ __forceinline__ void bring_queries(uint8_t* dst, int tile, int row0, int rows, const AttendParams& p,
-                                              const AttendSplit& sp, const Segment& g, int tid, int threads) {
+__device__ __forceinline__ void bring_queries(uint8_t* dst, int tile, const AttendParams& p, const AttendSplit& sp, const Segment& g,
+                                              int tid, int threads) {
   const int G = p.group, units = (p.cache.D + 15) / 16 * 2, step = threads / units;
-  const int unit = tid % units, tile_rows = sp.tile_tokens * G, inv_group = (65536 + G - 1) / G;  // row / G, rows below 128
+  const int unit = tid % units, tok0 = tile * sp.tile_tokens, rows = min(sp.tile_tokens, g.tokens - tok0) * G;
+  const int inv_group = (65536 + G - 1) / G;  // row / G, rows below 128
   if (tid / units < step)
 #pragma unroll 2
-    for (int row = row0 + tid / units; row < row0 + rows; row += step) {
-      const int tk = row * inv_group >> 16, tok = tile * sp.tile_tokens + tk;
-      const bool is = row < tile_rows && tok < g.tokens && 8 * unit < p.cache.D;
-      const T* const src = static_cast<const T*>(p.q) + (g.s.row + g.tok0 + tok) * p.q_stride +
+    for (int row = tid / units; row < rows; row += step) {
+      const int tk = row * inv_group >> 16;
+      const T* const src = static_cast<const T*>(p.q) + (g.s.row + g.tok0 + tok0 + tk) * p.q_stride +
                            static_cast<int64_t>(g.head * G + row - tk * G) * p.cache.D + 8 * unit;
+      const bool is = 8 * unit < p.cache.D;
       copy_async(dst + unit_offset(row, unit), is ? src : static_cast<const T*>(p.q), is);
     }
   asm volatile("cp.async.wait_all;" ::: "memory");
@@ -589,7 +590,7 @@ __device__ void line_warp(Shared* sh, uint8_t* q_smem, const AttendParams& p, co
       const unsigned use = queries[tile]++;
       if (index == 0 || sh->abort) continue;
       if (use > 0 && !warp_wait(sh, &sh->q_free[tile], (use - 1) & 1)) continue;
-      bring_queries<T>(q_smem + tile * kTileBytes, tile, 0, kAttendRows, p, sp, g, lane, 32);
+      bring_queries<T>(q_smem + tile * kTileBytes, tile, p, sp, g, lane, 32);
       warp_arrive(&sh->q_ready[tile]);
     }
   }
@@ -620,7 +621,7 @@ __device__ void soft_group(Shared* sh, uint8_t* q_smem, uint8_t* ring, const Att
     const int n = g.t1 - g.t0, ahead = two ? 1 : 2;
     const int tile = two ? w : 0;
     if (segment == 0) {  // everybody brings the first queries
-      bring_queries<T>(q_smem + tile * kTileBytes, tile, two ? 0 : 64 * w, two ? kAttendRows : 64, p, sp, g, r, 128);
+      bring_queries<T>(q_smem + tile * kTileBytes, tile, p, sp, g, two ? r : threadIdx.x, two ? 128 : kSoftThreads);
       if (!meet()) return;
       if (threadIdx.x == 0) mbar_arrive(&sh->q_ready[0]);
       if (threadIdx.x == 128 && two) mbar_arrive(&sh->q_ready[1]);
@@ -669,7 +670,7 @@ __device__ void soft_group(Shared* sh, uint8_t* q_smem, uint8_t* ring, const Att
           m = seen;
         } else {
           const float up = fmaxf(m, seen);
-          if (__any_sync(~0u, (up - m) * c > kGrowth)) {
+          if (__any_sync(~0u, valid && (up - m) * c > kGrowth)) {
             const float keep = m == up ? 1.f : ex2((m - up) * c);
             mbar_wait(&sh->o_done[w], (turn - 1) & 1, &sh->abort, &sh->code);
             tc_fence_after();
