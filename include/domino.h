@@ -410,7 +410,9 @@ DOMINO_API int domino_rope_append(const void* q, int64_t q_stride, const void* k
  *   a page of a sequence's keys lies outside [0, pages): the rows of that sequence are not specified,
  *   DOMINO_ERR_TIMEOUT; domino_check_status reads it).  domino_attend_workspace_bytes depends on the current device
  *   (0 without one, or for sizes that are refused), not on lengths.
- * Deterministic: the same call gives the same bits.  Two kernels on `stream`.  Returns as domino_rope. */
+ * Deterministic: the same call gives the same bits.  Two kernels on `stream` for every 1024 sequences.  Returns as
+ * domino_rope; DOMINO_ERR_UNSUPPORTED too for more than 128 query heads a head, 16384 query heads, or more work than 2e9
+ * units (heads x groups of at most 256 queries x (16 + 3 tiles of 128 places of the table)). */
 enum domino_mask { DOMINO_MASK_CAUSAL = 0, DOMINO_MASK_FULL = 1, DOMINO_MASK_TREE = 2 };
 DOMINO_API size_t domino_attend_workspace_bytes(int tokens, int q_heads, const domino_kv_cache* cache);
 DOMINO_API int domino_attend_paged(const void* q, int64_t q_stride, int tokens, int q_heads,
@@ -424,7 +426,7 @@ DOMINO_API int domino_attend_paged(const void* q, int64_t q_stride, int tokens, 
  *   accepted_nodes [B, N], accepted_count [B]: as domino_verify_tree_* write them (each entry above the one before).
  *   layer_stride: elements between layers, not looked at for one layer.  N <= 1048576.
  * Output: new_len int32 [B] = kv_len[b] - (n - 1) + accepted_count[b], the next step's length without its new tokens
- *   (n = 0 and none accepted: kv_len[b]); it may not be kv_len itself.  A sequence whose list is not rising, names a node
+ *   (n = 0 and none accepted: kv_len[b]); it may be neither kv_len nor accepted_count.  A sequence whose list is not rising, names a node
  *   outside the tree, whose places lie outside the table or in pages outside [0, pages), or whose count is out of range is
  *   left as it is, with new_len -1.
  * One kernel on `stream`, no workspace.  Returns as domino_rope. */

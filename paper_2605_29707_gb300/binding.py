@@ -174,12 +174,14 @@ def load():
 
 
 def _addr(x):
-    if x is None:
-        return None
+    if x is None or type(x) is int:
+        return x
+    try:
+        return x.data_ptr()
+    except AttributeError:
+        pass
     if isinstance(x, int):
         return x
-    if hasattr(x, "data_ptr"):
-        return x.data_ptr()
     if hasattr(x, "ctypes"):  # numpy array
         return x.ctypes.data
     raise TypeError(f"cannot take the address of {type(x)}")

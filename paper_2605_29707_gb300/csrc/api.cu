@@ -144,12 +144,24 @@ long long tree_capacity(int K, int k) {  // sum_{d=1..K} k^d, saturated
   return cap;
 }
 
+// The current device's SM count and compute capability.  They do not change: a device is asked once (1.5 us a call, which
+// small launches feel).
 int device_sms(int* sms, int* major, int* minor) {
+  constexpr int kKnown = 64;
+  static std::atomic<uint64_t> known[kKnown];  // SMs, major, minor in 16 bits each; 0: not asked yet
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess) return DOMINO_ERR_CUDA;
-  if (cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return DOMINO_ERR_CUDA;
-  if (cudaDeviceGetAttribute(major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess) return DOMINO_ERR_CUDA;
-  if (cudaDeviceGetAttribute(minor, cudaDevAttrComputeCapabilityMinor, dev) != cudaSuccess) return DOMINO_ERR_CUDA;
+  uint64_t v = dev >= 0 && dev < kKnown ? known[dev].load(std::memory_order_relaxed) : 0;
+  if (v == 0) {
+    if (cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return DOMINO_ERR_CUDA;
+    if (cudaDeviceGetAttribute(major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess) return DOMINO_ERR_CUDA;
+    if (cudaDeviceGetAttribute(minor, cudaDevAttrComputeCapabilityMinor, dev) != cudaSuccess) return DOMINO_ERR_CUDA;
+    v = static_cast<uint64_t>(*sms) << 32 | static_cast<uint64_t>(*major) << 16 | static_cast<uint64_t>(*minor);
+    if (dev >= 0 && dev < kKnown) known[dev].store(v, std::memory_order_relaxed);
+  }
+  *sms = static_cast<int>(v >> 32);
+  *major = static_cast<int>(v >> 16 & 0xffff);
+  *minor = static_cast<int>(v & 0xffff);
   return DOMINO_OK;
 }
 
@@ -956,6 +968,12 @@ int check_device(const void* logits) {
   const int rc = device_sms(&sms, &major, &minor);
   if (rc != DOMINO_OK) return rc;
   if (major != 10 || minor != 3) return DOMINO_ERR_UNSUPPORTED;
+  // (one device holds everything; the count does not change)
+  static const int devices = [] {
+    int n = 0;
+    return cudaGetDeviceCount(&n) == cudaSuccess ? n : 0;
+  }();
+  if (devices == 1) return DOMINO_OK;
   cudaPointerAttributes at{};
   if (cudaGetDevice(&dev) != cudaSuccess || cudaPointerGetAttributes(&at, logits) != cudaSuccess) return DOMINO_ERR_CUDA;
   return at.type == cudaMemoryTypeDevice && at.device != dev ? DOMINO_ERR_INVALID_ARG : DOMINO_OK;
@@ -1365,7 +1383,8 @@ int enqueue_attend_tc(const dm::AttendParams& a, const domino_kv_cache& c, int s
     const long long tiles = static_cast<long long>(a.batch.table_width) * c.page / dm::kAttendKeys + 1;
     const double units = static_cast<double>(groups) * (tiles * dm::kAttendTwoCost + dm::kAttendGroupCost) * c.heads;
     if (units > 2e9) return DOMINO_ERR_UNSUPPORTED;  // counted in 32 bits
-    const int rc = cuda_rc(dm::launch_attend_tc(keys, values, part, s, c.dtype, units < sms ? static_cast<int>(units) : sms, st));
+    const int grid = units / dm::kAttendLeast < sms ? static_cast<int>(units / dm::kAttendLeast) : sms;
+    const int rc = cuda_rc(dm::launch_attend_tc(keys, values, part, s, c.dtype, grid, st));
     if (rc != DOMINO_OK) return rc;
   }
   return DOMINO_OK;
@@ -1438,7 +1457,8 @@ int domino_cache_commit(const domino_kv_cache* cache, const domino_kv_batch* bat
   if (layers < 1 || N < 0 || N > (1 << 20) || !accepted_count || !new_len || (N > 0 && !accepted_nodes))
     return DOMINO_ERR_INVALID_ARG;
   if (layers > 32767) return DOMINO_ERR_UNSUPPORTED;
-  if (!stride_ok(layer_stride, layers, cache->head_dim) || new_len == batch->kv_len) return DOMINO_ERR_INVALID_ARG;
+  if (!stride_ok(layer_stride, layers, cache->head_dim) || new_len == batch->kv_len || new_len == accepted_count)
+    return DOMINO_ERR_INVALID_ARG;
   if (!aligned(accepted_nodes, 4) || !aligned(accepted_count, 4) || !aligned(new_len, 4)) return DOMINO_ERR_INVALID_ARG;
   rc = check_device(cache->k);
   if (rc != DOMINO_OK) return rc;

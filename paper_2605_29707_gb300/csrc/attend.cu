@@ -70,6 +70,7 @@ struct Shared {
   Sequence seq[kAttendSeqs];
 };
 constexpr size_t kSharedBytes = 1024 + static_cast<size_t>(2 + kStages) * kTileBytes + sizeof(Shared);
+static_assert(kSharedBytes <= 232448, "a CTA's shared memory");
 
 // Descriptors of 128-byte swizzled tiles differ in their low word alone (start address and, MN-major, the distance of
 // blocks): 32-bit sums step them.

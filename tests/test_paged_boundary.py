@@ -112,7 +112,7 @@ def test_attend_refusals(kw, code):
 
 @pytest.mark.parametrize("kw,code", [
     (dict(layers=0), BAD), (dict(layers=1 << 15), UNSUP), (dict(layer_stride=63), BAD), (dict(N=-1), BAD), (dict(N=(1 << 20) + 1), BAD),
-    (dict(accepted_nodes=None), BAD), (dict(accepted_count=None), BAD), (dict(new_len=None), BAD), (dict(new_len=P), BAD),
+    (dict(accepted_nodes=None), BAD), (dict(accepted_count=None), BAD), (dict(new_len=None), BAD), (dict(new_len=P), BAD), (dict(accepted_count=2 * P), BAD),
     (dict(accepted_nodes=P + 2), BAD), (dict(accepted_count=P + 2), BAD), (dict(new_len=2 * P + 2), BAD)])
 def test_commit_refusals(kw, code):
     assert _commit(**kw) == code
