@@ -9,7 +9,8 @@
 // O accumulator in tensor memory, and keeps one row a thread: with two tiles of queries each has its own and both take
 // every tile of keys; with one, the warpgroups take the tiles of keys in turn and add up at the end.  S = X K^T runs
 // with both operands in shared memory; the weights replace S in tensor memory and are the first operand of O += W V
-// there.  While one warpgroup takes its exponentials, the tensor core works for the other.  O is scaled down only where
+// there, half of the keys as soon as their weights stand.  While one warpgroup takes its exponentials, the tensor core works
+// for the other.  O is scaled down only where
 // the maximum has grown by more than 2^8 since m was set: the weights stay below 2^8, whose sums fp32 holds.
 //
 // Work is the line of all (sequence, head, group of queries, tile of keys), cut into equal stretches, one a CTA (one an SM):
@@ -58,7 +59,7 @@ struct Segment {
 };
 
 struct Shared {
-  uint64_t full[kStages], empty[kStages], s_full[2], w_ready[2], o_done[2], q_ready[2], q_free[2], seg_ready[kSegments],
+  uint64_t full[kStages], empty[kStages], s_full[2], w_half[2], w_ready[2], o_done[2], q_ready[2], q_free[2], seg_ready[kSegments],
       seg_done[kSegments], met;
   uint32_t tmem;
   int abort, code;
@@ -457,19 +458,20 @@ __device__ void multiply_warp(Shared* sh, uint32_t q_addr, uint32_t ring_addr, c
     }
     __syncwarp();
   };
-  // O of accumulator w, from its weights and the values in `stage`
-  auto weigh = [&](int w, int stage, bool add, bool last) {
+  // Half of O of accumulator w, from its weights of 64 keys and the values in `stage`
+  auto weigh = [&](int w, int half, int stage, bool add, bool last) {
     tc_fence_after();
-    const uint32_t b = desc_low(ring_addr + stage * kTileBytes, kHalfBytes);
+    const uint32_t b = desc_low(ring_addr + stage * kTileBytes + half * (kHalfBytes / 2), kHalfBytes);
     if (elect_one()) {
 #pragma unroll
-      for (int k = 0; k < kAttendKeys / 16; ++k)
-        mma_ts(tmem + kO + 128 * w, tmem + kS + 128 * w + 8 * k, b + k * (2048 >> 4), wv, k > 0 ? 1 : add);
-      tc_commit(&sh->o_done[w]);
-      if (last) tc_commit(&sh->empty[stage]);
+      for (int k = 0; k < kAttendKeys / 32; ++k)
+        mma_ts(tmem + kO + 128 * w, tmem + kS + 128 * w + 32 * half + 8 * k, b + k * (2048 >> 4), wv, k > 0 ? 1 : add);
+      if (half) tc_commit(&sh->o_done[w]);
+      if (half && last) tc_commit(&sh->empty[stage]);
     }
     __syncwarp();
   };
+  auto halves = [&](int w) { return warp_wait(sh, &sh->w_half[w], turns[w] & 1); };
   auto weights = [&](int w) { return warp_wait(sh, &sh->w_ready[w], turns[w]++ & 1); };
   auto queried = [&](int tile) { return warp_wait(sh, &sh->q_ready[tile], queries[tile]++ & 1); };
   const Segment* g;
@@ -485,17 +487,21 @@ __device__ void multiply_warp(Shared* sh, uint32_t q_addr, uint32_t ring_addr, c
       if (!queried(1)) return;
       scores(1, 1, k, true, n == 1);
       for (int j = 0; j < n; ++j) {
-        if (!weights(0)) return;
+        if (!halves(0)) return;
         const int v = take();
         if (v < 0) return;
-        weigh(0, v, j > 0, false);
+        weigh(0, 0, v, j > 0, false);
+        if (!weights(0)) return;
+        weigh(0, 1, v, true, false);
         if (j + 1 < n) {
           k = take();
           if (k < 0) return;
           scores(0, 0, k, false, j + 2 == n);
         }
+        if (!halves(1)) return;
+        weigh(1, 0, v, j > 0, true);
         if (!weights(1)) return;
-        weigh(1, v, j > 0, true);
+        weigh(1, 1, v, true, true);
         if (j + 1 < n) scores(1, 1, k, true, j + 2 == n);
       }
     } else {
@@ -506,10 +512,12 @@ __device__ void multiply_warp(Shared* sh, uint32_t q_addr, uint32_t ring_addr, c
       }
       for (int j = 0; j < n; ++j) {
         const int w = j & 1;
-        if (!weights(w)) return;
+        if (!halves(w)) return;
         const int v = take();
         if (v < 0) return;
-        weigh(w, v, j >= 2, true);
+        weigh(w, 0, v, j >= 2, true);
+        if (!weights(w)) return;
+        weigh(w, 1, v, true, true);
         if (j + 2 < n) {
           const int k = take();
           if (k < 0) return;
@@ -643,6 +651,28 @@ __device__ void soft_group(Shared* sh, uint8_t* q_smem, uint8_t* ring, const Att
       const bool masked = key0 + kAttendKeys > from;
       if (!warp_wait(sh, &sh->s_full[w], turn & 1)) return;
       tc_fence_after();
+      if (masked) {  // values that weights of 0 must not meet
+        const unsigned place = base + value_place(j, n, ahead);
+        const int stage = place % kStages, row0 = max(from - key0, 0);
+        if (!warp_wait(sh, &sh->full[stage], (place / kStages) & 1)) return;
+        if (unit_row < row_step)
+#pragma unroll 2
+          for (int row = row0 + unit_row; row < kAttendKeys; row += row_step) {
+            uint4* const at = reinterpret_cast<uint4*>(ring + stage * kTileBytes + unit_offset(row, unit));
+            if (key0 + row >= g.s.kv) {
+              *at = make_uint4(0, 0, 0, 0);
+            } else {
+              uint4 v = *at;
+              if (drop_odd<T>(&v.x) | drop_odd<T>(&v.y) | drop_odd<T>(&v.z) | drop_odd<T>(&v.w)) {
+                *reinterpret_cast<volatile unsigned*>(&sh->odd[segment & 1]) = segment + 1;
+                __threadfence_block();
+                *at = v;
+              }
+            }
+          }
+        fence_async_smem();
+        __syncwarp();
+      }
       auto softmax = [&](auto Masked) {
         constexpr bool kMasked = decltype(Masked)::value;
         float s[4][32], top[4];
@@ -703,6 +733,11 @@ __device__ void soft_group(Shared* sh, uint8_t* q_smem, uint8_t* ring, const Att
             pk[y / 2] = pack2(a, b, T());
           }
           tc_st_x32(s_col + 16 * x, pk);
+          if (x == 0) {
+            tc_wait_st();
+            tc_fence_before();
+            warp_arrive(&sh->w_half[w]);
+          }
         }
         l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
         tc_wait_st();
@@ -710,28 +745,9 @@ __device__ void soft_group(Shared* sh, uint8_t* q_smem, uint8_t* ring, const Att
       if (busy) {
         if (masked) softmax(std::true_type());
         else softmax(std::false_type());
-      }
-      if (masked) {  // values that weights of 0 must not meet
-        const unsigned place = base + value_place(j, n, ahead);
-        const int stage = place % kStages, row0 = max(from - key0, 0);
-        if (!warp_wait(sh, &sh->full[stage], (place / kStages) & 1)) return;
-        if (unit_row < row_step)
-#pragma unroll 2
-          for (int row = row0 + unit_row; row < kAttendKeys; row += row_step) {
-            uint4* const at = reinterpret_cast<uint4*>(ring + stage * kTileBytes + unit_offset(row, unit));
-            if (key0 + row >= g.s.kv) {
-              *at = make_uint4(0, 0, 0, 0);
-            } else {
-              uint4 v = *at;
-              if (drop_odd<T>(&v.x) | drop_odd<T>(&v.y) | drop_odd<T>(&v.z) | drop_odd<T>(&v.w)) {
-                *reinterpret_cast<volatile unsigned*>(&sh->odd[segment & 1]) = segment + 1;
-                __threadfence_block();
-                *at = v;
-              }
-            }
-          }
-        fence_async_smem();
-        __syncwarp();
+      } else {
+        tc_fence_before();
+        warp_arrive(&sh->w_half[w]);
       }
       tc_fence_before();
       warp_arrive(&sh->w_ready[w]);
@@ -852,6 +868,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(&sh->s_full[i], 1);
+      mbar_init(&sh->w_half[i], 4);
       mbar_init(&sh->w_ready[i], 4);  // a warp each
       mbar_init(&sh->o_done[i], 1);
       mbar_init(&sh->q_ready[i], 1);
