@@ -1380,7 +1380,8 @@ int enqueue_attend_tc(const dm::AttendParams& a, const domino_kv_cache& c, int s
     s.first = b == 0;
     // at most this much work: fewer CTAs where there is less of it than SMs
     const long long groups = a.tokens / (2 * plan.tile_tokens) + part.batch.B;
-    const long long tiles = static_cast<long long>(a.batch.table_width) * c.page / dm::kAttendKeys + 1;
+    const long long places = std::min(static_cast<long long>(a.batch.table_width) * c.page, 0x7fffff80LL);
+    const long long tiles = places / dm::kAttendKeys + 1;
     const double units = static_cast<double>(groups) * (tiles * dm::kAttendTwoCost + dm::kAttendGroupCost) * c.heads;
     if (units > 2e9) return DOMINO_ERR_UNSUPPORTED;  // counted in 32 bits
     const int grid = units / dm::kAttendLeast < sms ? static_cast<int>(units / dm::kAttendLeast) : sms;

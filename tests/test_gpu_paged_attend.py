@@ -1,5 +1,6 @@
 """Attention over a paged cache against its fp64 form; whatever no row sees is NaN in these caches."""
 import math
+import random
 
 import pytest
 import torch
@@ -63,6 +64,8 @@ SHAPES = [  # kv, new, hq, hkv, D, page, order
     ([333], [65], 128, 1, 128, 256, "pth"),
     ([2300], [2], 3, 1, 8, 128, "pth"),
     ([5000, 4999, 1], [1, 1, 1], 40, 8, 128, 16, "pht"),
+    ([450, 131], [9, 4], 65, 1, 64, 200, "pth"),
+    ([260, 1000], [150, 40], 6, 2, 104, 136, "pht"),
 ]
 
 
@@ -148,12 +151,13 @@ def test_growing_scores(dtype):
 @pytest.mark.parametrize("dtype", [b.DOMINO_BF16, b.DOMINO_F32])
 @pytest.mark.parametrize("mask", [CAUSAL, TREE])
 @pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
-def test_hidden_new_tokens_do_not_reach_other_rows(dtype, mask, bad):
+@pytest.mark.parametrize("hq", [4, 32])  # a tile of rows; two of them, and a second group
+def test_hidden_new_tokens_do_not_reach_other_rows(dtype, mask, bad, hq):
     """A new token's key and value hold NaN or infinities: rows that see it show them, the others are as without it."""
     p = ref.Paged([200, 300], [20, 20], 2, 64, dtype, 16, seed=11)
     parents = ref.random_trees(2, 19, 3)[0] if mask == TREE else None
     parent = torch.tensor(parents, dtype=torch.int32, device=DEV) if parents else None
-    q = randq(p.tokens, 4, 64, dtype, 11)
+    q = randq(p.tokens, hq, 64, dtype, 11)
     clean, _, _ = run(p, q, mask, parent, 19)
     token = 12
     page, off = int(p.table[1, (280 + token) // 16]), (280 + token) % 16
@@ -166,10 +170,10 @@ def test_hidden_new_tokens_do_not_reach_other_rows(dtype, mask, bad):
     second, was = out[20:], clean[20:]
     assert torch.equal(second[~see], was[~see])
     hit = second[see]
-    assert bool(hit[:, :2].isnan().all()) and bool(lse[20:][see][:, :2].isnan().all())
-    assert bool(hit[:, 2:, 5].isnan().all()) if math.isnan(bad) else bool((hit[:, 2:, 5] == bad).all())
+    assert bool(hit[:, :hq // 2].isnan().all()) and bool(lse[20:][see][:, :hq // 2].isnan().all())
+    assert bool(hit[:, hq // 2:, 5].isnan().all()) if math.isnan(bad) else bool((hit[:, hq // 2:, 5] == bad).all())
     rest = torch.arange(64, device=DEV) != 5
-    assert torch.equal(hit[:, 2:][..., rest], was[see][:, 2:][..., rest])
+    assert torch.equal(hit[:, hq // 2:][..., rest], was[see][:, hq // 2:][..., rest])
 
 
 def test_bad_pages_are_reported():
@@ -281,3 +285,49 @@ def test_short_workspace_is_refused():
     ws = torch.empty(n, dtype=torch.uint8, device=DEV)
     assert b.domino_attend_paged(q, 256, 3, 4, p.cache, p.batch, 1.0, CAUSAL, None, 0, torch.empty_like(q), 256, None, ws, n - 1, None) == \
         b.DOMINO_ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("seed", range(24))
+def test_random_batches(seed):
+    """Any mix of lengths, heads, pages and layouts."""
+    g = random.Random(seed)
+    dtype, mask = g.choice((b.DOMINO_BF16, b.DOMINO_F16)), g.choice((CAUSAL, FULL, TREE))
+    B, hkv, G = g.randint(1, 9), g.randint(1, 4), g.choice((1, 2, 3, 4, 5, 7, 8, 16, 33))
+    top = g.choice((1, 5, 40, 70))
+    new = [g.randint(0, top) for _ in range(B)]
+    kv = [max(0, n + g.choice((-2, 0, 1, 90, 127, 128, 700, 2000)) + g.randint(0, 3)) for n in new]
+    N = max(max(new) - g.randint(0, 2), 0)
+    p = ref.Paged(kv, new, hkv, 8 * g.randint(1, 16), dtype, 8 * g.choice((1, 2, 3, 5, 8, 16, 17, 32)),
+                  g.choice(("pth", "pht", "htp", "thp")), g.choice((0, 8, 24)), seed=seed)
+    parents = ref.random_trees(B, N, seed)[0] if mask == TREE else None
+    check(p, randq(p.tokens + g.randint(0, 2) + (p.tokens == 0), hkv * G, p.D, dtype, seed), mask, parents)
+
+
+def test_two_calls_at_once():
+    """Two streams, a workspace each: the results of either alone."""
+    ps = [ref.Paged([4000, 300], [33, 1], 4, 128, b.DOMINO_BF16, 16, seed=30 + i) for i in range(2)]
+    qs = [randq(34, 16, 128, b.DOMINO_BF16, 30 + i) for i in range(2)]
+    want = [run(p, q, CAUSAL) for p, q in zip(ps, qs)]
+    n = b.domino_attend_workspace_bytes(34, 16, ps[0].cache)
+    ws = [torch.empty(n, dtype=torch.uint8, device=DEV) for _ in range(2)]
+    outs, lses = [torch.empty_like(q) for q in qs], [torch.empty((34, 16), device=DEV) for _ in qs]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for i in range(2):
+            assert b.domino_attend_paged(qs[i], qs[i].stride(0), 34, 16, ps[i].cache, ps[i].batch, 128 ** -0.5, CAUSAL, None, 0, outs[i],
+                                         outs[i].stride(0), lses[i], ws[i], n, streams[i]) == 0
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert torch.equal(outs[i], want[i][0]) and torch.equal(lses[i], want[i][1])
+
+
+def test_a_refused_amount_of_work():
+    """Sizes whose line of work does not fit 32 bits are refused before anything is enqueued."""
+    p = ref.Paged([30] * 64, [1] * 64, 2, 64, b.DOMINO_BF16, 16, seed=20)  # 64 groups x 2 heads x 3 x 2^24 tiles of the table
+    batch = b.make_batch(p.table, 1 << 30, 1 << 30, p.kv_len, p.start, 64)
+    q = randq(64, 4, 64, b.DOMINO_BF16, 20)
+    n = b.domino_attend_workspace_bytes(64, 4, p.cache)
+    ws = torch.empty(n, dtype=torch.uint8, device=DEV)
+    assert b.domino_attend_paged(q, 256, 64, 4, p.cache, batch, 1.0, CAUSAL, None, 0, torch.empty_like(q), 256, None, ws, n, None) == \
+        b.DOMINO_ERR_UNSUPPORTED
