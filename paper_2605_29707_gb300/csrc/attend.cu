@@ -21,6 +21,23 @@
 // values nobody vouches for (places behind the last key, tokens of other branches), so in such tiles whatever is not
 // finite, or lies behind the last key, is set to 0 in shared memory, and rows that do see such a value get it added at the
 // end from the cache.
+//
+// Warps: eight for the softmax, one that brings keys, one values (TMA, a copy a piece of a page and 64 elements), one that
+// issues the products, one that walks the line, describes the segments to the others and brings the next one's queries.
+//
+// What bounds it (device time; floors at the measured copy and cuBLAS rates).  Single tokens: DRAM; 64 sequences of up to 8192
+// keys 176 us, 6.1 TB/s.  Long chunks: the tensor core and, over seconds, the power limit; 4096 tokens over 32768 keys 1310-1380
+// us in short runs, 1.50-1.57 PFLOP/s, 1465 when repeated for a second.  There two tiles of queries take 2700 cycles a tile of
+// keys without any softmax (the products' operands and the incoming tiles are 126 of the 128 bytes a cycle that shared
+// memory gives) and 3000 with it.  Trees and short chunks: what a segment costs besides its tiles, some 13000 cycles (queries,
+// masks, the last products, the results), and with the one token that a tree of 2^k nodes has over, a second group that reads
+// all keys again: 64 trees of 32 nodes, 64 heads on 8, 230 us at 5 TB/s, twice their bytes.  One short call: the chain of launch,
+// lengths, page, keys, softmax and join, 13 us.
+//
+// Tried and left out, us of the long chunk at the time: steering the products by one thread alone 1849 (the whole warp 1309); one
+// loop for both kinds of group 1460 (written out 1319); reading the scores twice from tensor memory 1583 (once 1370); two
+// threads a row 1440 (one 1372); queries as whole tiles with zeros, results through shared memory, keys backwards in every other
+// group (no gain).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <math.h>
@@ -35,7 +52,7 @@
 namespace dm {
 namespace {
 
-constexpr int kStages = 4;          // tiles of keys or values in flight
+constexpr int kStages = 4;          // tiles of keys or values in flight: 128 KB beside 64 KB of queries
 constexpr int kHalfBytes = 16384;   // 128 rows of 64 elements
 constexpr int kTileBytes = 2 * kHalfBytes;
 constexpr int kSoftThreads = 256;
@@ -44,7 +61,9 @@ constexpr int kThreads = kSoftThreads + 128;  // and two warps for keys and valu
 // 2 x 128 x 192 + 128 x 120 = 384 x 168.
 constexpr int kSoftRegs = 192, kOtherRegs = 120;
 constexpr int kS = 0, kO = 256;     // tensor memory columns: S of warpgroup w at 128 w, O at 256 + 128 w
-constexpr float kGrowth = 8.f;      // log2 of what a maximum may grow before O is scaled
+// log2 of what a maximum may grow before O is scaled.  fp16 weights of 2^8 are far from 65504, bf16's and the sums' range is
+// fp32's; scaling at every growth would wait for the products in most of the first tiles.
+constexpr float kGrowth = 8.f;
 
 constexpr int kSegments = 2;        // segments described ahead
 constexpr int kTreeWords = 3;       // a token's ancestors among the first 96 new tokens, a bit each
@@ -977,6 +996,8 @@ constexpr int kJoinAhead = 4;  // partial results in flight
 constexpr int kJoinWarps = kJoinThreads / 32, kJoinElems = 4;  // elements a thread
 constexpr int kJoinCols = kJoinWarps * kJoinElems;             // and a block
 
+// Bound by the latency of its loads: 3.8 us for one token's 8 parts of 8 heads, 8 for 8 groups of 19 parts, 15-20 for 152 groups of
+// two or three parts of 256 rows.
 // The group that CTA blockIdx.x began and others went on with: 32 of its rows' sums over all of them, in their order.  Rows
 // lie side by side in the slots: a lane takes a row, a warp four elements of a block's 32; the results turn round in shared
 // memory.

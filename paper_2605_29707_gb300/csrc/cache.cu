@@ -77,7 +77,10 @@ __host__ __device__ constexpr int rope_blocks(bool inside) { return inside ? 6 :
 // of x, then those of k, then those of v.  A share is a unit of N elements that holds pairs of neighbours (INSIDE), or
 // two units whose elements pair up; the units behind the turned ones, and all of v's, are copied.  The first heads are on
 // their way while the angles are computed.
-// Bound by DRAM where there are many tokens, by one thread's chain of latencies where there are few: XXX
+// Bound by DRAM where there are many tokens, by one thread's chain of latencies (sequence, page, heads) where there are few:
+// 12003 tokens of 48 fp16 heads into a cache 49.3 us, 6.0 TB/s; the gradient of 16384 x 32 bf16 heads 46.4 us, 5.8 TB/s; 3001 x
+// 14 heads of 80 fp32 elements 5.9 us; 17 tokens of 48 heads 4.7 us.  Angles in shared memory, or a thread for every head,
+// were not needed: a thread's angles are some 480 instructions among 2000.
 template <typename T, int N, bool INSIDE>
 __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const RopeParams p, int shares, int heads_a_block) {
   constexpr int kUnits = INSIDE ? 1 : 2, kHeads = units_ahead(INSIDE) / kUnits, kAngles = INSIDE ? N / 2 : N;
@@ -230,7 +233,8 @@ struct MoveUnit {
 // the targets of all moves before it: moves may read ahead of the earlier ones' writes, and a thread that reads eight
 // before it writes them leaves every unit what one move after the other would.
 // Bound by the chain of look-ups (sequence, list, table, keys) where little moves, by DRAM's rate on short rows where much
-// does: XXX
+// does: 64 sequences' nodes in 64 layers 13.4 us, 5.4 TB/s of what moves; 28 layers of one sequence 3.0 us.  With the places looked
+// up by every thread for itself, and a block a layer's keys or values, the two took 38 and 5.4 us.
 template <typename U>
 __global__ void __launch_bounds__(kCommitThreads) commit_kernel(const CommitParams p, int units, int layers_a_block) {
   using E = typename U::elem;
