@@ -78,8 +78,8 @@ struct Segment {
 };
 
 struct Shared {
-  uint64_t full[kStages], empty[kStages], s_full[2], w_half[2], w_ready[2], o_done[2], q_ready[2], q_free[2], seg_ready[kSegments],
-      seg_done[kSegments], met;
+  uint64_t full[kStages], empty[kStages], s_full[2], w_half[2], w_ready[2], o_done[2], q_ready[2], q_free[2];
+  uint64_t seg_ready[kSegments], seg_done[kSegments], met;
   uint32_t tmem;
   int abort, code;
   unsigned odd[2];  // by the segment's parity: the segment, from 1 on, that met a value that is not finite in a masked tile
@@ -564,8 +564,8 @@ __device__ __forceinline__ uint32_t unit_offset(int row, int unit) {
 // A tile's queries into shared memory, by `threads` threads of which this is number `tid`: 16 bytes each, zeros behind the
 // last element.  Rows without a query keep what they hold: it reaches nobody.
 template <typename T>
-__device__ __forceinline__ void bring_queries(uint8_t* dst, int tile, const AttendParams& p, const AttendSplit& sp, const Segment& g,
-                                              int tid, int threads) {
+__device__ __forceinline__ void bring_queries(uint8_t* dst, int tile, const AttendParams& p, const AttendSplit& sp,
+                                              const Segment& g, int tid, int threads) {
   const int G = p.group, units = (p.cache.D + 15) / 16 * 2, step = threads / units;
   const int unit = tid % units, tok0 = tile * sp.tile_tokens, rows = min(sp.tile_tokens, g.tokens - tok0) * G;
   const int inv_group = (65536 + G - 1) / G;  // row / G, rows below 128
@@ -839,9 +839,10 @@ __device__ void soft_group(Shared* sh, uint8_t* q_smem, uint8_t* ring, const Att
       }
     if (odd && valid) {  // what was left out of the products, where this row sees it
       const int end = min(g.s.kv, g.t1 * kAttendKeys);
+      const int32_t* const parent = p.parent ? p.parent + static_cast<long long>(g.seq) * p.N : nullptr;
 #pragma unroll 1
       for (int key = max(masked_from(p, g.s, g.tok0), g.t0 * kAttendKeys); key < end; ++key) {
-        if (!sees(p.mask, p.parent ? p.parent + static_cast<long long>(g.seq) * p.N : nullptr, p.N, i, static_cast<long long>(g.s.kv) - g.s.n, key)) continue;
+        if (!sees(p.mask, parent, p.N, i, static_cast<long long>(g.s.kv) - g.s.n, key)) continue;
         const long long off = place_offset(p.cache, p.batch, g.seq, key);
         if (off < 0) continue;
         const T* const v = static_cast<const T*>(p.cache.v) + off + g.head * p.cache.head_stride;
@@ -956,8 +957,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
   }
   __syncthreads();
-  const int units = sh->before[p.batch.B], each = max(kAttendLeast, (units + static_cast<int>(gridDim.x) - 1) / static_cast<int>(gridDim.x));
-  const int from = static_cast<int>(blockIdx.x) < (units + each - 1) / each ? static_cast<int>(blockIdx.x) * each : units;
+  const int units = sh->before[p.batch.B], ctas = gridDim.x, cta = blockIdx.x;
+  const int each = max(kAttendLeast, (units + ctas - 1) / ctas), from = cta < (units + each - 1) / each ? cta * each : units;
   Line line;
   line.begin(sh, p, sp, from, from + min(each, units - from));
   if (tid < kSoftThreads) {
@@ -993,19 +994,19 @@ __global__ void __launch_bounds__(kThreads, 1)
 constexpr int kJoinThreads = 256;
 constexpr int kJoinRows = 32;  // rows a block: a lane a row
 constexpr int kJoinAhead = 4;  // partial results in flight
-constexpr int kJoinWarps = kJoinThreads / 32, kJoinElems = 4;  // elements a thread
-constexpr int kJoinCols = kJoinWarps * kJoinElems;             // and a block
+constexpr int kJoinElems = 4;  // elements a thread
 
-// Bound by the latency of its loads: 3.8 us for one token's 8 parts of 8 heads, 8 for 8 groups of 19 parts, 15-20 for 152 groups of
-// two or three parts of 256 rows.
-// The group that CTA blockIdx.x began and others went on with: 32 of its rows' sums over all of them, in their order.  Rows
-// lie side by side in the slots: a lane takes a row, a warp four elements of a block's 32; the results turn round in shared
-// memory.
-template <typename T>
+// Bound by the latency of its loads: 2.5 us for one token's 8 parts of 8 heads, some 4 for 8 groups of 19 parts (5.7 with one way),
+// 15-20 for 152 groups of two or three parts of 256 rows.
+// The group that CTA blockIdx.x began and others went on with: 32 of its rows' sums over all of them, in a fixed order.  Rows
+// lie side by side in the slots: a lane takes a row, a warp four elements and every WAYS-th part; the ways meet and the
+// results turn round in shared memory.  Few rows have many parts: four ways.
+template <typename T, int WAYS>
 __global__ void __launch_bounds__(kJoinThreads) join_kernel(const AttendParams p, const AttendSplit sp) {
-  __shared__ float s_out[kJoinRows][kJoinCols + 1];
+  constexpr int kCols = kJoinThreads / 32 / WAYS * kJoinElems;  // elements a block
+  __shared__ float s_o[WAYS][kJoinRows][kCols + 1], s_m[WAYS][kJoinRows], s_l[WAYS][kJoinRows];
   asm volatile("griddepcontrol.wait;" ::: "memory");
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, way = warp % WAYS, cols = warp / WAYS * kJoinElems;
   if (blockIdx.x == 0 && blockIdx.y == 0 && blockIdx.z == 0 && warp == 0) {
     int code = 0;
     for (unsigned i = lane; i < gridDim.x; i += 32) {
@@ -1018,23 +1019,24 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const AttendParams p
   }
   const AttendTail tail = sp.tails[blockIdx.x];
   const int D = p.cache.D, G = p.group, rows = tail.tokens * G, first = blockIdx.x, row0 = blockIdx.y * kJoinRows;
-  const int col0 = blockIdx.z * kJoinCols, d = col0 + warp * kJoinElems;  // D is a multiple of 8: four elements, or none
+  const int col0 = blockIdx.z * kCols, d = col0 + cols;  // D is a multiple of 8: four elements, or none
   if (tail.last < 0 || row0 >= rows) return;
   const long long slot_rows = sp.slot_rows;
-  const int at = min(row0 + lane, rows - 1), tok = at / G, h = at - tok * G;
+  const int at = min(row0 + lane, rows - 1), tok = at / G;
   const int slot_row = tok < sp.tile_tokens ? at : kAttendRows + at - sp.tile_tokens * G;
   float m = -INFINITY, l = 0.f, o[kJoinElems];
 #pragma unroll
   for (int e = 0; e < kJoinElems; ++e) o[e] = 0.f;
-  for (int i0 = first; i0 <= tail.last; i0 += kJoinAhead) {
+  for (int i0 = first + way; i0 <= tail.last; i0 += WAYS * kJoinAhead) {
     float mi[kJoinAhead], li[kJoinAhead], v[kJoinAhead][kJoinElems];
 #pragma unroll
     for (int i = 0; i < kJoinAhead; ++i) {
-      if (i0 + i > tail.last) {
+      const int cta = i0 + WAYS * i;
+      if (cta > tail.last) {
         mi[i] = -INFINITY;
         continue;
       }
-      const long long slot = i0 + i == first ? 2 * first + 1 : 2 * (i0 + i);
+      const long long slot = cta == first ? 2 * first + 1 : 2 * cta;
       const float* const norm = sp.norms + slot * 2 * slot_rows + slot_row;
       const float* const part = sp.parts + (slot * D + d) * slot_rows + slot_row;
       mi[i] = norm[0];
@@ -1059,23 +1061,47 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const AttendParams p
       for (int e = 0; e < kJoinElems; ++e) o[e] = fmaf(v[i][e], f, o[e]);
     }
   }
+  if (cols == 0) {
+    s_m[way][lane] = m;
+    s_l[way][lane] = l;
+  }
+#pragma unroll
+  for (int e = 0; e < kJoinElems; ++e) s_o[way][lane][cols + e] = o[e];
+  __syncthreads();
+  const int r = threadIdx.x / (kCols / 8), x = threadIdx.x % (kCols / 8) * 8;
+  if (r >= kJoinRows || row0 + r >= rows || col0 + x >= D) return;
+  m = s_m[0][r];
+#pragma unroll
+  for (int w = 1; w < WAYS; ++w) m = fmaxf(m, s_m[w][r]);
+  float y[8] = {};
+  l = 0.f;
+#pragma unroll
+  for (int w = 0; w < WAYS; ++w) {
+    const float mw = s_m[w][r];
+    if (mw == -INFINITY) continue;
+    const float f = mw == m ? 1.f : ex2((mw - m) * p.scale_log2);
+    l = fmaf(s_l[w][r], f, l);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[e] = fmaf(s_o[w][r][x + e], f, y[e]);
+  }
   const float inv = 1.f / l;
 #pragma unroll
-  for (int e = 0; e < kJoinElems; ++e)
-    s_out[lane][warp * kJoinElems + e] = l == 0.f ? 0.f : o[e] * inv;
-  if (p.lse && blockIdx.z == 0 && warp == 0 && row0 + lane < rows)
-    p.lse[(tail.row + tok) * static_cast<long long>(p.hq) + tail.head * G + h] = l == 0.f ? -INFINITY : fmaf(m, p.scale, logf(l));
-  __syncthreads();
-  const int r = threadIdx.x / (kJoinCols / 8), x = threadIdx.x % (kJoinCols / 8) * 8;
-  if (r >= kJoinRows || row0 + r >= rows || col0 + x >= D) return;
+  for (int e = 0; e < 8; ++e) y[e] = l == 0.f ? 0.f : y[e] * inv;
   const int tk = (row0 + r) / G, head = tail.head * G + row0 + r - tk * G;
-  float y[8];
-#pragma unroll
-  for (int e = 0; e < 8; ++e) y[e] = s_out[r][x + e];
+  const long long row = tail.row + tk;
   Vec<T> v;
   pack(y, &v);
-  *reinterpret_cast<uint4*>(static_cast<T*>(p.out) + static_cast<long long>(tail.row + tk) * p.out_stride +
-                            static_cast<long long>(head) * D + col0 + x) = v.raw;
+  *reinterpret_cast<uint4*>(static_cast<T*>(p.out) + row * p.out_stride + static_cast<long long>(head) * D + col0 + x) = v.raw;
+  if (p.lse && col0 + x == 0) p.lse[row * p.hq + head] = l == 0.f ? -INFINITY : fmaf(m, p.scale, logf(l));
+}
+
+template <typename T, int WAYS>
+cudaError_t launch_join(cudaLaunchConfig_t cfg, const AttendParams& p, const AttendSplit& s, int grid) {
+  constexpr int kCols = kJoinThreads / 32 / WAYS * kJoinElems;
+  cfg.gridDim = dim3(grid, (s.slot_rows + kJoinRows - 1) / kJoinRows, (p.cache.D + kCols - 1) / kCols);
+  cfg.blockDim = dim3(kJoinThreads);
+  cfg.dynamicSmemBytes = 0;
+  return cudaLaunchKernelEx(&cfg, join_kernel<T, WAYS>, p, s);
 }
 
 template <typename T>
@@ -1095,10 +1121,7 @@ cudaError_t launch_tc_type(const CUtensorMap& keys, const CUtensorMap& values, c
   cfg.numAttrs = 1;
   e = cudaLaunchKernelEx(&cfg, attend_kernel<T>, keys, values, p, s);
   if (e != cudaSuccess) return e;
-  cfg.gridDim = dim3(grid, (s.slot_rows + kJoinRows - 1) / kJoinRows, (p.cache.D + kJoinCols - 1) / kJoinCols);
-  cfg.blockDim = dim3(kJoinThreads);
-  cfg.dynamicSmemBytes = 0;
-  return cudaLaunchKernelEx(&cfg, join_kernel<T>, p, s);
+  return s.slot_rows <= kAttendRows ? launch_join<T, 4>(cfg, p, s, grid) : launch_join<T, 1>(cfg, p, s, grid);
 }
 
 }  // namespace
