@@ -412,7 +412,7 @@ DOMINO_API int domino_rope_append(const void* q, int64_t q_stride, const void* k
  *   (0 without one, or for sizes that are refused), not on lengths.
  * Deterministic: the same call gives the same bits.  Two kernels on `stream` for every 1024 sequences.  Returns as
  * domino_rope; DOMINO_ERR_UNSUPPORTED too for more than 128 query heads a head, 16384 query heads, or more work than 2e9
- * units (heads x groups of at most 256 queries x (16 + 3 tiles of 128 places of the table)). */
+ * units (heads x groups of at most 256 queries x (12 + 3 tiles of 128 places of the table)). */
 enum domino_mask { DOMINO_MASK_CAUSAL = 0, DOMINO_MASK_FULL = 1, DOMINO_MASK_TREE = 2 };
 DOMINO_API size_t domino_attend_workspace_bytes(int tokens, int q_heads, const domino_kv_cache* cache);
 DOMINO_API int domino_attend_paged(const void* q, int64_t q_stride, int tokens, int q_heads,

@@ -375,7 +375,7 @@ constexpr int kAttendRows = 128;   // queries a tile
 constexpr int kAttendSeqs = 1024;  // sequences a launch
 // Units of work, about 1000 cycles each: a tile of keys with two tiles of queries, with one; a group of queries beside
 // its tiles; the least that a CTA takes (a stretch holds the beginning of a tile of any kind).
-constexpr int kAttendTwoCost = 3, kAttendOneCost = 2, kAttendGroupCost = 16, kAttendLeast = 3;
+constexpr int kAttendTwoCost = 3, kAttendOneCost = 2, kAttendGroupCost = 12, kAttendLeast = 3;
 struct AttendTail {  // a group of queries whose keys go on behind the CTA that began them
   int last;          // the CTA that ends them, -1: none
   int row, head, tokens;
