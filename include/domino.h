@@ -403,7 +403,7 @@ DOMINO_API int domino_rope_append(const void* q, int64_t q_stride, const void* k
  *     scale > 0, finite, with scale log2(e) normal in fp32.
  * bf16 and fp16 products run on the tensor cores where head_dim <= 128 and page are multiples of 8 and pointers and
  * strides multiples of 16 bytes: scores, maxima, sums and accumulators in fp32, the weights of the second product
- * rounded to dtype, one rounding at the end.  Everything else takes a plain kernel, in fp32 throughout, a warp a row:
+ * rounded to dtype, one rounding at the end.  Everything else takes a plain kernel, in fp32 throughout, a block a row:
  * right, and slow on long caches.
  * workspace: device memory of domino_attend_workspace_bytes(...) bytes, 256-byte aligned, of one call at a time; what
  *   it holds before does not matter.  Its first int32 receives the device status (DOMINO_OK, DOMINO_ERR_BAD_PAGE where
