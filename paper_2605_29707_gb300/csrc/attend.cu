@@ -82,6 +82,7 @@ struct Shared {
   uint64_t seg_ready[kSegments], seg_done[kSegments], met;
   uint32_t tmem;
   int abort, code;
+  unsigned used[2][kStages];  // keys, values: the last copy into a stage, plus 1
   unsigned odd[2];  // by the segment's parity: the segment, from 1 on, that met a value that is not finite in a masked tile
   float norm[2][2][kAttendRows];  // accumulator: maximum, sum
   Segment seg[kSegments];
@@ -392,7 +393,7 @@ __device__ void load_warp(Shared* sh, uint8_t* ring, const CUtensorMap* map, boo
   const uint32_t bytes = two_halves ? kTileBytes : kHalfBytes;
   const int pages_on = kAttendKeys / page_size, places_on = kAttendKeys % page_size;
   const uint64_t keep = l2_policy_evict_last(), drop = l2_policy_evict_first();
-  unsigned base = 0, used[kStages] = {};  // used: our last copy into a stage, plus 1
+  unsigned base = 0, used[kStages] = {};
   bool ok = true;
   const Segment* g;
   for (unsigned index = 0; ok && (g = next_segment(sh, index)) != nullptr; ++index) {
@@ -440,10 +441,9 @@ __device__ void load_warp(Shared* sh, uint8_t* ring, const CUtensorMap* map, boo
     base += 2 * n;
     segment_done(sh, index);
   }
-  if (sh->abort)  // nothing of ours stays in flight
+  if (lane == 0)
 #pragma unroll
-    for (int i = 0; i < kStages; ++i)
-      if (used[i]) drain_wait(&sh->full[i], ((used[i] - 1) / kStages) & 1);
+    for (int i = 0; i < kStages; ++i) sh->used[values][i] = used[i];
 }
 
 // The whole warp follows the segments, one thread issues: what steers the products stays in uniform registers.  The tensor core
@@ -983,7 +983,14 @@ __global__ void __launch_bounds__(kThreads, 1)
   __syncwarp();
   tc_fence_before();
   __syncthreads();
-  if (tid == 0) sp.codes[blockIdx.x] = sh->code;
+  if (tid == 0) {
+    sp.codes[blockIdx.x] = sh->code;
+    if (sh->abort)  // copies that nobody has waited for write into this CTA's memory
+      for (int i = 0; i < kStages; ++i) {
+        const unsigned last = max(sh->used[0][i], sh->used[1][i]);
+        if (last) drain_wait(&sh->full[i], ((last - 1) / kStages) & 1);
+      }
+  }
   if (warp == kSoftThreads / 32) {
     tc_fence_after();
     tmem_dealloc(sh->tmem, 512);
