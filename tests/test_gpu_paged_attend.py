@@ -228,11 +228,40 @@ def test_without_lse():
     assert torch.equal(run(p, q, FULL, lse=False)[0], run(p, q, FULL)[0])
 
 
-def test_many_sequences():
+@pytest.mark.parametrize("mask", [CAUSAL, TREE])
+def test_many_sequences(mask):
+    """More than one launch takes; a bad page of the first launch's sequences shows after the second."""
     n = 1500
     kv = [1 + (i * 37) % 90 for i in range(n)]
     p = ref.Paged(kv, [1 + i % 2 if kv[i] > 1 else i % 2 for i in range(n)], 1, 64, b.DOMINO_BF16, 16, seed=17)
-    check(p, randq(p.tokens, 2, 64, b.DOMINO_BF16, 17), CAUSAL)
+    parents = ref.random_trees(n, 1, 3)[0] if mask == TREE else None
+    q = randq(p.tokens, 2, 64, b.DOMINO_BF16, 17)
+    check(p, q, mask, parents)
+    good = int(p.table[5, 0])
+    p.table[5, 0] = -1
+    parent = torch.tensor(parents, dtype=torch.int32, device=DEV) if parents else None
+    assert run(p, q, mask, parent, 1)[2] == b.DOMINO_ERR_BAD_PAGE
+    p.table[5, 0] = good
+    check(p, q, mask, parents)
+
+
+def test_a_long_prompt_in_one_call():
+    """9000 tokens from the first place on, 8 heads on one: rows of every group against the 64-bit form."""
+    n, hq, D = 9000, 8, 64
+    p = ref.Paged([n], [n], 1, D, b.DOMINO_BF16, 64, seed=21)
+    q = randq(n, hq, D, b.DOMINO_BF16, 21)
+    out, lse, status = run(p, q, CAUSAL)
+    assert status == 0
+    k, v = p.read(p.k, 0)[:, 0].double(), p.read(p.v, 0)[:, 0].double()
+    u = torch.finfo(torch.bfloat16).eps / 2
+    for i in sorted({0, 1, 15, 16, 31, 32, 127, 128, 129, 4095, 4096, 8191, 8998, 8999} | set(range(7, n, 613))):
+        z = (q[i].double() @ k[:i + 1].T) * D ** -0.5
+        l = torch.logsumexp(z, 1)
+        w = (z - l[:, None]).exp()
+        want, A = w @ v[:i + 1], w @ v[:i + 1].abs()
+        e = 2 * (D + 8) * 2.0 ** -24 * (q[i].double().abs() @ k[:i + 1].abs().T).amax(1) * D ** -0.5 + 2.0 ** -20
+        assert bool(((out[i].double() - want).abs() <= u * want.abs() + (u + e[:, None]) * A).all()), i
+        assert bool(((lse[i].double() - l).abs() <= e / 2 + 2.0 ** -23 * l.abs()).all()), i
 
 
 def test_offsets_beyond_32_bits():
