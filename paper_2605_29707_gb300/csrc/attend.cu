@@ -789,6 +789,10 @@ __device__ void soft_group(Shared* sh, uint8_t* q_smem, uint8_t* ring, const Att
       f1 = m1 == -INFINITY ? 0.f : m1 == m ? 1.f : ex2((m1 - m) * c);
       l = sh->norm[0][1][r] * f0 + sh->norm[1][1][r] * f1;
     }
+    if (p.mask == kMaskTree && i > p.N) {  // past the tree: nothing seen, though tiles before the new tokens ask no mask
+      m = -INFINITY;
+      l = 0.f;
+    }
     const bool odd = *reinterpret_cast<volatile unsigned*>(&sh->odd[segment & 1]) == segment + 1;
     const bool whole = g.t0 == 0 && g.t1 == g.tiles;
     const float inv = l == 0.f ? 0.f : 1.f / l;
