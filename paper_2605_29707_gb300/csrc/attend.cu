@@ -1045,6 +1045,7 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const AttendParams p
       const int cta = i0 + WAYS * i;
       if (cta > tail.last) {
         mi[i] = -INFINITY;
+        li[i] = 0.f;
         continue;
       }
       const long long slot = cta == first ? 2 * first + 1 : 2 * cta;
@@ -1065,7 +1066,8 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const AttendParams p
     for (int e = 0; e < kJoinElems; ++e) o[e] *= keep;
 #pragma unroll
     for (int i = 0; i < kJoinAhead; ++i) {
-      if (mi[i] == -INFINITY) continue;  // no part, or one that saw nothing: sums of 0
+      // no part, or one that saw nothing: sums of 0.  (A NaN score is no maximum: it shows in the sum alone.)
+      if (mi[i] == -INFINITY && li[i] == 0.f) continue;
       const float f = mi[i] == m ? 1.f : ex2((mi[i] - m) * p.scale_log2);
       l = fmaf(li[i], f, l);
 #pragma unroll
@@ -1089,7 +1091,7 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const AttendParams p
 #pragma unroll
   for (int w = 0; w < WAYS; ++w) {
     const float mw = s_m[w][r];
-    if (mw == -INFINITY) continue;
+    if (mw == -INFINITY && s_l[w][r] == 0.f) continue;
     const float f = mw == m ? 1.f : ex2((mw - m) * p.scale_log2);
     l = fmaf(s_l[w][r], f, l);
 #pragma unroll
