@@ -331,7 +331,9 @@ DOMINO_API int domino_verify_tree_filtered(const void* target_logits, int dtype,
  *     they are only read.  kv_len [B], start [B + 1] (from 0 on, not falling): device int32, the sequences of a batch
  *     one after another; n may be 0.  Rows from start[B] on are left as they are.
  * The structures are host memory and may be freed after the call.  What the device finds out of range is cut off:
- * start at the token tensors' ends, kv_len at table_width page (and at 2^31 - 128); nothing outside the tensors is touched. */
+ * start at the token tensors' ends, keys at table_width page places (and at 2^31 - 128); nothing outside the tensors is
+ * touched.  A sequence may thus run past its table: its new tokens keep their places kv_len[b] - n + i, those past the
+ * table without a key.  Only where kv_len[b] - n itself lies past the table, kv_len[b] counts as the table's places. */
 typedef struct domino_kv_cache {
   void* k;
   void* v;

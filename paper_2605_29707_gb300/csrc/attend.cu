@@ -205,7 +205,7 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi, __half) {
 // Keys that some token below `last` of a sequence sees, in tiles; a group that sees none still has one, for its rows'
 // zeros.
 __device__ __forceinline__ int key_tiles(int mask, const Sequence& s, int last) {
-  const int seen = mask == kMaskCausal ? min(max(s.kv - s.n + last, 0), s.kv) : s.kv;
+  const int seen = mask == kMaskCausal ? min(max(s.first + last, 0), s.kv) : s.kv;
   return max(1, seen / kAttendKeys + (seen % kAttendKeys != 0));
 }
 
@@ -315,7 +315,7 @@ __device__ __forceinline__ int sequence_units(const AttendParams& p, const Atten
 // The first key that some token from tok0 on may not see.
 __device__ __forceinline__ int masked_from(const AttendParams& p, const Sequence& s, int tok0) {
   if (p.mask == kMaskFull) return s.kv;
-  return min(max(s.kv - s.n + (p.mask == kMaskCausal ? tok0 + 1 : 0), 0), s.kv);
+  return min(max(s.first + (p.mask == kMaskCausal ? tok0 + 1 : 0), 0), s.kv);
 }
 
 // Whether a tree's tokens have their ancestors in `above`.
@@ -326,10 +326,10 @@ __device__ __forceinline__ bool tree_in_words(const AttendParams& p, const Segme
 // Which of 128 keys from key0 on token i sees, a bit each.
 __device__ __forceinline__ void seen_bits(const AttendParams& p, const Segment& g, const uint32_t* above, int i, int key0,
                                           uint32_t (&bits)[4]) {
-  const int first = g.s.kv - g.s.n;
+  const int first = g.s.first;
   int limit = g.s.kv;  // every key below it is seen
   if (p.mask == kMaskCausal) limit = min(max(first + i + 1, 0), g.s.kv);
-  if (p.mask == kMaskTree) limit = i > p.N ? 0 : max(first, 0);
+  if (p.mask == kMaskTree) limit = i > p.N ? 0 : min(max(first, 0), g.s.kv);
 #pragma unroll
   for (int w = 0; w < 4; ++w) {
     const int n = limit - key0 - 32 * w;
@@ -343,6 +343,8 @@ __device__ __forceinline__ void seen_bits(const AttendParams& p, const Segment& 
       const uint32_t lo = word >= 0 && word < kTreeWords ? above[word] : 0;
       const uint32_t hi = word >= -1 && word < kTreeWords - 1 ? above[word + 1] : 0;
       bits[w] |= __funnelshift_r(lo, hi, t & 31);
+      const int n = g.s.kv - key0 - 32 * w;  // new tokens past the table have no key
+      if (n < 32) bits[w] &= n <= 0 ? 0u : (1u << n) - 1;
     }
     return;
   }
@@ -353,7 +355,7 @@ __device__ __forceinline__ void seen_bits(const AttendParams& p, const Segment& 
     const uint32_t bit = 1u << (at & 31);
 #pragma unroll
     for (int w = 0; w < 4; ++w)
-      if (at >> 5 == w) bits[w] |= bit;
+      if (at >> 5 == w && key0 + at < g.s.kv) bits[w] |= bit;
     if (a == 0) break;
   }
 }
@@ -846,7 +848,7 @@ __device__ void soft_group(Shared* sh, uint8_t* q_smem, uint8_t* ring, const Att
       const int32_t* const parent = p.parent ? p.parent + static_cast<long long>(g.seq) * p.N : nullptr;
 #pragma unroll 1
       for (int key = max(masked_from(p, g.s, g.tok0), g.t0 * kAttendKeys); key < end; ++key) {
-        if (!sees(p.mask, parent, p.N, i, static_cast<long long>(g.s.kv) - g.s.n, key)) continue;
+        if (!sees(p.mask, parent, p.N, i, g.s.first, key)) continue;
         const long long off = place_offset(p.cache, p.batch, g.seq, key);
         if (off < 0) continue;
         const T* const v = static_cast<const T*>(p.cache.v) + off + g.head * p.cache.head_stride;

@@ -31,7 +31,7 @@ __global__ void __launch_bounds__(32 * kRowWarps) attend_rows_kernel(const Atten
   const Sequence s = load_sequence(c, p.batch, p.tokens, seq);
   const int i = token - s.row;
   if (i < 0 || i >= s.n) return;
-  const long long first = static_cast<long long>(s.kv) - s.n;
+  const long long first = s.first;
   const int32_t* const parent = p.parent ? p.parent + static_cast<long long>(seq) * p.N : nullptr;
   const T* const q = static_cast<const T*>(p.q) + token * p.q_stride + static_cast<long long>(head) * c.D;
   for (int d = threadIdx.x; d < c.D; d += 32 * kRowWarps) s_q[d] = to_f32(q[d]);

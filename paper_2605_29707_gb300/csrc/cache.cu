@@ -95,7 +95,7 @@ __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const RopeParams p, 
     const int seq = find_sequence(p.batch, token);
     if (seq < 0) return;  // a row behind the last sequence
     const Sequence s = load_sequence(p.cache, p.batch, p.tokens, seq);
-    const int i = token - s.row, first = s.kv - s.n;
+    const int i = token - s.row, first = s.first;
     pos = first + i;
     dst = place_offset(p.cache, p.batch, seq, pos);
     if (p.depth && i >= 1 && i <= p.N) pos = first + p.depth[static_cast<long long>(seq) * p.N + i - 1];

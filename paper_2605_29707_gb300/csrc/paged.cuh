@@ -12,18 +12,22 @@ __device__ __forceinline__ int table_places(const PagedCache& c, const PagedBatc
 }
 
 struct Sequence {
-  int row;  // its first new token's row
-  int n;    // new tokens
-  int kv;   // keys, the new ones among them
+  int row;    // its first new token's row
+  int n;      // new tokens
+  int kv;     // keys, the new ones among them
+  int first;  // its first new token's place: kv - n, or more where the last ones lie past the table
 };
 
-// What the batch says of sequence b, cut off at the tensors' ends.
+// What the batch says of sequence b, cut off at the tensors' ends.  Keys end with the table, and new tokens keep their
+// places even so; only a length whose keys before the new ones pass the table is taken for the table's end.
 __device__ __forceinline__ Sequence load_sequence(const PagedCache& c, const PagedBatch& b, int tokens, int seq) {
   const int s0 = b.start[seq], s1 = b.start[seq + 1], kv = b.kv_len[seq];
   Sequence s;
   s.row = min(max(s0, 0), tokens);
   s.n = min(max(s1, s.row), tokens) - s.row;
-  s.kv = min(max(kv, 0), table_places(c, b));
+  const int places = table_places(c, b), first = max(kv, 0) - s.n;
+  s.kv = min(max(kv, 0), places);
+  s.first = first <= places ? first : s.kv - s.n;
   return s;
 }
 
