@@ -356,8 +356,8 @@ typedef struct domino_kv_batch {
  *   DOMINO_ROPE_HALF: the pair is (x[i], x[i + rot / 2]);  DOMINO_ROPE_PAIRS: (x[2 i], x[2 i + 1]).
  * freq and amplitude carry any stretching for long contexts (positions divided by a factor, speeds blended by
  * frequency, amplitudes scaled with its logarithm).  gradient != 0 turns back, by -a: applied to the gradient by y it
- * gives the gradient by x.  The angle is taken modulo a turn exactly, at any position; cos, sin and the products in
- * fp32, one rounding to dtype.
+ * gives the gradient by x.  The angle is taken modulo a turn, good to |p| 2^-64 of a turn at any speed; cos, sin and
+ * the products in fp32, one rounding to dtype.
  *   x, y: device of `dtype`, element-aligned, [tokens][heads][head_dim] with strides in elements between tokens and
  *     between heads (each at least head_dim; one whose extent is 1 is not looked at); y may be x with the same strides,
  *     and shares no memory with it otherwise.  positions: device int32 [tokens], any sign.  freq: device fp32

@@ -4,8 +4,8 @@
 // Rotary positions.  Pair i of a token at position p turns by a = p f_i, cos and sin times an amplitude:
 //   (y0, y1) = (x0 cos a - x1 sin a, x1 cos a + x0 sin a).
 // At p = 2^20 the fp32 product p f_i is wrong by 0.03 radians, so the angle is kept as a fraction of a turn in 64-bit
-// fixed point: F_i = f_i / (2 pi) modulo 1, from f_i's 24-bit mantissa and 64 bits of 1 / (2 pi), in integers; p F_i
-// modulo 2^64 is the angle, exact but for F_i's last bit, 2^-33 of a turn at p = 2^31.  The nearest quarter turn comes off in
+// fixed point: F_i = f_i / (2 pi) modulo 1, from f_i's 24-bit mantissa and 96 bits of 1 / (2 pi), in integers; p F_i
+// modulo 2^64 is the angle, exact but for F_i's last bit, 2^-33 of a turn at p = 2^31, at any speed.  The nearest quarter turn comes off in
 // integers too, and cos and sin of the rest, at most an eighth of a turn, are taken in fp32.
 #include <math.h>
 
@@ -22,12 +22,14 @@ constexpr int kRopeThreads = 256;
 
 // f / (2 pi) in units of 2^-64 of a turn, modulo a turn: f = m 2^e with m below 2^24, |f| <= 1024.
 __device__ __forceinline__ uint64_t turn_speed(float f) {
-  constexpr uint64_t kInv2Pi = 0x28BE60DB9391054AULL;  // floor(2^64 / (2 pi))
+  constexpr uint64_t kInv2Pi = 0x28BE60DB9391054AULL;  // floor(2^64 / (2 pi)), and its next 32 bits
+  constexpr uint32_t kInv2PiNext = 0x7F09D5F4u;
   const uint32_t bits = __float_as_uint(f);
   const int be = (bits >> 23) & 0xff;
   const uint64_t m = be ? (bits & 0x7fffffu) | 0x800000u : bits & 0x7fffffu;
   const int down = 150 - (be ? be : 1);  // f = m 2^-down
-  const uint64_t lo = kInv2Pi * m, hi = __umul64hi(kInv2Pi, m);
+  const uint32_t next = __umulhi(kInv2PiNext, static_cast<uint32_t>(m));  // what speeds above 1 bring up
+  const uint64_t lo = kInv2Pi * m + next, hi = __umul64hi(kInv2Pi, m) + (lo < next ? 1 : 0);
   uint64_t F;
   if (down <= 0) F = -down < 64 ? lo << -down : 0;
   else if (down < 64) F = (lo >> down) | (hi << (64 - down));
