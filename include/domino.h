@@ -168,7 +168,8 @@ DOMINO_API int domino_draft_step_host(const void* hidden_host, const int32_t* pr
 
 /* Synchronises `stream` and returns the device status word of the last step that used
  * `workspace`: DOMINO_OK, DOMINO_ERR_BAD_TOKEN or DOMINO_ERR_TIMEOUT (DOMINO_ERR_CUDA if the
- * read itself fails).  Each domino_draft_step clears the word when it starts. */
+ * read itself fails).  Each domino_draft_step clears the word when it starts.  The same for the workspace
+ * of domino_attend_paged (DOMINO_ERR_BAD_PAGE too), which every call sets. */
 DOMINO_API int domino_check_status(const void* workspace, void* stream);
 
 /* Failure-detection test hook; the paper has no counterpart.  It lets a test check that a
@@ -188,6 +189,10 @@ DOMINO_API int domino_check_status(const void* workspace, void* stream);
  *                              for the copy runs out, the row is read directly instead, and the
  *                              outputs are those of any other call; rows that are not copied so
  *                              (V not a multiple of 4) withhold nothing;
+ *   DOMINO_HOLD_KEY_TILE       CTA gru_cta of the next domino_attend_paged launch on the tensor cores does
+ *                              not bring its first tile of keys; its waits run out, the other CTAs
+ *                              are as ever, the call's workspace shows DOMINO_ERR_TIMEOUT and the
+ *                              rows that the CTA had part in are undefined;
  *   DOMINO_HOLD_OFF            disarms the hook.
  * The held CTA disarms the hook when its launch ends, so it affects one step.  Every kernel of
  * the held step still completes (its outputs are undefined) and the workspace stays usable: the
@@ -197,7 +202,8 @@ enum domino_hold {
   DOMINO_HOLD_OFF = 0,
   DOMINO_HOLD_STATE = 1,
   DOMINO_HOLD_CLEAR_BARRIER = 2,
-  DOMINO_HOLD_ROW_COPY = 3
+  DOMINO_HOLD_ROW_COPY = 3,
+  DOMINO_HOLD_KEY_TILE = 4
 };
 DOMINO_API int domino_debug_hold(int what, int gru_cta, int step);
 

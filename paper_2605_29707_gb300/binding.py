@@ -58,6 +58,7 @@ DOMINO_HOLD_OFF = 0
 DOMINO_HOLD_STATE = 1
 DOMINO_HOLD_CLEAR_BARRIER = 2
 DOMINO_HOLD_ROW_COPY = 3
+DOMINO_HOLD_KEY_TILE = 4
 
 KERNEL_KINDS = ("gather", "gru_input_proj", "w1_hidden_proj", "gru", "vocab_gemm_softmax_topk", "merge_tree",
                 "rollout_base_gemm", "rollout_steps", "tree_verify", "sample_filtered", "distill",
@@ -438,5 +439,6 @@ def domino_debug_hold(what, gru_cta=-1, step=-1) -> int:
     """Test hook: the next GRU launch's CTA ``gru_cta`` withholds its states of position ``step``
     (DOMINO_HOLD_STATE) or its clear-barrier arrival (DOMINO_HOLD_CLEAR_BARRIER); DOMINO_HOLD_OFF
     disarms.  The step then reports DOMINO_ERR_TIMEOUT through its device status.
-    DOMINO_HOLD_ROW_COPY: the next sampled verification does not stage part of row ``gru_cta``."""
+    DOMINO_HOLD_ROW_COPY: the next sampled verification does not stage part of row ``gru_cta``.
+    DOMINO_HOLD_KEY_TILE: CTA ``gru_cta`` of the next attention on the tensor cores lacks its first tile of keys."""
     return int(load().domino_debug_hold(int(what), int(gru_cta), int(step)))

@@ -861,11 +861,17 @@ int domino_abi_version(void) { return DOMINO_ABI_VERSION; }
 int domino_debug_hold(int what, int gru_cta, int step) {
   if (what == DOMINO_HOLD_OFF) {
     dm::arm_row_hold(-1);
+    dm::arm_attend_hold(-1);
     return cuda_rc(dm::arm_gru_hold(dm::kHoldOff, -1, -1));
   }
   if (what == DOMINO_HOLD_ROW_COPY) {  // gru_cta: the row
     if (gru_cta < 0) return DOMINO_ERR_INVALID_ARG;
     dm::arm_row_hold(gru_cta);
+    return DOMINO_OK;
+  }
+  if (what == DOMINO_HOLD_KEY_TILE) {
+    if (gru_cta < 0) return DOMINO_ERR_INVALID_ARG;
+    dm::arm_attend_hold(gru_cta);
     return DOMINO_OK;
   }
   if (what != DOMINO_HOLD_STATE && what != DOMINO_HOLD_CLEAR_BARRIER) return DOMINO_ERR_INVALID_ARG;

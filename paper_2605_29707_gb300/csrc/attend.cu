@@ -42,6 +42,7 @@
 #include <cuda_fp16.h>
 #include <math.h>
 
+#include <atomic>
 #include <type_traits>
 
 #include "kernels.h"
@@ -395,6 +396,7 @@ __device__ void load_warp(Shared* sh, uint8_t* ring, const CUtensorMap* map, boo
   const uint32_t bytes = two_halves ? kTileBytes : kHalfBytes;
   const int pages_on = kAttendKeys / page_size, places_on = kAttendKeys % page_size;
   const uint64_t keep = l2_policy_evict_last(), drop = l2_policy_evict_first();
+  const unsigned held = !values && sp.held == static_cast<int>(blockIdx.x) ? 0u : ~0u;  // test hook: the copy withheld
   unsigned base = 0, used[kStages] = {};
   bool ok = true;
   const Segment* g;
@@ -427,10 +429,10 @@ __device__ void load_warp(Shared* sh, uint8_t* ring, const CUtensorMap* map, boo
       ok = at < kStages || warp_wait(sh, &sh->empty[stage], (at / kStages - 1) & 1);
       if (!ok) break;
       uint8_t* dst = ring + stage * kTileBytes;
-      if (elect_one()) mbar_arrive_expect_tx(&sh->full[stage], bytes);
+      if (at != held && elect_one()) mbar_arrive_expect_tx(&sh->full[stage], bytes);
       __syncwarp();
 #pragma unroll 1
-      for (int q = 0; q < pieces; ++q, dst += sp.piece * 128) {
+      for (int q = at != held ? 0 : pieces; q < pieces; ++q, dst += sp.piece * 128) {
         const int y = __shfl_sync(~0u, here, q), w = __shfl_sync(~0u, page, q);
         if (elect_one()) {
           tma_load_4d(dst, map, &sh->full[stage], 0, y, head, w, policy);
@@ -1141,8 +1143,14 @@ cudaError_t launch_tc_type(const CUtensorMap& keys, const CUtensorMap& values, c
 
 }  // namespace
 
+// Test hook state (domino_debug_hold): the CTA of the next launch that withholds its first tile of keys; -1: none.
+static std::atomic<int> g_held_cta{-1};
+void arm_attend_hold(int cta) { g_held_cta = cta; }
+
 cudaError_t launch_attend_tc(const CUtensorMap& keys, const CUtensorMap& values, const AttendParams& p,
-                             const AttendSplit& s, int dtype, int grid, cudaStream_t stream) {
+                             const AttendSplit& split, int dtype, int grid, cudaStream_t stream) {
+  AttendSplit s = split;
+  s.held = g_held_cta.load(std::memory_order_relaxed) < 0 ? -1 : g_held_cta.exchange(-1);
   if (dtype == kBf16) return launch_tc_type<__nv_bfloat16>(keys, values, p, s, grid, stream);
   return launch_tc_type<__half>(keys, values, p, s, grid, stream);
 }

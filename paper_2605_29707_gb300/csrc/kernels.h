@@ -385,11 +385,14 @@ struct AttendSplit {
   int tile_tokens; // tokens of a tile of queries: 128 / group
   int slot_rows;   // rows of a partial result
   int first;       // the call's first launch: later ones keep an earlier error
+  int held;        // test hook: the CTA whose first tile of keys is not brought, -1: none
   int* codes;         // [grid] a CTA's status
   AttendTail* tails;  // [grid]
   float* norms;       // [2 grid][2][slot_rows] maximum and sum
   float* parts;       // [2 grid][D][slot_rows]
 };
+// Test hook (domino_debug_hold): the next launch withholds the first tile of keys of CTA `cta` (-1: disarmed).
+void arm_attend_hold(int cta);
 // keys, values: tensor maps (element, token, head, page) with boxes of 64 elements and `piece` tokens.
 cudaError_t launch_attend_tc(const CUtensorMap& keys, const CUtensorMap& values, const AttendParams& p,
                              const AttendSplit& s, int dtype, int grid, cudaStream_t stream);
