@@ -9,6 +9,7 @@
 // integers too, and cos and sin of the rest, at most an eighth of a turn, are taken in fp32.
 #include <math.h>
 
+#include <algorithm>
 #include <type_traits>
 
 #include "kernels.h"
@@ -303,9 +304,10 @@ template <typename U>
 cudaError_t launch_commit_units(const CommitParams& p, int sms, cudaStream_t stream) {
   const long long slots = static_cast<long long>(kCommitBlocks) * sms;
   const long long each = (static_cast<long long>(p.layers) * p.batch.B + slots - 1) / slots;
-  const int layers = static_cast<int>(each > p.layers ? p.layers : each);
+  const int units = p.cache.heads * p.cache.D / U::kN, most = (1 << 30) / (2 * units);  // a block counts units in 32 bits
+  const int layers = static_cast<int>(std::min({each, static_cast<long long>(p.layers), static_cast<long long>(most)}));
   const dim3 grid(static_cast<unsigned>(p.batch.B), static_cast<unsigned>((p.layers + layers - 1) / layers));
-  commit_kernel<U><<<grid, kCommitThreads, 0, stream>>>(p, p.cache.heads * p.cache.D / U::kN, layers);
+  commit_kernel<U><<<grid, kCommitThreads, 0, stream>>>(p, units, layers);
   return cudaGetLastError();
 }
 
