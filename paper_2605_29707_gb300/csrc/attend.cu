@@ -63,7 +63,8 @@ constexpr int kThreads = kSoftThreads + 128;  // and two warps for keys and valu
 constexpr int kSoftRegs = 192, kOtherRegs = 120;
 constexpr int kS = 0, kO = 256;     // tensor memory columns: S of warpgroup w at 128 w, O at 256 + 128 w
 // log2 of what a maximum may grow before O is scaled.  fp16 weights of 2^8 are far from 65504, bf16's and the sums' range is
-// fp32's; scaling at every growth would wait for the products in most of the first tiles.
+// fp32's; scaling at every growth would wait for the products in most of the first tiles.  (Leaving small growths to the
+// end's division is a published method.)
 constexpr float kGrowth = 8.f;
 
 constexpr int kSegments = 2;        // segments described ahead

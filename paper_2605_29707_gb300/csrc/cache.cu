@@ -73,6 +73,8 @@ struct Unit {
 // Loads of a thread in flight, and blocks an SM that share the heads out: neighbours in one unit, or two units that pair up.
 // us at 4 / 8 / 16 loads (8 blocks) and 4 / 8 / 16 blocks (the loads as chosen): 12003 tokens x 48 fp16 heads in a cache, pairs
 // of neighbours, 50.5 / 49.6 / 56.8 and 52.8 / 49.6 / 50.3; 16384 x 32 bf16 heads, halves, 47.4 / 53.5 / 73.3 and 45.9 / 47.4 / 48.6.
+// Units of 16 bytes take 54 to 68 registers, so 3 or 4 blocks of the 4 or 6 are on an SM at once; that was weighed on these
+// large calls alone, and small ones end unevenly (3001 x 14 fp32 heads: 940 blocks, a wave and a half).
 __host__ __device__ constexpr int units_ahead(bool inside) { return inside ? 8 : 4; }
 __host__ __device__ constexpr int rope_blocks(bool inside) { return inside ? 6 : 4; }
 
@@ -82,7 +84,7 @@ __host__ __device__ constexpr int rope_blocks(bool inside) { return inside ? 6 :
 // their way while the angles are computed.
 // Bound by DRAM where there are many tokens, by one thread's chain of latencies (sequence, page, heads) where there are few:
 // 12003 tokens of 48 fp16 heads into a cache 49.3 us, 6.0 TB/s; the gradient of 16384 x 32 bf16 heads 46.4 us, 5.8 TB/s; 3001 x
-// 14 heads of 80 fp32 elements 5.9 us; 17 tokens of 48 heads 4.7 us.  Angles in shared memory, or a thread for every head,
+// 14 heads of 80 fp32 elements 5.9 us from L2 (9.4 from DRAM, 1.5 TB/s); 17 tokens of 48 heads 4.7 us.  Angles in shared memory, or a thread for every head,
 // were not needed: a thread's angles are some 480 instructions among 2000.
 template <typename T, int N, bool INSIDE>
 __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const RopeParams p, int shares, int heads_a_block) {
@@ -235,9 +237,11 @@ struct MoveUnit {
 // for all layers; a thread takes one unit of a place through all moves.  The list rises, so node j's source lies behind
 // the targets of all moves before it: moves may read ahead of the earlier ones' writes, and a thread that reads eight
 // before it writes them leaves every unit what one move after the other would.
-// Bound by the chain of look-ups (sequence, list, table, keys) where little moves, by DRAM's rate on short rows where much
-// does: 64 sequences' nodes in 64 layers 13.4 us, 5.4 TB/s of what moves; 28 layers of one sequence 3.0 us.  With the places looked
-// up by every thread for itself, and a block a layer's keys or values, the two took 38 and 5.4 us.
+// Bound by the chain of look-ups (sequence, list, table, keys) where little moves, by a thread's loads in flight where much
+// does (a layer's moves of a sequence, 0 to 8, before the next layer's): 64 sequences' nodes in 64 layers 18.0 us with the
+// rows in DRAM, 4.0 TB/s of the 73 MB that move, and 13.4 us with them in L2, which holds them when the call is repeated;
+// 28 layers of one sequence 3.0 us.  With the places looked up by every thread for itself, and a block a layer's keys or
+// values, the two took 38 and 5.4 us (repeated).
 template <typename U>
 __global__ void __launch_bounds__(kCommitThreads) commit_kernel(const CommitParams p, int units, int layers_a_block) {
   using E = typename U::elem;

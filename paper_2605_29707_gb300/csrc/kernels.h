@@ -397,7 +397,7 @@ void arm_attend_hold(int cta);
 cudaError_t launch_attend_tc(const CUtensorMap& keys, const CUtensorMap& values, const AttendParams& p,
                              const AttendSplit& s, int dtype, int grid, cudaStream_t stream);
 
-// Any type and layout: a warp a row.  Status already cleared.
+// Any type and layout: a block of eight warps a row.  Status already cleared.
 cudaError_t launch_attend_rows(const AttendParams& p, int dtype, bool vector, cudaStream_t stream);
 
 }  // namespace dm

@@ -1,6 +1,7 @@
 // rows.cuh -- building blocks of the kernels that work on rows of vocabulary logits split over a
 // cluster of CTAs (sample.cuh, distill.cu): element types, units of 16 bytes, accesses to the cluster's
-// shared memory, and reductions and scans over a block.
+// shared memory, and reductions and scans over a block.  The operators on a paged cache (cache.cu, attend.cu,
+// attend_rows.cu) take the element types and units from here.
 #pragma once
 
 #include <cuda_bf16.h>
