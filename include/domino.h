@@ -408,7 +408,7 @@ DOMINO_API int domino_rope_append(const void* q, int64_t q_stride, const void* k
  * included, does not reach it, NaN and infinities neither.
  *   q [tokens][q_heads][head_dim] of the cache's dtype, heads contiguous, with its token stride; out likewise (it may be q with
  *     the same stride); lse fp32 [tokens][q_heads] or NULL.  q_heads a multiple of heads, at most 128 times as many.
- *     scale > 0, finite, with scale log2(e) normal in fp32.
+ *     scale > 0, finite, with scale log2(e) normal in fp32; scores, scale q . k_j, below 2e38 in size.
  * bf16 and fp16 products run on the tensor cores where head_dim <= 128 and page are multiples of 8 and pointers and
  * strides multiples of 16 bytes: scores, maxima, sums and accumulators in fp32, the weights of the second product
  * rounded to dtype, one rounding at the end.  Everything else takes a plain kernel, in fp32 throughout, a block a row:
