@@ -339,7 +339,7 @@ DOMINO_API int domino_verify_tree_filtered(const void* target_logits, int dtype,
  * The structures are host memory and may be freed after the call.  What the device finds out of range is cut off:
  * start at the token tensors' ends, keys at table_width page places (and at 2^31 - 128); nothing outside the tensors is
  * touched.  A sequence may thus run past its table: its new tokens keep their places kv_len[b] - n + i, those past the
- * table without a key.  Only where kv_len[b] - n itself lies past the table, kv_len[b] counts as the table's places. */
+ * table without a key.  Only a kv_len[b] of 2^30 and more with kv_len[b] - n past the table counts as the table's places. */
 typedef struct domino_kv_cache {
   void* k;
   void* v;

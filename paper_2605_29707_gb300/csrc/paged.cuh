@@ -11,6 +11,8 @@ __device__ __forceinline__ int table_places(const PagedCache& c, const PagedBatc
   return n > 0x7fffff80LL ? 0x7fffff80 : static_cast<int>(n);
 }
 
+constexpr int kNoLength = 1 << 30;
+
 struct Sequence {
   int row;    // its first new token's row
   int n;      // new tokens
@@ -19,7 +21,7 @@ struct Sequence {
 };
 
 // What the batch says of sequence b, cut off at the tensors' ends.  Keys end with the table, and new tokens keep their
-// places even so; only a length whose keys before the new ones pass the table is taken for the table's end.
+// places even so; only what is no length, 2^30 and more past a table that holds fewer, is taken for the table's end.
 __device__ __forceinline__ Sequence load_sequence(const PagedCache& c, const PagedBatch& b, int tokens, int seq) {
   const int s0 = b.start[seq], s1 = b.start[seq + 1], kv = b.kv_len[seq];
   Sequence s;
@@ -27,7 +29,7 @@ __device__ __forceinline__ Sequence load_sequence(const PagedCache& c, const Pag
   s.n = min(max(s1, s.row), tokens) - s.row;
   const int places = table_places(c, b), first = max(kv, 0) - s.n;
   s.kv = min(max(kv, 0), places);
-  s.first = first <= places ? first : s.kv - s.n;
+  s.first = first <= places || kv < kNoLength ? first : s.kv - s.n;
   return s;
 }
 

@@ -15,7 +15,8 @@ DEV = "cuda"
 CAUSAL, FULL, TREE = b.DOMINO_MASK_CAUSAL, b.DOMINO_MASK_FULL, b.DOMINO_MASK_TREE
 
 # pages, page, new tokens, tokens past the table
-ENDS = [(4, 16, 4, 2), (4, 16, 4, 4), (4, 16, 1, 1), (5, 7, 12, 11), (3, 64, 33, 1), (1, 8, 20, 3)]
+ENDS = [(4, 16, 4, 2), (4, 16, 4, 4), (4, 16, 1, 1), (5, 7, 12, 11), (3, 64, 33, 1), (1, 8, 20, 3),
+        (4, 16, 1, 2), (4, 16, 1, 900), (5, 7, 6, 7), (2, 128, 40, 5000)]  # the tokens before these are past it already
 
 
 def _full(pages, page, n, past, hkv, D, dtype, seed):
